@@ -442,6 +442,131 @@ som_status som_update_finish_f16(uint16_t* W, int64_t F, int64_t ldw, int32_t ro
                                  size_t ws_bytes, hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * Dense documents: the layer between states of a language model (dense rows
+ * in 16 or 8 bits) and a map's features, forward and backward.  Matrices are
+ * row-major with a row stride in elements (ld >= columns); neither the stride
+ * nor the base has to be aligned beyond the element, but rows that start on
+ * 16 bytes are read fastest.  No element beyond a row's last column is read.
+ * Sums, statistics and activations are in fp32; each
+ * output is rounded once.  Zero rows are a valid no-op unless stated.  Results
+ * do not depend on other work on the device: no floating-point atomics.
+ * ------------------------------------------------------------------------- */
+
+typedef enum som_dtype {
+  SOM_F32 = 0,
+  SOM_F16 = 1,  /* IEEE binary16 */
+  SOM_BF16 = 2,
+  SOM_E4M3 = 3  /* 8 bits, 4 of exponent: largest value 448, no infinities */
+} som_dtype;
+
+typedef enum som_act {
+  SOM_ACT_NONE = 0,
+  SOM_ACT_RELU = 1,
+  SOM_ACT_GELU = 2,      /* v (1 + erf(v / sqrt 2)) / 2 */
+  SOM_ACT_GELU_TANH = 3, /* v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2 */
+  SOM_ACT_SILU = 4       /* v / (1 + exp(-v)) */
+} som_act;
+
+/* Root-mean-square norm with the residual's addition:
+ *
+ *     h = x + residual,  s = 1 / sqrt(mean_c h_c^2 + eps),  y_c = h_c s weight_c.
+ *
+ * x, residual (may be NULL), h (may be NULL: not written) and weight [cols]
+ * (NULL: all ones) are of type `dtype` (fp32, fp16 or bf16); the norm is taken of
+ * the sum before its rounding to h.  h may be x or residual themselves (same
+ * stride), which updates a residual stream in place.  y is of type `dtype`, or
+ * with q8 of 8 bits (SOM_E4M3) with an fp32 factor for each row: y = q scale[row], scale
+ * = max_c |y_c| / 448 (1 for a row of zeros).  scale is NULL without q8.
+ * A row holding a NaN or an infinity gives NaNs.  1 <= cols < 2^31. */
+som_status som_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
+                        int32_t dtype, int64_t rows, int64_t cols, float eps, int32_t q8, void* y, int64_t ldy,
+                        void* h, int64_t ldh, float* scale, hipStream_t stream);
+
+/* Its gradient, from the stored h and the gradients dy of y and dh of h (NULL: none):
+ *
+ *     g = dy weight,  dx = s g - h s^3 mean_c(g h) + dh,  dweight_c = sum_rows dy h s.
+ *
+ * dx (of type `dtype`, as dy, h, dh and weight are) is the gradient of x and of the residual
+ * alike; dweight [cols] (fp32) may be NULL.  An output in 8 bits is differentiated as
+ * if it were not rounded.  dx may be dy or dh (same stride).  With rows == 0
+ * dweight is set to zero.  ws: som_rms_norm_backward_workspace_bytes(rows, cols),
+ * 256-byte aligned. */
+size_t som_rms_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
+som_status som_rms_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, const void* weight,
+                                 const void* dh, int64_t lddh, int32_t dtype, int64_t rows, int64_t cols,
+                                 float eps, void* dx, int64_t lddx, float* dweight, void* ws, size_t ws_bytes,
+                                 hipStream_t stream);
+
+/* Matrix product with bias, activation and residual:
+ *
+ *     pre[m][n] = alpha x_scale[m] w_scale[n] sum_k x[m][k] W[k][n] + bias[n],
+ *     y[m][n] = act(pre[m][n]) + residual[m][n].
+ *
+ * x [M][ldx] and W are of type x_dtype (fp16, bf16 or SOM_E4M3).  W is
+ * feature-major like a codebook, W[k * ldw + n], or with w_units set unit-major,
+ * W[n * ldw + k]; 8-bit weights are unit-major only (the matrix instructions
+ * take 16 bytes of one unit at a time).  y, residual and pre are of type y_dtype
+ * (x_dtype or fp32; fp32, fp16 or bf16 for 8-bit x).  bias [N], x_scale [M] and
+ * w_scale [N] are fp32.  A dense document's scores against a codebook are
+ * alpha = -2 with the codebook's norms as bias.
+ *
+ * e may be NULL (alpha 1, nothing else).  residual may be y itself.  pre, if given,
+ * receives the activation's argument, which the gradient needs.
+ * M in [0, 2^31), N and K in [1, 2^30], M * N up to 2^42.  ws:
+ * som_product_workspace_bytes(M, N, K, x_dtype) bytes, 256-byte aligned (0
+ * bytes: ws may be NULL). */
+typedef struct som_epilogue {
+  int32_t act;           /* som_act */
+  int32_t reserved;      /* 0 */
+  float alpha;
+  const float* x_scale;  /* [M] or NULL */
+  const float* w_scale;  /* [N] or NULL */
+  const float* bias;     /* [N] or NULL */
+  const void* residual;  /* [M][ldr] or NULL */
+  int64_t ldr;
+  void* pre;             /* [M][ldp] or NULL */
+  int64_t ldp;
+} som_epilogue;
+
+size_t som_product_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t x_dtype);
+som_status som_product(const void* x, int64_t ldx, const void* W, int64_t ldw, int32_t w_units, int32_t x_dtype,
+                       int64_t M, int64_t N, int64_t K, void* y, int64_t ldy, int32_t y_dtype,
+                       const som_epilogue* e, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Its gradients, from dy and the activation's argument pre (both of x's type,
+ * fp16 or bf16; pre may be NULL without an activation):
+ *
+ *     dP = dy act'(pre),  dx = alpha dP W^T,  dW = alpha x^T dP,  dbias_n = sum_m dP.
+ *
+ * dx and dW (laid out as W is) are of x's type, dbias is fp32; each may be
+ * NULL.  With an activation dP is rounded to x's type for the two products
+ * (dbias sums it unrounded).  The residual's gradient is dy.  relu' is 0 at 0.
+ * With M == 0 dW and dbias are set to zero.
+ * ws: som_product_backward_workspace_bytes, 256-byte aligned. */
+size_t som_product_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype);
+som_status som_product_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* W, int64_t ldw,
+                                int32_t w_units, int32_t dtype, int64_t M, int64_t N, int64_t K, int32_t act,
+                                const void* pre, int64_t ldp, float alpha, void* dx, int64_t lddx, void* dW,
+                                int64_t lddw, float* dbias, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Dropout whose mask is a function of (seed, offset, row, column) and is never
+ * stored: the same call on a gradient is the backward pass.  With t = round(65536 p)
+ * (half to even) and u the 16 random bits of an element,
+ *
+ *     y = x 65536 / (65536 - t) where u >= t, else 0,  + residual;
+ *
+ * t = 65536 drops everything.  u is half-word col % 8 (low half of each word
+ * first) of the four words that Philox4x32 with ten rounds (Salmon et al., "Parallel
+ * random numbers: as easy as 1, 2, 3", SC 2011) makes of the counter (col / 8,
+ * row, offset's low word, offset's high word) and the key (seed's low word,
+ * seed's high word).  A dropped element's x is not looked at (a NaN there gives
+ * 0).  x, residual (may be NULL) and y are of type `dtype` (fp32, fp16, bf16); y
+ * may be x or residual (same stride).  0 <= p <= 1; rows < 2^32, cols < 2^31. */
+som_status som_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, int32_t dtype, int64_t rows,
+                       int64_t cols, double p, uint64_t seed, uint64_t offset, void* y, int64_t ldy,
+                       hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Measurement aid: read-bandwidth probe.  Reads `bytes` (a multiple of 16) of
  * device memory at `buf` (16-byte aligned) `passes` times with coalesced
  * 128-bit loads, every workgroup of an XCD re-reading the same part of the

@@ -32,4 +32,11 @@ from .som import (  # noqa: F401
     som_update_accumulate,
     som_update_finish,
     som_update_workspace_bytes,
+    som_rms_norm,
+    som_rms_norm_backward,
+    som_product,
+    som_product_backward,
+    som_product_backward_workspace_bytes,
+    som_product_workspace_bytes,
+    som_dropout,
 )

@@ -6,41 +6,13 @@
 #include <mutex>
 #include <string>
 
-#include "../../include/som.h"
-#include "common.h"
+#include "api_common.h"
 
 namespace {
 
-thread_local std::string g_error;
+using namespace som::api;
 
-som_status fail(som_status s, const std::string& msg) {
-  g_error = msg;
-  return s;
-}
-
-som_status ok() {
-  g_error.clear();
-  return SOM_OK;
-}
-
-som_status hip_fail(hipError_t e, const char* where) {
-  return fail(SOM_ERR_HIP, std::string(where) + ": " + hipGetErrorString(e));
-}
-
-constexpr int64_t kI32Max = 2147483647;
 constexpr int64_t kMaxTiles = int64_t(1) << 24;  // tiles or groups per launch
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-template <typename P>
-P* at(void* base, size_t off) {
-  return reinterpret_cast<P*>(static_cast<char*>(base) + off);
-}
-
-template <typename P>
-const P* at(const void* base, size_t off) {
-  return reinterpret_cast<const P*>(static_cast<const char*>(base) + off);
-}
 
 // One 128-bit load holds 4 fp32 or 8 fp16 weights; rows must start on one.
 som_status check_codebook(const void* W, int weights, int64_t F, int64_t N, int64_t ldw) {

@@ -1,0 +1,546 @@
+// The matrix product's kernel: C[i][j] = sum_k P(i, k) Q(j, k) on the matrix cores, with
+// the epilogue of som_product or, where the k axis is split, fp32 partial sums.
+//
+// An operand lies in memory with k contiguous (KC: rows of its own index, P[i * ld
+// + k]) or strided (rows of k, P[k * ld + i]); a feature-major weight matrix in the
+// forward product is the strided kind, and the products of the backward pass have
+// all three pairs.  A workgroup takes a BI x BJ tile of C and steps along k 128 bytes
+// at a time (64 elements of 16 bits, 128 of 8): a step of an operand is BR * 128
+// bytes of LDS in chunks of 16, moved straight from global memory (the lanes of a
+// load write consecutive chunks; which global chunk each lane fetches is permuted, so
+// that the fragment reads meet no bank twice):
+//
+//   KC   row r holds chunks c = 0..7 of its 128 bytes at slot c ^ (r / 2 % 8);
+//        a lane reads the chunk (k group) of its row with one 128-bit read
+//   KS   row k (64 of them) holds BR * 2 bytes in pairs of chunks (16 columns) at
+//        pair ^ swizzle(k); a lane gets 4 k of its column from each transposing
+//        64-bit read
+//
+// Where rows do not start on 16 bytes, at columns that end inside a chunk and in the
+// last, partial step the chunks go through registers, element by element at the ends:
+// no element outside the matrices is read, and what lies beyond k counts as zero in both
+// operands (so a NaN there cannot reach a sum).
+//
+// The matrix instructions take Q as their first operand: a lane then holds four
+// consecutive j of one i, which is how the epilogue reads and writes rows of C.
+#pragma once
+
+#include "dense.h"
+
+namespace som {
+
+struct ProductArgs {
+  const void *P, *Q;
+  int64_t ldp, ldq;          // elements
+  int64_t I, J, K;
+  int elem;                  // kF16, kBF16, kE4M3
+  bool p_kc, q_kc;
+  // epilogue
+  float alpha;
+  int act;
+  const float *p_scale, *q_scale, *bias;
+  const void* residual;
+  int64_t ldr;
+  void* pre;
+  int64_t ldpre;
+  void* out;
+  int64_t ldo;
+  int out_type;
+  // launch
+  float* partial;            // [splits][I][round_up(J, 4)] or nullptr
+  int64_t k_split;           // elements of k per split (a multiple of the step)
+  int splits;
+  uint32_t tiles_i, tiles_j, per_xcd;
+  bool dma;                  // rows of both operands start on 16 bytes
+};
+
+// Tile shapes (rows of C x columns): 256 x 256, 128 x 128, 64 x 128, 32 x 128, 16 x 128.
+enum Shape { kShape256 = 0, kShape128, kShape64, kShape32, kShape16, kShapes };
+struct ProductPlan {
+  int shape;
+  int splits;
+  int64_t k_split;
+  size_t partial_floats;
+};
+ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc);
+// Fills the launch's fields of `a` and enqueues it (and the join of a split k axis);
+// `partial`: plan_product's floats.
+hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream);
+hipError_t launch_product_f16(int shape, const ProductArgs& a, hipStream_t stream);
+hipError_t launch_product_bf16(int shape, const ProductArgs& a, hipStream_t stream);
+hipError_t launch_product_e4m3(int shape, const ProductArgs& a, hipStream_t stream);
+
+// dP = dy act'(pre), rounded to the type, and dP's column sums.
+struct ActGradArgs {
+  const void *dy, *pre;
+  void* dp;                  // [M][ldp] or nullptr
+  float *dbias, *part;       // or nullptr; part: act_grad_ws_floats
+  int64_t lddy, ldpre, lddp, M, N;
+  int elem, act;
+};
+size_t act_grad_ws_floats(int64_t M, int64_t N);
+hipError_t launch_act_grad(const ActGradArgs& a, hipStream_t stream);
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef u4 u4_at1 __attribute__((aligned(1)));
+typedef u4 u4_at2 __attribute__((aligned(2)));
+
+constexpr int kStepBytes = 128;
+constexpr int kXcds = 8;
+constexpr int64_t kDmaMaxLd = int64_t(1) << 22;   // elements: a tile's offsets fit 32 bits
+
+// ---------------------------------------------------------------------------
+// Epilogue
+// ---------------------------------------------------------------------------
+
+constexpr int kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSilu = 4;   // som_act
+
+// 1 / (1 + e^-z); e^-z = infinity gives 0.
+__device__ __forceinline__ float sigmoid(float z) { return 1.0f / (1.0f + __expf(-z)); }
+
+constexpr float kGeluK = 1.5957691216057308f;     // 2 sqrt(2 / pi): 1 + tanh(z) = 2 sigmoid(2 z)
+constexpr float kGeluC = 0.044715f;
+
+__device__ __forceinline__ float act_of(int act, float v) {
+  switch (act) {
+    case kActRelu:
+      return v > 0.0f ? v : (v != v ? v : 0.0f);
+    case kActGelu:
+      return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+    case kActGeluTanh:
+      return v * sigmoid(kGeluK * (v + kGeluC * v * v * v));
+    case kActSilu:
+      return v * sigmoid(v);
+    default:
+      return v;
+  }
+}
+
+// The activation's derivative.
+__device__ __forceinline__ float act_grad(int act, float v) {
+  switch (act) {
+    case kActRelu:
+      return v > 0.0f ? 1.0f : 0.0f;
+    case kActGelu:
+      return 0.5f * (1.0f + erff(v * 0.70710678118654752f)) + v * __expf(-0.5f * v * v) * 0.39894228040143268f;
+    case kActGeluTanh: {
+      const float s = sigmoid(kGeluK * (v + kGeluC * v * v * v));
+      return s + v * s * (1.0f - s) * kGeluK * (1.0f + 3.0f * kGeluC * v * v);
+    }
+    case kActSilu: {
+      const float s = sigmoid(v);
+      return s * (1.0f + v * (1.0f - s));
+    }
+    default:
+      return 1.0f;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ f4 load4(const void* base, int64_t at, int n) {
+  typedef T v4 __attribute__((ext_vector_type(4)));
+  typedef v4 v4_at __attribute__((aligned(sizeof(T))));
+  const T* p = static_cast<const T*>(base) + at;
+  f4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (n >= 4) {
+    const v4 r = *reinterpret_cast<const v4_at*>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = static_cast<float>(r[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) v[e] = static_cast<float>(p[e]);
+  }
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(void* base, int64_t at, int n, f4 v) {
+  typedef T v4 __attribute__((ext_vector_type(4)));
+  typedef v4 v4_at __attribute__((aligned(sizeof(T))));
+  T* p = static_cast<T*>(base) + at;
+  if (n >= 4) {
+    v4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = static_cast<T>(v[e]);
+    *reinterpret_cast<v4_at*>(p) = r;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) p[e] = static_cast<T>(v[e]);
+  }
+}
+
+__device__ __forceinline__ f4 load4_as(int type, const void* base, int64_t at, int n) {
+  if (type == kF32) return load4<float>(base, at, n);
+  return type == kF16 ? load4<f16>(base, at, n) : load4<bf16>(base, at, n);
+}
+__device__ __forceinline__ void store4_as(int type, void* base, int64_t at, int n, f4 v) {
+  if (type == kF32)
+    store4<float>(base, at, n, v);
+  else if (type == kF16)
+    store4<f16>(base, at, n, v);
+  else
+    store4<bf16>(base, at, n, v);
+}
+
+// Columns [j, j + n), n in 1..4, of row i from their sums.
+__device__ __forceinline__ void finish4(const ProductArgs& a, int64_t i, int64_t j, int n, f4 v) {
+  float f = a.alpha;
+  if (a.p_scale) f *= a.p_scale[i];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] *= f;
+  if (a.q_scale) v *= load4<float>(a.q_scale, j, n);
+  if (a.bias) v += load4<float>(a.bias, j, n);
+  if (a.pre) store4_as(a.out_type, a.pre, i * a.ldpre + j, n, v);
+  if (a.act != kActNone)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = act_of(a.act, v[e]);
+  if (a.residual) v += load4_as(a.out_type, a.residual, i * a.ldr + j, n);
+  store4_as(a.out_type, a.out, i * a.ldo + j, n, v);
+}
+
+// ---------------------------------------------------------------------------
+// Operand steps in LDS
+// ---------------------------------------------------------------------------
+
+// Wait for all but the N newest vector-memory operations, and for this wave's LDS
+// reads, then meet the workgroup.
+template <int N>
+__device__ __forceinline__ void arrive() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// 16 bytes per lane from base + off to LDS at `lds` (uniform) + 16 * lane.  A vector
+// instruction may have written the base's scalar registers just before (a lane read
+// into them): a memory instruction may read those five wait states later at the
+// earliest, and the compiler, which keeps that distance elsewhere, does not look into
+// this statement.  (m0 needs one.)
+__device__ __forceinline__ void dma16(const char* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
+}
+
+// Pair swizzle of a k-strided row (see above): the rows that one transposing read
+// takes (k % 4, k / 8 % 2 of them) go to different pairs of chunks.
+template <int BR>
+__device__ __forceinline__ int ks_swizzle(int k) {
+  return BR >= 128 ? (k & 3) | ((k >> 3) & 1) << 2 : ((k >> 1) & 1) | ((k >> 3) & 1) << 1;
+}
+
+// A pointer that is the same in every lane, in scalar registers.
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u >> 32));
+  return reinterpret_cast<const char*>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+// One operand's side of a workgroup: BR rows of C's axis, moved by THREADS threads.
+template <int ES, bool KC, int BR, int THREADS>
+struct Operand {
+  static constexpr int kBytes = BR * kStepBytes;
+  static constexpr int kChunks = kBytes / 16;
+  static constexpr int kEach = (kChunks + THREADS - 1) / THREADS;    // per thread
+  static constexpr int kPer = 16 / ES;                               // elements per chunk
+  static constexpr int kStep = kStepBytes / ES;                      // k elements per step
+  static_assert(KC || (ES == 2 && BR >= 64), "k-strided operands have 16 bits");
+  static_assert(kChunks % 64 == 0, "whole waves move whole loads");
+
+  const char* base;      // the tile's first row (KC) or column, at k = 0
+  int64_t ld;            // bytes per row
+  int64_t rows;          // rows (KC) or columns of the matrix from the tile's first on
+  uint32_t off[kEach];
+
+  // this thread's nth chunk: position in LDS, and its row and first element
+  static __device__ __forceinline__ int pos(int n) { return n * THREADS + static_cast<int>(threadIdx.x); }
+  static __device__ __forceinline__ void place(int p, int* row, int* chunk) {
+    if constexpr (KC) {
+      *row = p >> 3;
+      *chunk = (p & 7) ^ ((*row >> 1) & 7);
+    } else {
+      constexpr int kRow = BR / 8;
+      *row = p / kRow;
+      *chunk = (p % kRow) ^ (ks_swizzle<BR>(*row) << 1);
+    }
+  }
+  static constexpr bool whole = kChunks % THREADS == 0;
+  static __device__ __forceinline__ bool mine(int n) { return whole || pos(n) < kChunks; }
+
+  __device__ __forceinline__ void init(const void* p, int64_t ld_elems, int64_t first, int64_t extent) {
+    ld = ld_elems * ES;
+    base = uniform(static_cast<const char*>(p) + (KC ? first * ld : first * ES));
+    rows = extent - first;
+#pragma unroll
+    for (int n = 0; n < kEach; ++n) {
+      int r, c;
+      place(pos(n), &r, &c);
+      // rows and chunks past the matrix: the first one again, whose sums are not kept
+      if constexpr (KC)
+        off[n] = static_cast<uint32_t>((r < rows ? r : 0) * ld + c * 16);
+      else
+        off[n] = static_cast<uint32_t>(r * ld + (c * 8 < rows ? c : 0) * 16);
+    }
+  }
+  // columns that end inside a chunk of this tile
+  __device__ __forceinline__ bool ragged() const { return !KC && rows < BR && rows % 8 != 0; }
+  __device__ __forceinline__ const char* at(int32_t k) const { return base + (KC ? int64_t(k) * ES : k * ld); }
+
+  // whole step from k on, asynchronously
+  __device__ __forceinline__ void fetch(int32_t k, uint32_t lds) const {
+    const char* b = uniform(at(k));
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int n = 0; n < kEach; ++n)
+      if (whole || n * THREADS + wave * 64 < kChunks) dma16(b, off[n], lds + (n * THREADS + wave * 64) * 16);
+  }
+
+  // step [k, end) through registers
+  __device__ __forceinline__ void load(int32_t k, int32_t end, u4 (&v)[kEach]) const {
+#pragma unroll
+    for (int n = 0; n < kEach; ++n) {
+      int r, c;
+      place(pos(n), &r, &c);
+      int64_t left = KC ? (r < rows ? end - (k + c * kPer) : 0) : (k + r < end ? rows - c * 8 : 0);
+      if (!mine(n)) left = 0;
+      const char* p = at(k) + (r * ld + c * 16);
+      if (left >= kPer) {
+        v[n] = ES == 2 ? u4(*reinterpret_cast<const u4_at2*>(p)) : u4(*reinterpret_cast<const u4_at1*>(p));
+      } else {
+        v[n] = u4{0, 0, 0, 0};
+        if constexpr (ES == 2) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (e < left) v[n][e / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[e]) << (16 * (e % 2));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (e < left) v[n][e / 4] |= static_cast<uint32_t>(reinterpret_cast<const uint8_t*>(p)[e]) << (8 * (e % 4));
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void store(char* lds, const u4 (&v)[kEach]) const {
+#pragma unroll
+    for (int n = 0; n < kEach; ++n)
+      if (mine(n)) *reinterpret_cast<u4*>(lds + pos(n) * 16) = v[n];
+  }
+
+  // A lane's share of rows [16 t, 16 t + 16) of this wave's: `lane_base` is for
+  // t = 0, k = 0 of a wave whose rows start at `first`.
+  static __device__ __forceinline__ uint32_t lane_base(int first) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, i = lane & 15;
+    if constexpr (KC) {
+      return static_cast<uint32_t>((first + i) * kStepBytes + ((g ^ ((i >> 1) & 7)) << 4));
+    } else {
+      const int k = g * 8 + (i >> 2);
+      return static_cast<uint32_t>(k * BR * 2 + ((((first >> 4) ^ ks_swizzle<BR>(k)) << 5) | (i & 3) << 3));
+    }
+  }
+};
+
+typedef short s8 __attribute__((ext_vector_type(8)));
+typedef int i4 __attribute__((ext_vector_type(4)));
+typedef f16 h2 __attribute__((ext_vector_type(2)));
+typedef f16 h8 __attribute__((ext_vector_type(8)));
+typedef bf16 b8 __attribute__((ext_vector_type(8)));
+
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) s4 lds_s4;
+typedef __attribute__((address_space(3))) u4 lds_u4;
+
+// 16 bytes (KC: chunk g + 4 h of the row; KS: k = 32 h + 8 g + 0..7 of the column).
+template <bool KC, int BR>
+__device__ __forceinline__ i4 fragment(lds_char* step, uint32_t lane_base, int t, int h) {
+  if constexpr (KC) {
+    const u4 v = *reinterpret_cast<lds_u4*>(step + ((lane_base ^ (h << 6)) + t * 16 * kStepBytes));
+    return __builtin_bit_cast(i4, v);
+  } else {
+    const uint32_t at = (lane_base ^ (t << 5)) + h * 32 * BR * 2;
+    union {
+      s4 half[2];
+      i4 all;
+    } v;
+    v.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s4*>(step + at));
+    v.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s4*>(step + at + 4 * BR * 2));
+    return v.all;
+  }
+}
+
+// A fragment as the matrix instructions take it: 8 k of 16 bits, or two times 8 of 8
+// bits, widened (exactly) to fp16.  The 8-bit matrix instructions are not used: they
+// line products up before they add them and drop bits that a sum in fp32 keeps (errors
+// of 2^-17 of the sum of magnitudes against the 64-bit oracle, the instructions of
+// 32 k and of 128 k alike).
+template <int E>
+struct Frag {
+  static constexpr int kParts = E == kE4M3 ? 2 : 1;
+  i4 part[kParts];
+  __device__ __forceinline__ explicit Frag(i4 v) {
+    if constexpr (E == kE4M3) {
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        h8 w;
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+          const h2 lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[2 * p + d], 1.0f, false);
+          const h2 hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[2 * p + d], 1.0f, true);
+          w[4 * d] = lo[0];
+          w[4 * d + 1] = lo[1];
+          w[4 * d + 2] = hi[0];
+          w[4 * d + 3] = hi[1];
+        }
+        part[p] = __builtin_bit_cast(i4, w);
+      }
+    } else {
+      part[0] = v;
+    }
+  }
+};
+
+// c + the products over the fragments' k.
+template <int E>
+__device__ __forceinline__ f4 mfma(const Frag<E>& q, const Frag<E>& p, f4 c) {
+#pragma unroll
+  for (int i = 0; i < Frag<E>::kParts; ++i) {
+    if constexpr (E == kBF16)
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, q.part[i]), __builtin_bit_cast(b8, p.part[i]),
+                                                  c, 0, 0, 0);
+    else
+      c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, q.part[i]), __builtin_bit_cast(h8, p.part[i]),
+                                                 c, 0, 0, 0);
+  }
+  return c;
+}
+
+// ---------------------------------------------------------------------------
+// The kernel
+// ---------------------------------------------------------------------------
+
+// WI x WJ waves, each with TI x TJ tiles of 16 x 16; NS steps in LDS.
+template <int E, bool PKC, bool QKC, int WI, int WJ, int TI, int TJ, int NS>
+__global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
+  constexpr int ES = E == kE4M3 ? 1 : 2;
+  constexpr int BI = WI * TI * 16, BJ = WJ * TJ * 16, THREADS = WI * WJ * 64;
+  using OpP = Operand<ES, PKC, BI, THREADS>;
+  using OpQ = Operand<ES, QKC, BJ, THREADS>;
+  constexpr int kStage = OpP::kBytes + OpQ::kBytes;
+  constexpr int kStep = kStepBytes / ES;
+  extern __shared__ __align__(1024) char lds[];
+
+  // XCD x (workgroups are dealt to the XCDs in turn) takes the tiles [x * per_xcd, ...):
+  // tiles in bands of kBand rows of tiles, so that the ones it runs at once share
+  // both operands' rows in its L2
+  constexpr uint32_t kBand = 4;
+  const uint32_t lin = blockIdx.x % kXcds * a.per_xcd + blockIdx.x / kXcds;
+  const uint32_t tiles = a.tiles_i * a.tiles_j;
+  if (lin >= tiles * a.splits) return;
+  const uint32_t split = lin / tiles, rest = lin % tiles;
+  const uint32_t band = rest / (kBand * a.tiles_j), in = rest % (kBand * a.tiles_j);
+  const uint32_t height = min(kBand, a.tiles_i - band * kBand);
+  const int64_t i0 = static_cast<int64_t>(band * kBand + in % height) * BI;
+  const int64_t j0 = static_cast<int64_t>(in / height) * BJ;
+  const int32_t k0 = static_cast<int32_t>(split * a.k_split);
+  const int32_t k1 = static_cast<int32_t>(min(a.K, k0 + a.k_split));
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wi = wave / WJ, wj = wave % WJ;
+  OpP p;
+  OpQ q;
+  p.init(a.P, a.ldp, i0, a.I);
+  q.init(a.Q, a.ldq, j0, a.J);
+  const uint32_t pb = OpP::lane_base(wi * TI * 16), qb = OpQ::lane_base(wj * TJ * 16);
+  lds_char* const l3 = (lds_char*)lds;
+  const uint32_t l0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(l3));
+
+  f4 acc[TI][TJ];
+#pragma unroll
+  for (int x = 0; x < TI; ++x)
+#pragma unroll
+    for (int y = 0; y < TJ; ++y) acc[x][y] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  auto compute = [&](int slot) {
+    lds_char* sp = l3 + slot * kStage;
+    lds_char* sq = sp + OpP::kBytes;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      i4 raw[TJ];
+#pragma unroll
+      for (int y = 0; y < TJ; ++y) raw[y] = fragment<QKC, BJ>(sq, qb, y, h);
+#pragma unroll
+      for (int x = 0; x < TI; ++x) {
+        const Frag<E> fp(fragment<PKC, BI>(sp, pb, x, h));
+#pragma unroll
+        for (int y = 0; y < TJ; ++y) acc[x][y] = mfma<E>(Frag<E>(raw[y]), fp, acc[x][y]);
+      }
+    }
+  };
+
+  const int32_t steps = (k1 - k0 + kStep - 1) / kStep;
+  int32_t t = 0;
+  if (a.dma && !p.ragged() && !q.ragged()) {
+    // whole steps: NS - 1 on their way while one is worked on
+    const int32_t full = (k1 - k0) / kStep;
+    // loads of this wave per step: the last one of P may be the other waves'
+    constexpr int kMost = OpP::kEach + OpQ::kEach;
+    static_assert(OpQ::whole, "every wave moves the same share of Q");
+    const bool most = OpP::whole || (OpP::kEach - 1) * THREADS + wave * 64 < OpP::kChunks;
+    auto fetch = [&](int32_t s) {
+      const uint32_t at = l0 + static_cast<uint32_t>(s % NS) * kStage;
+      p.fetch(k0 + s * kStep, at);
+      q.fetch(k0 + s * kStep, at + OpP::kBytes);
+    };
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s)
+      if (s < full) fetch(s);
+    for (; t < full; ++t) {
+      if (NS == 2 || t + NS - 2 >= full)
+        arrive<0>();
+      else if (most)
+        arrive<(NS - 2) * kMost>();
+      else
+        arrive<(NS - 2) * (kMost - 1)>();
+      if (t + NS - 1 < full) fetch(t + NS - 1);
+      compute(static_cast<int>(t % NS));
+    }
+    arrive<0>();
+  }
+  if (t < steps) {
+    u4 vp[OpP::kEach], vq[OpQ::kEach];
+    p.load(k0 + t * kStep, k1, vp);
+    q.load(k0 + t * kStep, k1, vq);
+    for (int slot = 0; t < steps; ++t, slot ^= 1) {
+      p.store(lds + slot * kStage, vp);
+      q.store(lds + slot * kStage + OpP::kBytes, vq);
+      __syncthreads();
+      if (t + 1 < steps) {
+        p.load(k0 + (t + 1) * kStep, k1, vp);
+        q.load(k0 + (t + 1) * kStep, k1, vq);
+      }
+      compute(slot);
+    }
+  }
+
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int x = 0; x < TI; ++x) {
+    const int64_t i = i0 + (wi * TI + x) * 16 + (lane & 15);
+    if (i < a.I) {
+#pragma unroll
+      for (int y = 0; y < TJ; ++y) {
+        const int64_t j = j0 + (wj * TJ + y) * 16 + (lane >> 4) * 4;
+        if (j < a.J) {
+          if (a.splits > 1) {
+            const int64_t ld = (a.J + 3) / 4 * 4;
+            *reinterpret_cast<f4*>(a.partial + (split * a.I + i) * ld + j) = acc[x][y];
+          } else {
+            finish4(a, i, j, static_cast<int>(min<int64_t>(4, a.J - j)), acc[x][y]);
+          }
+        }
+      }
+    }
+  }
+}
+
+}  // namespace som

@@ -55,7 +55,19 @@ EXPORTS = (
     "som_update_finish_f16",
     "som_probe_read",
     "som_probe_lds",
+    "som_rms_norm",
+    "som_rms_norm_backward_workspace_bytes",
+    "som_rms_norm_backward",
+    "som_product_workspace_bytes",
+    "som_product",
+    "som_product_backward_workspace_bytes",
+    "som_product_backward",
+    "som_dropout",
 )
+
+# som_dtype and som_act
+DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
 class SomError(RuntimeError):
@@ -77,6 +89,21 @@ class som_bmu_opts(ctypes.Structure):
         ("schedule", ctypes.c_int32),
         ("neuron_chunk", ctypes.c_int32),
         ("sweep", ctypes.c_int32),
+    ]
+
+
+class som_epilogue(ctypes.Structure):
+    _fields_ = [
+        ("act", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("alpha", ctypes.c_float),
+        ("x_scale", ctypes.c_void_p),
+        ("w_scale", ctypes.c_void_p),
+        ("bias", ctypes.c_void_p),
+        ("residual", ctypes.c_void_p),
+        ("ldr", ctypes.c_int64),
+        ("pre", ctypes.c_void_p),
+        ("ldp", ctypes.c_int64),
     ]
 
 
@@ -159,6 +186,27 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.som_probe_lds.argtypes = [_i32, _vp, ctypes.POINTER(ctypes.c_int64), _vp]
     lib.som_cluster_order.restype = _i32
     lib.som_cluster_order.argtypes = [_vp, _vp, _i64, _i64, _i64, _vp, _vp, _sz, _vp]
+    lib.som_rms_norm.restype = _i32
+    lib.som_rms_norm.argtypes = [_vp, _i64, _vp, _i64, _vp, _i32, _i64, _i64, ctypes.c_float, _i32, _vp, _i64, _vp,
+                                 _i64, _vp, _vp]
+    lib.som_rms_norm_backward_workspace_bytes.restype = _sz
+    lib.som_rms_norm_backward_workspace_bytes.argtypes = [_i64, _i64]
+    lib.som_rms_norm_backward.restype = _i32
+    lib.som_rms_norm_backward.argtypes = [_vp, _i64, _vp, _i64, _vp, _vp, _i64, _i32, _i64, _i64, ctypes.c_float, _vp,
+                                          _i64, _vp, _vp, _sz, _vp]
+    for name in ("som_product_workspace_bytes", "som_product_backward_workspace_bytes"):
+        fn = getattr(lib, name)
+        fn.restype = _sz
+        fn.argtypes = [_i64, _i64, _i64, _i32]
+    lib.som_product.restype = _i32
+    lib.som_product.argtypes = [_vp, _i64, _vp, _i64, _i32, _i32, _i64, _i64, _i64, _vp, _i64, _i32,
+                                ctypes.POINTER(som_epilogue), _vp, _sz, _vp]
+    lib.som_product_backward.restype = _i32
+    lib.som_product_backward.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _i64, _i64, _i64, _i32, _vp,
+                                         _i64, ctypes.c_float, _vp, _i64, _vp, _i64, _vp, _vp, _sz, _vp]
+    lib.som_dropout.restype = _i32
+    lib.som_dropout.argtypes = [_vp, _i64, _vp, _i64, _i32, _i64, _i64, ctypes.c_double, ctypes.c_uint64,
+                                ctypes.c_uint64, _vp, _i64, _vp]
     _lib = lib
     return lib
 
@@ -609,3 +657,240 @@ def som_probe_lds(iters: int, sink: torch.Tensor, stream=None) -> int:
     _check(lib.som_probe_lds(int(iters), _ptr(sink), ctypes.byref(nbytes), _stream(stream)))
     return int(nbytes.value)
 
+
+
+# ---------------------------------------------------------------------------
+# Dense documents
+# ---------------------------------------------------------------------------
+
+def _rows(t: torch.Tensor, name: str, dtype=None, shape=None):
+    """Check a matrix of contiguous rows; return its pointer and row stride."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a ROCm device (got {t.device})")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    rows, cols = t.shape
+    if shape is not None and (rows, cols) != shape:
+        raise ValueError(f"{name} must be {shape[0]} x {shape[1]} (got {rows} x {cols})")
+    ld, one = t.stride()
+    if cols > 1 and one != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    if rows <= 1:
+        ld = max(ld, cols)
+    elif ld < cols:
+        raise ValueError(f"{name}: rows must not overlap")
+    return t.data_ptr(), ld
+
+
+def _vector(t: Optional[torch.Tensor], name: str, n: int, dtype=torch.float32):
+    if t is None:
+        return None
+    _dev(t, dtype, name)
+    if t.numel() != n:
+        raise ValueError(f"{name} must have {n} entries")
+    return t.data_ptr()
+
+
+def _float_type(t: torch.Tensor, name: str, types) -> int:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dtype not in types:
+        raise TypeError(f"{name} must be one of {', '.join(str(x) for x in types)} (got {t.dtype})")
+    return DTYPES[t.dtype]
+
+
+_FLOATS = (torch.float32, torch.float16, torch.bfloat16)
+_HALVES = (torch.float16, torch.bfloat16)
+
+
+def _weights(W: torch.Tensor, name: str, dtype):
+    """A K x N weight matrix: (pointer, row stride, 1 if unit-major).
+
+    Feature-major rows (W[k, :] contiguous, like a codebook) or, as the
+    transposed view of an N x K matrix, unit-major ones."""
+    if not isinstance(W, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if W.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    units = W.stride(0) == 1 and (W.stride(1) != 1 or dtype == torch.float8_e4m3fn)
+    p, ld = _rows(W.t() if units else W, name, dtype)
+    return p, ld, int(units)
+
+
+def _scratch(ws, need: int, device):
+    if ws is None:
+        if need == 0:
+            return None, 0
+        ws = _workspace(need, device)
+    _dev(ws, torch.uint8, "ws")
+    return ws, ws.numel()
+
+
+def som_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 residual: Optional[torch.Tensor] = None, q8: bool = False, y: Optional[torch.Tensor] = None,
+                 h: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, stream=None):
+    """(y, h, scale) of the root-mean-square norm of the rows of x + residual.
+
+    h = x + residual (None without a residual, unless given), y = h /
+    sqrt(mean h^2 + eps) * weight in x's type (fp32, fp16, bf16).  With ``q8`` y
+    is float8_e4m3fn and scale (fp32, else None) holds each row's factor:
+    y * scale[:, None] is the norm.  ``h`` may be x or the residual, which
+    updates a residual stream in place."""
+    lib = load()
+    dt = _float_type(x, "x", _FLOATS)
+    xp, ldx = _rows(x, "x")
+    rows, cols = x.shape
+    shape = (rows, cols)
+    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", x.dtype, shape)
+    wp = _vector(weight, "weight", cols, x.dtype)
+    yt = torch.float8_e4m3fn if q8 else x.dtype
+    if y is None:
+        y = torch.empty(shape, dtype=yt, device=x.device)
+    yp, ldy = _rows(y, "y", yt, shape)
+    if h is None and residual is not None:
+        h = torch.empty(shape, dtype=x.dtype, device=x.device)
+    hp, ldh = (None, 0) if h is None else _rows(h, "h", x.dtype, shape)
+    if q8 and scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if scale is not None and not q8:
+        raise ValueError("scale goes with q8")
+    sp = _vector(scale, "scale", rows)
+    _check(lib.som_rms_norm(xp, ldx, rp, ldr, wp, dt, rows, cols, eps, 1 if q8 else 0, yp, ldy, hp, ldh, sp,
+                            _stream(stream)))
+    return y, h, scale
+
+
+def som_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                          dh: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                          dweight: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """(dx, dweight) of som_rms_norm: from the gradient of y, the h it returned (x
+    without a residual) and the gradient ``dh`` that reaches h itself.  dx is the
+    gradient of x and of the residual; dweight is fp32."""
+    lib = load()
+    dt = _float_type(h, "h", _FLOATS)
+    hp, ldh = _rows(h, "h")
+    rows, cols = h.shape
+    shape = (rows, cols)
+    gp, ldg = _rows(dy, "dy", h.dtype, shape)
+    wp = _vector(weight, "weight", cols, h.dtype)
+    ep, lde = (None, 0) if dh is None else _rows(dh, "dh", h.dtype, shape)
+    if dx is None:
+        dx = torch.empty(shape, dtype=h.dtype, device=h.device)
+    xp, ldx = _rows(dx, "dx", h.dtype, shape)
+    if dweight is None:
+        dweight = torch.empty(cols, dtype=torch.float32, device=h.device)
+    dwp = _vector(dweight, "dweight", cols)
+    ws, n = _scratch(ws, lib.som_rms_norm_backward_workspace_bytes(rows, cols), h.device)
+    _check(lib.som_rms_norm_backward(gp, ldg, hp, ldh, wp, ep, lde, dt, rows, cols, eps, xp, ldx, dwp, _ptr(ws), n,
+                                     _stream(stream)))
+    return dx, dweight
+
+
+def som_product_workspace_bytes(M: int, N: int, K: int, dtype=torch.bfloat16) -> int:
+    return int(load().som_product_workspace_bytes(M, N, K, DTYPES[dtype]))
+
+
+def som_product(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
+                residual: Optional[torch.Tensor] = None, alpha: float = 1.0,
+                x_scale: Optional[torch.Tensor] = None, w_scale: Optional[torch.Tensor] = None,
+                y: Optional[torch.Tensor] = None, dtype=None, pre: Optional[torch.Tensor] = None,
+                ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """act(alpha x_scale w_scale (x @ W) + bias) + residual.
+
+    x [M, K] and W [K, N] in fp16, bf16 or float8_e4m3fn; W with contiguous rows
+    (feature-major, like a codebook) or as the transposed view of an N x K matrix
+    (unit-major; the only layout of 8-bit weights).  y has type ``dtype`` (x's, or
+    fp32; 8-bit x: bf16 unless given).  bias [N], x_scale [M] and w_scale [N] are fp32.
+    act: none, relu, gelu, gelu_tanh or silu.  ``pre`` (like y), if given, receives
+    the activation's argument for som_product_backward.  A dense document's scores
+    against a codebook: alpha=-2, bias=its norms, dtype=torch.float32."""
+    lib = load()
+    xt = _float_type(x, "x", (*_HALVES, torch.float8_e4m3fn))
+    xp, ldx = _rows(x, "x")
+    M, K = x.shape
+    Wp, ldw, units = _weights(W, "W", x.dtype)
+    if W.shape[0] != K:
+        raise ValueError(f"x has {K} columns and W {W.shape[0]} rows")
+    N = W.shape[1]
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}")
+    shape = (M, N)
+    if y is None:
+        y = torch.empty(shape, dtype=dtype or (torch.bfloat16 if xt == 3 else x.dtype), device=x.device)
+    elif dtype is not None and y.dtype != dtype:
+        raise TypeError(f"y must be {dtype} (got {y.dtype})")
+    yt = _float_type(y, "y", _FLOATS)
+    yp, ldy = _rows(y, "y", None, shape)
+    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", y.dtype, shape)
+    pp, ldp = (None, 0) if pre is None else _rows(pre, "pre", y.dtype, shape)
+    e = som_epilogue(ACTIVATIONS[act], 0, alpha, _vector(x_scale, "x_scale", M), _vector(w_scale, "w_scale", N),
+                     _vector(bias, "bias", N), rp, ldr, pp, ldp)
+    ws, n = _scratch(ws, lib.som_product_workspace_bytes(M, N, K, xt), x.device)
+    _check(lib.som_product(xp, ldx, Wp, ldw, units, xt, M, N, K, yp, ldy, yt, ctypes.byref(e), _ptr(ws), n,
+                           _stream(stream)))
+    return y
+
+
+def som_product_backward_workspace_bytes(M: int, N: int, K: int, dtype=torch.bfloat16) -> int:
+    return int(load().som_product_backward_workspace_bytes(M, N, K, DTYPES[dtype]))
+
+
+def som_product_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, act: str = "none",
+                         pre: Optional[torch.Tensor] = None, alpha: float = 1.0, dx: Optional[torch.Tensor] = None,
+                         dW: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
+                         ws: Optional[torch.Tensor] = None, stream=None):
+    """(dx, dW, dbias) of som_product, in x's type (fp16 or bf16), dW laid out as W
+    is; dbias is fp32.  ``pre`` is what som_product stored (not needed without an
+    activation).  The residual's gradient is dy."""
+    lib = load()
+    dt = _float_type(x, "x", _HALVES)
+    xp, ldx = _rows(x, "x")
+    M, K = x.shape
+    Wp, ldw, units = _weights(W, "W", x.dtype)
+    if W.shape[0] != K:
+        raise ValueError(f"x has {K} columns and W {W.shape[0]} rows")
+    N = W.shape[1]
+    gp, ldg = _rows(dy, "dy", x.dtype, (M, N))
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}")
+    if pre is None and act != "none":
+        raise ValueError("pre is needed for an activation's gradient")
+    pp, ldp = (None, 0) if pre is None else _rows(pre, "pre", x.dtype, (M, N))
+    if dx is None:
+        dx = torch.empty((M, K), dtype=x.dtype, device=x.device)
+    dxp, lddx = _rows(dx, "dx", x.dtype, (M, K))
+    if dW is None:
+        dW = torch.empty((N, K), dtype=x.dtype, device=x.device).t() if units else \
+            torch.empty((K, N), dtype=x.dtype, device=x.device)
+    dWp, lddw = _rows(dW.t() if units else dW, "dW", x.dtype, (N, K) if units else (K, N))
+    if dbias is None:
+        dbias = torch.empty(N, dtype=torch.float32, device=x.device)
+    dbp = _vector(dbias, "dbias", N)
+    ws, n = _scratch(ws, lib.som_product_backward_workspace_bytes(M, N, K, dt), x.device)
+    _check(lib.som_product_backward(gp, ldg, xp, ldx, Wp, ldw, units, dt, M, N, K, ACTIVATIONS[act], pp, ldp, alpha,
+                                    dxp, lddx, dWp, lddw, dbp, _ptr(ws), n, _stream(stream)))
+    return dx, dW, dbias
+
+
+def som_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual: Optional[torch.Tensor] = None,
+                y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """x with each element dropped at rate p (a multiple of 2^-16, rounded to), the kept
+    ones divided by the share kept, plus the residual.  The mask is a function of
+    (seed, offset, row, column): the same call on the gradient is the backward pass."""
+    lib = load()
+    dt = _float_type(x, "x", _FLOATS)
+    xp, ldx = _rows(x, "x")
+    rows, cols = x.shape
+    shape = (rows, cols)
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        raise ValueError("seed and offset must be in [0, 2^64)")
+    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", x.dtype, shape)
+    if y is None:
+        y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    yp, ldy = _rows(y, "y", x.dtype, shape)
+    _check(lib.som_dropout(xp, ldx, rp, ldr, dt, rows, cols, p, seed, offset, yp, ldy, _stream(stream)))
+    return y

@@ -1,0 +1,482 @@
+"""The dense-document operators on the GPU against the fp64 oracle.
+
+Tolerances (u = 2^-24, t = half a unit of the output type: 2^-24, 2^-11, 2^-8,
+and the type's smallest step for values below its normal range):
+  a sum of n fp32 terms added in any order is within n u times the sum of their
+  magnitudes (twice that where the matrix cores add them); the few operations
+  around it, the exponential and erf add at most 2^-17 of what they give;
+  the output is rounded once, by t of itself."""
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from oracle import dense as oracle  # noqa: E402
+
+if torch.cuda.is_available():
+    import paper_2609_05138_amd as som
+else:  # collected on CPU-only machines, never run there
+    som = None
+
+DEV = "cuda:0"
+T = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}
+HALF = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f32": 2.0 ** -126, "f16": 2.0 ** -24, "bf16": 2.0 ** -126}
+U, CALC = 2.0 ** -24, 2.0 ** -17
+
+
+def _wide(values, dtype, pad, lead=0, fill=float("nan")):
+    """values as a view into a wider array whose other columns hold `fill`."""
+    rows, cols = values.shape
+    wide = torch.full((rows, lead + cols + pad), fill, dtype=torch.float32, device=DEV).to(dtype)
+    wide[:, lead:lead + cols] = torch.as_tensor(values, dtype=torch.float32, device=DEV).to(dtype)
+    return wide[:, lead:lead + cols]
+
+
+def _out(rows, cols, dtype, pad):
+    """An output inside a wider array of a known value."""
+    wide = torch.full((rows, cols + pad), 7.0, dtype=torch.float32, device=DEV).to(dtype)
+    return wide, wide[:, :cols]
+
+
+def _untouched(wide, cols):
+    return bool((wide[:, cols:].float() == 7.0).all())
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _near(got, want, tol, what=""):
+    got = _np(got)
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4],
+                           np.broadcast_to(tol, want.shape)[bad][:4])
+
+
+# --------------------------------------------------------------------------- norm
+
+NORM_SHAPES = [(1, 1), (1, 8), (3, 7), (5, 511), (2, 512), (9, 513), (1, 4096), (7, 2049), (3, 8192), (2, 9001),
+               (1030, 64), (1030, 515), (1025, 2056), (1026, 8200), (2, 16385), (2, 32768), (2, 33001)]
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", NORM_SHAPES)
+def test_norm(rows, cols, kind):
+    rng = np.random.default_rng(rows * 7919 + cols)
+    pad = (rows + cols) % 3 * 4
+    x, r = (_wide(rng.normal(size=(rows, cols)) * s, T[kind], pad) for s in (3.0, 1.0))
+    w = torch.as_tensor(rng.normal(1.0, 0.2, cols)).to(DEV).to(T[kind])
+    for weight, residual in ((w, r), (w, None), (None, r)):
+        want, h64 = oracle.rms_norm(_np(x), None if weight is None else _np(weight), 1e-6,
+                                    None if residual is None else _np(residual))
+        wide, y = _out(rows, cols, T[kind], pad)
+        y2, h, scale = som.som_rms_norm(x, weight, 1e-6, residual=residual, y=y)
+        assert y2 is y and scale is None and _untouched(wide, cols)
+        # the sum of squares has `cols` positive terms, added at most cols / 64 + 64 deep
+        calc = CALC + (cols / 64 + 64) * U
+        _near(y, want, np.abs(want) * (HALF[kind] + calc) + TINY[kind], "y")
+        if residual is None:
+            assert h is None
+        else:
+            _near(h, h64, np.abs(h64) * HALF[kind] + U * (np.abs(_np(x)) + np.abs(_np(r))) + TINY[kind], "h")
+        q, _, scale = som.som_rms_norm(x, weight, 1e-6, residual=residual, q8=True)
+        assert q.dtype == T["e4m3"]
+        _near(scale, np.abs(want).max(1) / 448.0, np.abs(want).max(1) / 448.0 * 2 * calc, "scale")
+        # 3 bits of fraction: half a unit is 2^-4 of the value at most, 2^-10 scales below 2^-6 of them
+        s = _np(scale)[:, None]
+        _near(q.float() * scale[:, None], want, np.abs(want) * (2.0 ** -4 + 2 * calc) + s * 2.0 ** -10, "q")
+
+
+def test_norm_special_rows():
+    cols = 600
+    x = torch.randn((6, cols), device=DEV)
+    x[1] = 0.0
+    x[2, 17] = float("nan")
+    x[3, 599] = float("inf")
+    x[4] = 1e-30                        # mean of squares underflows to 0: eps alone
+    w = torch.ones(cols, device=DEV)
+    y, _, _ = som.som_rms_norm(x, w, 1e-6)
+    q, _, scale = som.som_rms_norm(x, w, 1e-6, q8=True)
+    assert bool((y[1] == 0).all()) and bool((q[1].float() == 0).all()) and float(scale[1]) == 1.0
+    assert bool(y[2].isnan().all()) and bool(q[2].float().isnan().all())
+    assert bool(y[3, 599].isnan()) and bool((y[3, :599] == 0).all()) and bool(q[3, 599].float().isnan())
+    assert torch.allclose(y[4], torch.full_like(y[4], 1e-27), rtol=1e-5, atol=0)
+    for i in (0, 5):
+        assert bool(y[i].isfinite().all()) and float(q[i].float().abs().max()) == 448.0
+    y, _, _ = som.som_rms_norm(x[1:2], w, 0.0)                       # 0 * infinity
+    assert bool(y.isnan().all())
+
+
+@pytest.mark.parametrize("cols", [40, 4097, 40000])
+def test_norm_updates_a_residual_stream_in_place(cols):
+    rng = np.random.default_rng(cols)
+    x, r = (torch.as_tensor(rng.normal(size=(5, cols))).to(DEV).to(torch.bfloat16) for _ in range(2))
+    want = som.som_rms_norm(x, None, 1e-5, residual=r)
+    for target in (0, 1):
+        a, b = x.clone(), r.clone()
+        y, h, _ = som.som_rms_norm(a, None, 1e-5, residual=b, h=(a, b)[target])
+        assert torch.equal(y, want[0]) and torch.equal((a, b)[target], want[1])
+        assert torch.equal((b, a)[target], (r, x)[target])
+
+
+BACK_SHAPES = [(1, 1), (1, 9), (5, 512), (6, 513), (3, 2048), (4, 2051), (1100, 70), (700, 4096), (5, 4100), (3, 8192),
+               (3, 8195), (2, 16384), (3, 16385), (70, 20000)]
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", BACK_SHAPES)
+def test_norm_gradient(rows, cols, kind):
+    rng = np.random.default_rng(rows * 31 + cols)
+    pad = (rows + cols) % 3 * 4
+    h, dy, dh = (_wide(rng.normal(size=(rows, cols)) * s, T[kind], pad) for s in (2.0, 0.3, 0.2))
+    w = torch.as_tensor(rng.normal(1.0, 0.2, cols)).to(DEV).to(T[kind])
+    for weight, extra in ((w, dh), (w, None), (None, dh)):
+        w64 = None if weight is None else _np(weight)
+        want, dw = oracle.rms_norm_backward(_np(dy), _np(h), w64, 1e-6, None if extra is None else _np(extra))
+        wide, dx = _out(rows, cols, T[kind], pad)
+        dweight = torch.full((cols,), float("nan"), device=DEV)
+        som.som_rms_norm_backward(dy, h, weight, 1e-6, dh=extra, dx=dx, dweight=dweight)
+        assert _untouched(wide, cols)
+        s = 1.0 / np.sqrt((_np(h) ** 2).mean(1, keepdims=True) + 1e-6)
+        g = _np(dy) if weight is None else _np(dy) * w64
+        calc = CALC + (cols / 64 + 64) * U
+        size = np.abs(s * g) + np.abs(_np(h)) * s ** 3 * np.abs(g * _np(h)).mean(1, keepdims=True)
+        size = size + (0 if extra is None else np.abs(_np(dh)))
+        _near(dx, want, np.abs(want) * HALF[kind] + size * 2 * calc + TINY[kind], "dx")
+        _near(dweight, dw, np.abs(_np(dy) * _np(h) * s).sum(0) * (2 * calc + rows * U) + 1e-30, "dweight")
+
+
+def test_norm_gradient_in_place_and_empty():
+    h, dy, dh = (torch.randn((50, 333), device=DEV) for _ in range(3))
+    want, dw = som.som_rms_norm_backward(dy, h, None, 1e-6, dh=dh)
+    for k in range(2):
+        a = [dy.clone(), dh.clone()]
+        som.som_rms_norm_backward(a[0], h, None, 1e-6, dh=a[1], dx=a[k])
+        assert torch.equal(a[k], want)
+    dweight = torch.full((333,), 5.0, device=DEV)
+    som.som_rms_norm_backward(dy[:0], h[:0], None, 1e-6, dweight=dweight)
+    assert not bool(dweight.any())
+    y, _, _ = som.som_rms_norm(h[:0])
+    assert y.shape == (0, 333)
+
+
+def test_norm_rows_past_32_bits():
+    # the last rows start beyond 2^32 bytes and 2^31 elements
+    rows, cols, ld = 70001, 40, 32768
+    x = torch.empty((rows, ld), dtype=torch.bfloat16, device=DEV)[:, 17:17 + cols]
+    x.copy_(torch.randn((rows, cols), device=DEV))
+    got, _, _ = som.som_rms_norm(x, None, 1e-6)
+    want, _ = oracle.rms_norm(_np(x[-50:]), None, 1e-6)
+    _near(got[-50:], want, np.abs(want) * (HALF["bf16"] + 2 * CALC))
+    dx, _ = som.som_rms_norm_backward(x, x, None, 1e-6, dx=x)
+    assert dx.shape == (rows, cols) and bool(dx.isfinite().all())
+
+
+# --------------------------------------------------------------------------- product
+
+def _weight_layout(W, units, dtype, pad, lead=0):
+    if units:
+        return _wide(W.T, dtype, pad, lead).t()
+    return _wide(W, dtype, pad, lead)
+
+
+# M, N, K: each tile shape, its edges, split k axes, partial steps and chunks
+SIZES = [(1, 1, 1), (1, 8, 64), (1, 130, 300), (3, 257, 65), (16, 128, 128), (17, 100, 1000), (32, 129, 640), (33, 64, 63),
+         (64, 300, 2048), (65, 128, 200), (128, 256, 128), (129, 255, 131), (200, 1000, 72), (257, 511, 96),
+         (1, 4096, 4096), (300, 40, 4096), (40, 3001, 520)]
+
+
+@pytest.mark.parametrize("units", [False, True])
+@pytest.mark.parametrize("kind", ["f16", "bf16", "e4m3"])
+@pytest.mark.parametrize("M,N,K", SIZES)
+def test_product_of_integers_is_exact(M, N, K, kind, units):
+    if kind == "e4m3" and not units:
+        pytest.skip("8-bit weights are unit-major")
+    rng = np.random.default_rng(M * 17 + N * 5 + K)
+    x, W = rng.integers(-3, 4, (M, K)).astype(float), rng.integers(-3, 4, (K, N)).astype(float)
+    want = x @ W                                          # below 2^24: exact in fp32
+    # rows that start on 16 bytes, and ones that do not; NaN around both
+    for pad, lead in ((-K % 16, 0), (5, 0), (16 - (K + 3) % 16, 3)):
+        xd = _wide(x, T[kind], pad, lead)
+        wp = -(K if units else N) % 16 if pad == -K % 16 else pad
+        Wd = _weight_layout(W, units, T[kind], wp, lead)
+        wide, y = _out(M, N, torch.float32, 3)
+        got = som.som_product(xd, Wd, y=y)
+        assert got is y and np.array_equal(_np(y), want), (pad, lead, np.argwhere(_np(y) != want)[:5].tolist())
+        assert _untouched(wide, N)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("kind,out", [("f16", "f16"), ("f16", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("e4m3", "bf16"),
+                                      ("e4m3", "f16"), ("e4m3", "f32")])
+@pytest.mark.parametrize("M,N,K", [(1, 77, 500), (19, 333, 2100), (130, 140, 70), (256, 512, 128)])
+def test_product_epilogue(M, N, K, kind, out, act):
+    rng = np.random.default_rng(M + N + K)
+    e4m3 = kind == "e4m3"
+    units = e4m3 or (M + N) % 2 == 1
+    x = _wide(rng.normal(size=(M, K)), T[kind], 8)
+    W = _weight_layout(rng.normal(size=(K, N)) * 2 * K ** -0.5, units, T[kind], 8)
+    bias = torch.as_tensor(rng.normal(size=N)).to(DEV).float()
+    res = _wide(rng.normal(size=(M, N)), T[out], 5)
+    sx = torch.as_tensor(rng.uniform(0.5, 2.0, M)).to(DEV).float() if e4m3 else None
+    sw = torch.as_tensor(rng.uniform(0.5, 2.0, N)).to(DEV).float() if e4m3 else None
+    pre_wide, pre = _out(M, N, T[out], 2)
+    wide, y = _out(M, N, T[out], 5)
+    som.som_product(x, W, bias=bias, act=act, residual=res, alpha=-1.5, x_scale=sx, w_scale=sw, y=y, pre=pre)
+    assert _untouched(wide, N) and _untouched(pre_wide, N)
+    x64, W64 = _np(x), _np(W)
+    f = (1.0 if sx is None else _np(sx)[:, None]) * (1.0 if sw is None else _np(sw)[None])
+    want, pre64 = oracle.product(x64, W64, _np(bias), act, _np(res), -1.5, None if sx is None else _np(sx),
+                                 None if sw is None else _np(sw))
+    size = 1.5 * (np.abs(x64) @ np.abs(W64)) * f
+    tol = (K + 8) * 2 * U * size + 4 * U * (np.abs(pre64) + np.abs(_np(bias)))
+    _near(pre, pre64, tol + np.abs(pre64) * HALF[out] + TINY[out], "pre")
+    # |act'| <= 1.13
+    v = oracle.activation(act, pre64)
+    tol = 1.2 * tol + CALC * np.abs(v) + 4 * U * np.abs(pre64) + 2 * U * np.abs(want) + np.abs(want) * HALF[out]
+    _near(y, want, tol + TINY[out], "y")
+    # the residual may be the output itself
+    again = res.clone()
+    som.som_product(x, W, bias=bias, act=act, residual=again, alpha=-1.5, x_scale=sx, w_scale=sw, y=again)
+    assert torch.equal(again, y)
+
+
+def test_product_ignores_what_lies_outside():
+    # infinities in the padding, and a NaN inside reaches its own row or column only
+    rng = np.random.default_rng(5)
+    x = _wide(rng.normal(size=(40, 100)), T["bf16"], 28, fill=float("inf"))
+    W = _wide(rng.normal(size=(100, 72)), T["bf16"], 8, fill=float("inf"))
+    base = som.som_product(x, W)
+    assert bool(base.isfinite().all())
+    x[7, 99] = float("nan")
+    W[99, 31] = float("inf")
+    got = som.som_product(x, W)
+    keep = torch.ones((40, 72), dtype=torch.bool, device=DEV)
+    keep[7] = False
+    keep[:, 31] = False
+    assert torch.equal(got[keep], base[keep]) and bool(got[7].isnan().all()) and not bool(got[:, 31].isfinite().any())
+
+
+def test_scores_of_dense_documents_are_the_units_distances():
+    rng = np.random.default_rng(8)
+    F, N, B = 300, 900, 50
+    ldw = som.som_codebook_ldw(N)
+    W = torch.zeros((F, ldw), dtype=torch.float16, device=DEV)
+    W[:, :N] = torch.as_tensor(rng.random((F, N))).to(DEV).half()
+    norms = som.som_codebook_norms(W, N=N)
+    units = rng.integers(0, N, B)
+    x = W[:, torch.as_tensor(units, device=DEV)].t().contiguous()      # the documents are units
+    scores = som.som_product(x, W[:, :N], bias=norms, alpha=-2.0, dtype=torch.float32)
+    assert torch.equal(scores.argmin(1).cpu(), torch.as_tensor(units))
+    want = ((_np(x)[:, :, None] - _np(W[:, :N])[None]) ** 2).sum(1) - (_np(x) ** 2).sum(1)[:, None]
+    size = 2 * np.abs(_np(x)) @ np.abs(_np(W[:, :N])) + _np(norms)
+    _near(scores, want, (F + 16) * 2 * U * size)
+
+
+BACK_SIZES = [(1, 1, 1), (1, 64, 128), (2, 130, 70), (33, 77, 129), (64, 128, 64), (100, 300, 260), (257, 129, 65),
+              (1000, 40, 90), (520, 512, 256)]
+
+
+@pytest.mark.parametrize("units", [False, True])
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", BACK_SIZES)
+def test_product_gradient_of_integers_is_exact(M, N, K, kind, units):
+    rng = np.random.default_rng(M * 3 + N * 7 + K)
+    x, W, dy = (rng.integers(-1, 2, s).astype(float) for s in ((M, K), (K, N), (M, N)))
+    # at most two non-zero terms per sum beyond 256 would round in the output type:
+    # compare against the exact sums rounded to it
+    for pad in (0, 8 - K % 8, 3):
+        xd, dyd = _wide(x, T[kind], pad), _wide(dy, T[kind], pad)
+        Wd = _weight_layout(W, units, T[kind], pad)
+        dx, dW, dbias = som.som_product_backward(dyd, xd, Wd, alpha=2.0)
+        want = oracle.product_backward(dy, x, W, alpha=2.0)
+        for got, w64, t in ((dx, want[0], T[kind]), (dW, want[1], T[kind]), (dbias, want[2], torch.float32)):
+            assert got.shape == w64.shape
+            assert torch.equal(got, torch.as_tensor(w64).to(t).to(DEV)), (pad, t)
+        assert dW.stride() == ((1, K) if units else (N, 1)) or 1 in (N, K)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("M,N,K,units", [(1, 90, 33, False), (70, 65, 200, True), (300, 136, 128, False)])
+def test_product_gradient(M, N, K, units, kind, act):
+    rng = np.random.default_rng(M + 2 * N + K)
+    x, dy = _wide(rng.normal(size=(M, K)), T[kind], 8), _wide(rng.normal(size=(M, N)) * 0.1, T[kind], 8)
+    W = _weight_layout(rng.normal(size=(K, N)) * K ** -0.5, units, T[kind], 8)
+    pre = _wide(rng.normal(size=(M, N)) * 2, T[kind], 1)
+    dx, dW, dbias = som.som_product_backward(dy, x, W, act=act, pre=None if act == "none" else pre, alpha=0.75)
+    x64, W64, dy64, pre64 = _np(x), _np(W), _np(dy), _np(pre)
+    want = oracle.product_backward(dy64, x64, W64, act, pre64, 0.75)
+    # dP: calculated within 2^-17 of |dy| (1 + |pre|), then rounded for the products
+    dP = np.abs(dy64) if act == "none" else np.abs(dy64 * oracle.activation_grad(act, pre64))
+    off = 0.0 * dy64 if act == "none" else CALC * np.abs(dy64) * (1 + np.abs(pre64))
+    r = off if act == "none" else off + (dP + off) * HALF[kind] + TINY[kind]
+    big = dP + r
+    _near(dx, want[0], 0.75 * (r @ np.abs(W64).T + (N + 8) * 2 * U * (big @ np.abs(W64).T))
+          + (np.abs(want[0])) * HALF[kind] * 1.01 + TINY[kind], "dx")
+    _near(dW, want[1], 0.75 * (np.abs(x64).T @ r + (M + 8) * 2 * U * (np.abs(x64).T @ big))
+          + np.abs(want[1]) * HALF[kind] * 1.01 + TINY[kind], "dW")
+    _near(dbias, want[2], off.sum(0) + (M + 8) * U * dP.sum(0) + 1e-30, "dbias")
+
+
+def test_product_of_no_rows():
+    x, W = torch.empty((0, 64), dtype=torch.float16, device=DEV), torch.ones((64, 32), dtype=torch.float16, device=DEV)
+    assert som.som_product(x, W).shape == (0, 32)
+    dx, dW, dbias = som.som_product_backward(torch.empty((0, 32), dtype=torch.float16, device=DEV), x, W)
+    assert dx.shape == (0, 64) and not bool(dW.any()) and not bool(dbias.any())
+    wide, dW = _out(64, 32, torch.float16, 5)
+    som.som_product_backward(torch.empty((0, 32), dtype=torch.float16, device=DEV), x, W, dW=dW)
+    assert not bool(dW.any()) and _untouched(wide, 32)
+
+
+def test_product_past_32_bits():
+    # the output's last rows start beyond 2^31 elements, x's beyond 2^32 bytes
+    M, K, N, ld = 70001, 64, 31000, 32768
+    x = torch.empty((M, ld), dtype=torch.bfloat16, device=DEV)[:, 8:8 + K]
+    x.copy_(torch.randint(-3, 4, (M, K), device=DEV))
+    W = torch.randint(-3, 4, (K, N), device=DEV).to(torch.bfloat16)
+    y = som.som_product(x, W)
+    for rows in (slice(0, 40), slice(M - 40, M)):
+        want = x[rows].double() @ W.double()
+        assert torch.equal(y[rows].double(), want.to(torch.bfloat16).double())
+    del W
+    # k strided by a long row: the gradient of the weights, contraction over 70,001 rows
+    dy = torch.randint(-1, 2, (M, 16), device=DEV).to(torch.bfloat16)
+    dx, dW, dbias = som.som_product_backward(dy, x, torch.ones((K, 16), dtype=torch.bfloat16, device=DEV))
+    assert torch.equal(dW, (x.double().t().contiguous() @ dy.double()).to(torch.bfloat16))
+    assert torch.equal(dbias.double(), dy.double().sum(0))
+
+
+# --------------------------------------------------------------------------- dropout
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 8), (3, 7), (2, 64), (5, 300), (33, 17), (2, 2055)])
+def test_dropout(rows, cols, kind):
+    rng = np.random.default_rng(rows * 100 + cols)
+    pad = (rows + cols) % 2 * 3
+    x, r = (_wide(rng.normal(size=(rows, cols)), T[kind], pad) for _ in range(2))
+    for p, seed, offset in ((0.3, 1 << 40 | 12345, 7), (0.5, 0, 3 << 33), (0.0, 5, 0), (1.0, 5, 0), (0.999, 9, 1)):
+        for residual in (None, r):
+            want = oracle.dropout(_np(x), p, seed, offset, None if residual is None else _np(residual))
+            wide, y = _out(rows, cols, T[kind], pad)
+            assert som.som_dropout(x, p, seed, offset, residual=residual, y=y) is y and _untouched(wide, cols)
+            size = np.abs(want) + (0 if residual is None else 2 * np.abs(_np(r)))
+            _near(y, want, np.abs(want) * HALF[kind] + 4 * U * size + TINY[kind], (p, residual is None))
+            if residual is None:
+                assert np.array_equal(_np(y) == 0, want == 0)
+
+
+def test_dropout_mask_is_the_same_for_the_gradient_and_in_place():
+    x = torch.randn((40, 333), device=DEV)
+    y = som.som_dropout(x, 0.4, 77, 5)
+    g = som.som_dropout(torch.ones_like(x), 0.4, 77, 5)
+    assert torch.equal(y, x * g)                     # dy/dx is the kept share's inverse or 0
+    wide = torch.randn((40, 500), device=DEV)
+    view = wide[:, 50:383]                           # the mask goes by row and column, not by address
+    view.copy_(x)
+    assert torch.equal(som.som_dropout(view, 0.4, 77, 5), y)
+    som.som_dropout(view, 0.4, 77, 5, y=view)
+    assert torch.equal(view, y)
+    assert torch.equal(som.som_dropout(x[:, :16], 0.4, 77, 5), y[:, :16])
+    r = torch.randn_like(x)
+    want = som.som_dropout(x, 0.4, 77, 5, residual=r)
+    assert torch.equal(som.som_dropout(x, 0.4, 77, 5, residual=r, y=r), want)
+    x[:, 3] = float("nan")                           # a dropped NaN is gone
+    assert torch.equal(som.som_dropout(x, 0.4, 77, 5)[:, 3].isnan(), g[:, 3] != 0)
+    assert som.som_dropout(x[:0], 0.4, 1).shape == (0, 333)
+
+
+def test_dropout_share_of_many():
+    # 2^24 draws: the share kept within five standard deviations, rows and columns unlike
+    n = 4096
+    y = som.som_dropout(torch.ones((n, n), dtype=torch.bfloat16, device=DEV), 0.2, 3)
+    p = 1.0 - round(0.2 * 65536) / 65536
+    kept = (y != 0).double()
+    assert abs(float(kept.mean()) - p) < 5 * np.sqrt(p * (1 - p)) / n
+    sd = np.sqrt(p * (1 - p) / n)
+    assert float((kept.mean(0) - p).abs().max()) < 7 * sd and float((kept.mean(1) - p).abs().max()) < 7 * sd
+
+
+# --------------------------------------------------------------------------- all
+
+def _steps():
+    x, r = (torch.randn((100, 512), device=DEV).to(torch.bfloat16) for _ in range(2))
+    w = torch.randn(512, device=DEV).to(torch.bfloat16)
+    W = (torch.randn((512, 700), device=DEV) * 0.05).to(torch.bfloat16)
+    Wq = W.t().contiguous().to(torch.float8_e4m3fn).t()
+    b = torch.randn(700, device=DEV)
+
+    def step():
+        y, h, _ = som.som_rms_norm(x, w, residual=r)
+        q, _, s = som.som_rms_norm(x, w, residual=r, q8=True)
+        pre = torch.empty((100, 700), dtype=torch.bfloat16, device=DEV)
+        z = som.som_product(y, W, bias=b, act="gelu", pre=pre)
+        zq = som.som_product(q, Wq, bias=b, x_scale=s)
+        one = som.som_product(y[:1], W, bias=b)
+        d = som.som_dropout(z, 0.1, 3, 4, residual=zq)
+        g = som.som_product_backward(d, y, W, act="gelu", pre=pre)
+        return [y, h, q.float(), s, pre, z, zq, one, d, *g, *som.som_rms_norm_backward(g[0], h, w, dh=y)]
+
+    return (x, r, W, b), step
+
+
+def test_another_stream_and_repeats_give_the_same_bits():
+    _, step = _steps()
+    want = step()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream(device=DEV)
+    with torch.cuda.stream(side):
+        got = step()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert all(torch.equal(a, b) for a, b in zip(step(), want))
+
+
+def test_replays_of_a_graph_give_the_eager_result():
+    inputs, step = _steps()
+    side = torch.cuda.Stream(device=DEV)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for k in range(3):
+        for t in inputs:
+            t.copy_(torch.randn(t.shape, device=DEV) * 0.1)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        assert all(torch.equal(a, b) for a, b in zip(got, step())), k
+
+
+def test_the_binding_refuses():
+    x = torch.zeros((4, 64), dtype=torch.bfloat16, device=DEV)
+    W = torch.zeros((64, 32), dtype=torch.bfloat16, device=DEV)
+    for call in (lambda: som.som_rms_norm(x.t()), lambda: som.som_rms_norm(x[:, :1].expand(4, 64)),
+                 lambda: som.som_rms_norm(x, residual=x[:2]), lambda: som.som_rms_norm(x, scale=torch.zeros(4, device=DEV)),
+                 lambda: som.som_rms_norm(x, torch.zeros(63, dtype=torch.bfloat16, device=DEV)),
+                 lambda: som.som_product(x, W[:32]), lambda: som.som_product(x, W, act="swish"),
+                 lambda: som.som_product(x, W[:, ::2]), lambda: som.som_product(x.cpu(), W),
+                 lambda: som.som_product_backward(x[:, :32], x, W, act="silu"), lambda: som.som_dropout(x, 0.1, -1),
+                 lambda: som.som_dropout(x[:1].expand(4, 64), 0.1, 0)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: som.som_rms_norm(x.to(torch.float8_e4m3fn)), lambda: som.som_rms_norm(x, residual=x.float()),
+                 lambda: som.som_product(x, W.half()), lambda: som.som_product(x.float(), W.float()),
+                 lambda: som.som_product(x, W, y=x.float()[:, :32], dtype=torch.bfloat16),
+                 lambda: som.som_product(x, W, bias=torch.zeros(32, dtype=torch.bfloat16, device=DEV)),
+                 lambda: som.som_dropout(x.int(), 0.1, 0)):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: som.som_dropout(x, 1.5, 0), lambda: som.som_dropout(x, float("nan"), 0),
+                 lambda: som.som_rms_norm(x, eps=-1.0),
+                 lambda: som.som_product(x.to(torch.float8_e4m3fn), W.to(torch.float8_e4m3fn)),
+                 lambda: som.som_product(x, W, y=torch.empty((4, 32), dtype=torch.float16, device=DEV))):
+        with pytest.raises(som.SomError):
+            call()
