@@ -47,7 +47,7 @@ struct ProductArgs {
   int64_t ldo;
   int out_type;
   // launch
-  float* partial;            // [splits][I][round_up(J, 4)] or nullptr
+  float* partial;            // [splits][I][round_up(J, 8)] or nullptr
   int64_t k_split;           // elements of k per split (a multiple of the step)
   int splits;
   uint32_t tiles_i, tiles_j, per_xcd;
@@ -138,68 +138,50 @@ __device__ __forceinline__ float act_grad(int act, float v) {
   }
 }
 
-template <typename T>
-__device__ __forceinline__ f4 load4(const void* base, int64_t at, int n) {
-  typedef T v4 __attribute__((ext_vector_type(4)));
-  typedef v4 v4_at __attribute__((aligned(sizeof(T))));
-  const T* p = static_cast<const T*>(base) + at;
-  f4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (n >= 4) {
-    const v4 r = *reinterpret_cast<const v4_at*>(p);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = static_cast<float>(r[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 3; ++e)
-      if (e < n) v[e] = static_cast<float>(p[e]);
-  }
-  return v;
-}
-
-template <typename T>
-__device__ __forceinline__ void store4(void* base, int64_t at, int n, f4 v) {
-  typedef T v4 __attribute__((ext_vector_type(4)));
-  typedef v4 v4_at __attribute__((aligned(sizeof(T))));
-  T* p = static_cast<T*>(base) + at;
-  if (n >= 4) {
-    v4 r;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = static_cast<T>(v[e]);
-    *reinterpret_cast<v4_at*>(p) = r;
-  } else {
-#pragma unroll
-    for (int e = 0; e < 3; ++e)
-      if (e < n) p[e] = static_cast<T>(v[e]);
-  }
-}
-
-__device__ __forceinline__ f4 load4_as(int type, const void* base, int64_t at, int n) {
-  if (type == kF32) return load4<float>(base, at, n);
-  return type == kF16 ? load4<f16>(base, at, n) : load4<bf16>(base, at, n);
-}
-__device__ __forceinline__ void store4_as(int type, void* base, int64_t at, int n, f4 v) {
+__device__ __forceinline__ void load8_as(int type, const void* base, int64_t at, int n, float (&v)[8]) {
   if (type == kF32)
-    store4<float>(base, at, n, v);
+    load8(static_cast<const float*>(base) + at, n, v);
   else if (type == kF16)
-    store4<f16>(base, at, n, v);
+    load8(static_cast<const f16*>(base) + at, n, v);
   else
-    store4<bf16>(base, at, n, v);
+    load8(static_cast<const bf16*>(base) + at, n, v);
+}
+__device__ __forceinline__ void store8_as(int type, void* base, int64_t at, int n, const float (&v)[8]) {
+  if (type == kF32)
+    store8(static_cast<float*>(base) + at, n, v);
+  else if (type == kF16)
+    store8(static_cast<f16*>(base) + at, n, v);
+  else
+    store8(static_cast<bf16*>(base) + at, n, v);
 }
 
-// Columns [j, j + n), n in 1..4, of row i from their sums.
-__device__ __forceinline__ void finish4(const ProductArgs& a, int64_t i, int64_t j, int n, f4 v) {
-  float f = a.alpha;
+// Columns [j, j + n), n in 1..8, of row i from their sums.
+__device__ __forceinline__ void finish8(const ProductArgs& a, int64_t i, int64_t j, int n, float (&v)[8]) {
+  float f = a.alpha, w[8];
   if (a.p_scale) f *= a.p_scale[i];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] *= f;
-  if (a.q_scale) v *= load4<float>(a.q_scale, j, n);
-  if (a.bias) v += load4<float>(a.bias, j, n);
-  if (a.pre) store4_as(a.out_type, a.pre, i * a.ldpre + j, n, v);
-  if (a.act != kActNone)
+  for (int e = 0; e < 8; ++e) v[e] *= f;
+  if (a.q_scale) {
+    load8(a.q_scale + j, n, w);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = act_of(a.act, v[e]);
-  if (a.residual) v += load4_as(a.out_type, a.residual, i * a.ldr + j, n);
-  store4_as(a.out_type, a.out, i * a.ldo + j, n, v);
+    for (int e = 0; e < 8; ++e) v[e] *= w[e];
+  }
+  if (a.bias) {
+    load8(a.bias + j, n, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += w[e];
+  }
+  if (a.pre) store8_as(a.out_type, a.pre, i * a.ldpre + j, n, v);
+  if (a.act != kActNone) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = act_of(a.act, v[e]);
+  }
+  if (a.residual) {
+    load8_as(a.out_type, a.residual, i * a.ldr + j, n, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += w[e];
+  }
+  store8_as(a.out_type, a.out, i * a.ldo + j, n, v);
 }
 
 // ---------------------------------------------------------------------------
@@ -436,11 +418,13 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
   const uint32_t lin = blockIdx.x % kXcds * a.per_xcd + blockIdx.x / kXcds;
   const uint32_t tiles = a.tiles_i * a.tiles_j;
   if (lin >= tiles * a.splits) return;
-  const uint32_t split = lin / tiles, rest = lin % tiles;
-  const uint32_t band = rest / (kBand * a.tiles_j), in = rest % (kBand * a.tiles_j);
+  // (divisions go through the vector unit: back to scalar registers)
+  const uint32_t split = __builtin_amdgcn_readfirstlane(lin / tiles), rest = lin - split * tiles;
+  const uint32_t band = __builtin_amdgcn_readfirstlane(rest / (kBand * a.tiles_j)), in = rest - band * kBand * a.tiles_j;
   const uint32_t height = min(kBand, a.tiles_i - band * kBand);
-  const int64_t i0 = static_cast<int64_t>(band * kBand + in % height) * BI;
-  const int64_t j0 = static_cast<int64_t>(in / height) * BJ;
+  const uint32_t across = __builtin_amdgcn_readfirstlane(in / height);
+  const int64_t i0 = static_cast<int64_t>(band * kBand + (in - across * height)) * BI;
+  const int64_t j0 = static_cast<int64_t>(across) * BJ;
   const int32_t k0 = static_cast<int32_t>(split * a.k_split);
   const int32_t k1 = static_cast<int32_t>(min(a.K, k0 + a.k_split));
 
@@ -460,51 +444,90 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
 #pragma unroll
     for (int y = 0; y < TJ; ++y) acc[x][y] = f4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  auto compute = [&](int slot) {
+  // the fragments of half a step (h) and their products
+  struct Half {
+    i4 q[TJ], p[TI];
+  };
+  auto read = [&](Half& f, int slot, int h) {
     lds_char* sp = l3 + slot * kStage;
     lds_char* sq = sp + OpP::kBytes;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      i4 raw[TJ];
+    for (int y = 0; y < TJ; ++y) f.q[y] = fragment<QKC, BJ>(sq, qb, y, h);
 #pragma unroll
-      for (int y = 0; y < TJ; ++y) raw[y] = fragment<QKC, BJ>(sq, qb, y, h);
+    for (int x = 0; x < TI; ++x) f.p[x] = fragment<PKC, BI>(sp, pb, x, h);
+  };
+  auto multiply = [&](const Half& f) {
 #pragma unroll
-      for (int x = 0; x < TI; ++x) {
-        const Frag<E> fp(fragment<PKC, BI>(sp, pb, x, h));
+    for (int x = 0; x < TI; ++x) {
+      const Frag<E> fp(f.p[x]);
 #pragma unroll
-        for (int y = 0; y < TJ; ++y) acc[x][y] = mfma<E>(Frag<E>(raw[y]), fp, acc[x][y]);
-      }
+      for (int y = 0; y < TJ; ++y) acc[x][y] = mfma<E>(Frag<E>(f.q[y]), fp, acc[x][y]);
     }
+  };
+  // One half's products while the other half is read: a read or two after every few
+  // products, so that neither unit waits for the other's queue.
+  constexpr int kReads = TI * (PKC ? 1 : 2) + TJ * (QKC ? 1 : 2);
+  constexpr int kProducts = TI * TJ * Frag<E>::kParts;
+  constexpr int kRun = kProducts / kReads > 0 ? kProducts / kReads : 1;
+  auto mix = [] {
+#pragma unroll
+    for (int n = 0; n < kReads; ++n) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);       // a read of LDS
+      __builtin_amdgcn_sched_group_barrier(0x008, kRun, 0);    // matrix instructions
+    }
+    __builtin_amdgcn_sched_barrier(0);
   };
 
   const int32_t steps = (k1 - k0 + kStep - 1) / kStep;
   int32_t t = 0;
   if (a.dma && !p.ragged() && !q.ragged()) {
-    // whole steps: NS - 1 on their way while one is worked on
+    // Whole steps.  Step t's second half is read while its first is multiplied; then, all
+    // of step t being read and step t + 1 there, one barrier, step t + NS on its way
+    // into t's place, and t + 1's first half is read while t's second is multiplied.
     const int32_t full = (k1 - k0) / kStep;
     // loads of this wave per step: the last one of P may be the other waves'
     constexpr int kMost = OpP::kEach + OpQ::kEach;
     static_assert(OpQ::whole, "every wave moves the same share of Q");
     const bool most = OpP::whole || (OpP::kEach - 1) * THREADS + wave * 64 < OpP::kChunks;
-    auto fetch = [&](int32_t s) {
-      const uint32_t at = l0 + static_cast<uint32_t>(s % NS) * kStage;
+    auto fetch = [&](int32_t s, int slot) {
+      const uint32_t at = l0 + static_cast<uint32_t>(slot) * kStage;
       p.fetch(k0 + s * kStep, at);
       q.fetch(k0 + s * kStep, at + OpP::kBytes);
     };
-#pragma unroll
-    for (int s = 0; s < NS - 1; ++s)
-      if (s < full) fetch(s);
-    for (; t < full; ++t) {
-      if (NS == 2 || t + NS - 2 >= full)
+    // step s has arrived, with the steps after it up to the newest on their way
+    auto arrived = [&](int32_t s, int after) {
+      if (after == 0 || s + after >= full)
         arrive<0>();
-      else if (most)
-        arrive<(NS - 2) * kMost>();
+      else if (after == 1)
+        most ? arrive<kMost>() : arrive<kMost - 1>();
+      else if (after == 2)
+        most ? arrive<2 * kMost>() : arrive<2 * (kMost - 1)>();
       else
-        arrive<(NS - 2) * (kMost - 1)>();
-      if (t + NS - 1 < full) fetch(t + NS - 1);
-      compute(static_cast<int>(t % NS));
+        most ? arrive<3 * kMost>() : arrive<3 * (kMost - 1)>();
+    };
+    static_assert(NS >= 2 && NS <= 4, "the waits are written for two to four steps");
+    if (full > 0) {
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+        if (s < full) fetch(s, s);
+      arrived(0, NS - 1);
+      Half f[2];
+      read(f[0], 0, 0);
+      int slot = 0;
+      for (; t < full; ++t) {
+        __builtin_amdgcn_sched_barrier(0);
+        read(f[1], slot, 1);
+        multiply(f[0]);
+        mix();
+        arrived(t + 1, NS - 2);
+        if (t + NS < full) fetch(t + NS, slot);
+        slot = slot + 1 == NS ? 0 : slot + 1;
+        __builtin_amdgcn_sched_barrier(0);
+        read(f[0], slot, 0);           // (after the last step: bytes that no product uses)
+        multiply(f[1]);
+        mix();
+      }
     }
-    arrive<0>();
   }
   if (t < steps) {
     u4 vp[OpP::kEach], vq[OpQ::kEach];
@@ -518,28 +541,48 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
         p.load(k0 + (t + 1) * kStep, k1, vp);
         q.load(k0 + (t + 1) * kStep, k1, vq);
       }
-      compute(slot);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        Half f;
+        read(f, slot, h);
+        multiply(f);
+      }
     }
   }
 
+  // The epilogue by rows: 16 rows of the wave's columns at a time go through its own
+  // part of LDS, so that a lane has eight consecutive columns and the wave's reads and
+  // writes of C are whole lines.  (Four floats of padding: the 16 lanes that write a
+  // column of quads start at different banks.)
+  constexpr int kCols = TJ * 16, kPad = kCols + 4, kLanes = kCols / 8, kRows = 64 / kLanes;
+  static_assert(WI * WJ * 16 * kPad * 4 <= NS * kStage, "the rows fit the steps' place");
+  __syncthreads();                     // every wave is done with the steps
+  typedef __attribute__((address_space(3))) f4 lds_f4;
+  lds_char* const mine = l3 + wave * (16 * kPad * 4);
   const int lane = threadIdx.x & 63;
+  const int col = lane % kLanes * 8;
+  const int64_t j = j0 + wj * kCols + col;
+  const int n = static_cast<int>(min<int64_t>(8, a.J - j));
 #pragma unroll
   for (int x = 0; x < TI; ++x) {
-    const int64_t i = i0 + (wi * TI + x) * 16 + (lane & 15);
-    if (i < a.I) {
 #pragma unroll
-      for (int y = 0; y < TJ; ++y) {
-        const int64_t j = j0 + (wj * TJ + y) * 16 + (lane >> 4) * 4;
-        if (j < a.J) {
-          if (a.splits > 1) {
-            const int64_t ld = (a.J + 3) / 4 * 4;
-            *reinterpret_cast<f4*>(a.partial + (split * a.I + i) * ld + j) = acc[x][y];
-          } else {
-            finish4(a, i, j, static_cast<int>(min<int64_t>(4, a.J - j)), acc[x][y]);
-          }
-        }
+    for (int y = 0; y < TJ; ++y)
+      *reinterpret_cast<lds_f4*>(mine + ((lane & 15) * kPad + y * 16 + (lane >> 4) * 4) * 4) = acc[x][y];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int r = lane / kLanes; r < 16; r += kRows) {
+      const f4 lo = *reinterpret_cast<lds_f4*>(mine + (r * kPad + col) * 4);
+      const f4 hi = *reinterpret_cast<lds_f4*>(mine + (r * kPad + col + 4) * 4);
+      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      const int64_t i = i0 + (wi * TI + x) * 16 + r;
+      if (i < a.I && n > 0) {
+        if (a.splits > 1)
+          store8(a.partial + (split * a.I + i) * ((a.J + 7) / 8 * 8) + j, 8, v);
+        else
+          finish8(a, i, j, n, v);
       }
     }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 

@@ -5,17 +5,21 @@
 namespace som {
 namespace {
 
-// C from its partial sums, added in the order of the splits; four columns a thread.
+// C from its partial sums, added in the order of the splits; eight columns a thread.
 __global__ void __launch_bounds__(256) k_join(const ProductArgs a) {
-  const int64_t ld = (a.J + 3) / 4 * 4, quads = ld / 4;
+  const int64_t ld = (a.J + 7) / 8 * 8, groups = ld / 8;
   const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (at >= quads * a.I) return;
-  const int64_t i = at / quads, j = at % quads * 4;
-  const f4* p = reinterpret_cast<const f4*>(a.partial + i * ld + j);
-  const int64_t step = a.I * ld / 4;
-  f4 v = p[0];
-  for (int s = 1; s < a.splits; ++s) v += p[s * step];
-  finish4(a, i, j, static_cast<int>(min<int64_t>(4, a.J - j)), v);
+  if (at >= groups * a.I) return;
+  const int64_t i = at / groups, j = at % groups * 8;
+  const float* p = a.partial + i * ld + j;
+  float v[8], w[8];
+  load8(p, 8, v);
+  for (int s = 1; s < a.splits; ++s) {
+    load8(p + s * a.I * ld, 8, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += w[e];
+  }
+  finish8(a, i, j, static_cast<int>(min<int64_t>(8, a.J - j)), v);
 }
 
 // 512 columns (64 lanes of 8) x every (4 gridDim.y)th row; the four waves' column
@@ -89,7 +93,7 @@ ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc) {
   const int64_t per = (steps + splits - 1) / splits;
   splits = (steps + per - 1) / per;
   ProductPlan p{shape, static_cast<int>(splits), per * step, 0};
-  if (splits > 1) p.partial_floats = static_cast<size_t>(splits) * I * ((J + 3) / 4 * 4);
+  if (splits > 1) p.partial_floats = static_cast<size_t>(splits) * I * ((J + 7) / 8 * 8);
   return p;
 }
 
@@ -112,8 +116,8 @@ hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream) {
                  : a.elem == kBF16 ? launch_product_bf16(p.shape, a, stream)
                                    : launch_product_e4m3(p.shape, a, stream);
   if (e != hipSuccess || p.splits == 1) return e;
-  const int64_t quads = (a.J + 3) / 4 * a.I;
-  hipLaunchKernelGGL(k_join, dim3(static_cast<uint32_t>((quads + 255) / 256)), dim3(256), 0, stream, a);
+  const int64_t groups = (a.J + 7) / 8 * a.I;
+  hipLaunchKernelGGL(k_join, dim3(static_cast<uint32_t>((groups + 255) / 256)), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
