@@ -97,18 +97,38 @@ constexpr int64_t kDmaMaxLd = int64_t(1) << 22;   // elements: a tile's offsets 
 
 constexpr int kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSilu = 4;   // som_act
 
-// 1 / (1 + e^-z); e^-z = infinity gives 0.
-__device__ __forceinline__ float sigmoid(float z) { return 1.0f / (1.0f + __expf(-z)); }
+constexpr float kLog2e = 1.4426950408889634f;
+
+// 1 / (1 + e^-z), within a few units of fp32; e^-z = infinity gives 0.
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * z));
+}
 
 constexpr float kGeluK = 1.5957691216057308f;     // 2 sqrt(2 / pi): 1 + tanh(z) = 2 sigmoid(2 z)
 constexpr float kGeluC = 0.044715f;
 
+// The normal distribution's share below v, and e^(-v^2 / 2): erfc by the rational
+// approximation 7.1.26 of Abramowitz and Stegun (Handbook of Mathematical Functions),
+// within 1.5e-7; the small side is calculated and the large one is its complement, so a
+// negative v does not lose digits.
+__device__ __forceinline__ float normal_below(float v, float* e) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(v), 1.0f));
+  float s = fmaf(t, 1.061405429f, -1.453152027f);
+  s = fmaf(t, s, 1.421413741f);
+  s = fmaf(t, s, -0.284496736f);
+  s = fmaf(t, s, 0.254829592f);
+  *e = __builtin_amdgcn_exp2f(-0.5f * kLog2e * v * v);
+  const float tail = 0.5f * t * s * *e;
+  return v >= 0.0f ? 1.0f - tail : tail;
+}
+
 __device__ __forceinline__ float act_of(int act, float v) {
+  float e;
   switch (act) {
     case kActRelu:
       return v > 0.0f ? v : (v != v ? v : 0.0f);
     case kActGelu:
-      return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+      return v * normal_below(v, &e);
     case kActGeluTanh:
       return v * sigmoid(kGeluK * (v + kGeluC * v * v * v));
     case kActSilu:
@@ -123,8 +143,11 @@ __device__ __forceinline__ float act_grad(int act, float v) {
   switch (act) {
     case kActRelu:
       return v > 0.0f ? 1.0f : 0.0f;
-    case kActGelu:
-      return 0.5f * (1.0f + erff(v * 0.70710678118654752f)) + v * __expf(-0.5f * v * v) * 0.39894228040143268f;
+    case kActGelu: {
+      float e;
+      const float below = normal_below(v, &e);
+      return fmaf(v * e, 0.39894228040143268f, below);
+    }
     case kActGeluTanh: {
       const float s = sigmoid(kGeluK * (v + kGeluC * v * v * v));
       return s + v * s * (1.0f - s) * kGeluK * (1.0f + 3.0f * kGeluC * v * v);
@@ -138,14 +161,6 @@ __device__ __forceinline__ float act_grad(int act, float v) {
   }
 }
 
-__device__ __forceinline__ void load8_as(int type, const void* base, int64_t at, int n, float (&v)[8]) {
-  if (type == kF32)
-    load8(static_cast<const float*>(base) + at, n, v);
-  else if (type == kF16)
-    load8(static_cast<const f16*>(base) + at, n, v);
-  else
-    load8(static_cast<const bf16*>(base) + at, n, v);
-}
 __device__ __forceinline__ void store8_as(int type, void* base, int64_t at, int n, const float (&v)[8]) {
   if (type == kF32)
     store8(static_cast<float*>(base) + at, n, v);
@@ -155,31 +170,77 @@ __device__ __forceinline__ void store8_as(int type, void* base, int64_t at, int 
     store8(static_cast<bf16*>(base) + at, n, v);
 }
 
+// What the epilogue takes from memory for eight columns: of all rows, and of one row
+// (the residual as it lies there, so that it can be asked for ahead of its use).
+struct ColumnTerms {
+  float scale[8], bias[8];
+};
+struct RowTerms {
+  float scale;
+  u4 residual[2];
+};
+
+// n <= 0: nothing is read
+__device__ __forceinline__ ColumnTerms column_terms(const ProductArgs& a, int64_t j, int n) {
+  ColumnTerms c;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    c.scale[e] = 1.0f;
+    c.bias[e] = 0.0f;
+  }
+  if (a.q_scale) load8(a.q_scale + j, n, c.scale);
+  if (a.bias) load8(a.bias + j, n, c.bias);
+  return c;
+}
+
+__device__ __forceinline__ RowTerms row_terms(const ProductArgs& a, int64_t i, int64_t j, int n) {
+  RowTerms r;
+  r.scale = a.alpha;
+  r.residual[0] = r.residual[1] = u4{0, 0, 0, 0};
+  if (n <= 0) return r;
+  if (a.p_scale) r.scale *= a.p_scale[i];
+  if (!a.residual) return r;
+  if (a.out_type == kF32) {
+    const float* p = static_cast<const float*>(a.residual) + i * a.ldr + j;
+    if (n == 8) {
+      r.residual[0] = *reinterpret_cast<const u4_at2*>(p);
+      r.residual[1] = *reinterpret_cast<const u4_at2*>(p + 4);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (e < n) r.residual[e / 4][e % 4] = __float_as_uint(p[e]);
+    }
+  } else {
+    const uint16_t* p = static_cast<const uint16_t*>(a.residual) + i * a.ldr + j;
+    if (n == 8) {
+      r.residual[0] = *reinterpret_cast<const u4_at2*>(p);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (e < n) r.residual[0][e / 2] |= static_cast<uint32_t>(p[e]) << (16 * (e % 2));
+    }
+  }
+  return r;
+}
+
 // Columns [j, j + n), n in 1..8, of row i from their sums.
-__device__ __forceinline__ void finish8(const ProductArgs& a, int64_t i, int64_t j, int n, float (&v)[8]) {
-  float f = a.alpha, w[8];
-  if (a.p_scale) f *= a.p_scale[i];
+__device__ __forceinline__ void finish8(const ProductArgs& a, int64_t i, int64_t j, int n, float (&v)[8],
+                                        const ColumnTerms& c, const RowTerms& r) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] *= f;
-  if (a.q_scale) {
-    load8(a.q_scale + j, n, w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= w[e];
-  }
-  if (a.bias) {
-    load8(a.bias + j, n, w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += w[e];
-  }
+  for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e] * r.scale, c.scale[e], c.bias[e]);
   if (a.pre) store8_as(a.out_type, a.pre, i * a.ldpre + j, n, v);
   if (a.act != kActNone) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = act_of(a.act, v[e]);
   }
   if (a.residual) {
-    load8_as(a.out_type, a.residual, i * a.ldr + j, n, w);
+    typedef f16 h8 __attribute__((ext_vector_type(8)));
+    typedef bf16 b8 __attribute__((ext_vector_type(8)));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += w[e];
+    for (int e = 0; e < 8; ++e)
+      v[e] += a.out_type == kF32   ? __uint_as_float(r.residual[e / 4][e % 4])
+              : a.out_type == kF16 ? static_cast<float>(__builtin_bit_cast(h8, r.residual[0])[e])
+                                   : static_cast<float>(__builtin_bit_cast(b8, r.residual[0])[e]);
   }
   store8_as(a.out_type, a.out, i * a.ldo + j, n, v);
 }
@@ -233,7 +294,8 @@ struct Operand {
   const char* base;      // the tile's first row (KC) or column, at k = 0
   int64_t ld;            // bytes per row
   int64_t rows;          // rows (KC) or columns of the matrix from the tile's first on
-  uint32_t off[kEach];
+  uint32_t off;          // this thread's first chunk from the tile's start
+  uint32_t over;         // the same chunk of the tile's first row (KC)
 
   // this thread's nth chunk: position in LDS, and its row and first element
   static __device__ __forceinline__ int pos(int n) { return n * THREADS + static_cast<int>(threadIdx.x); }
@@ -254,28 +316,33 @@ struct Operand {
     ld = ld_elems * ES;
     base = uniform(static_cast<const char*>(p) + (KC ? first * ld : first * ES));
     rows = extent - first;
-#pragma unroll
-    for (int n = 0; n < kEach; ++n) {
-      int r, c;
-      place(pos(n), &r, &c);
-      // rows and chunks past the matrix: the first one again, whose sums are not kept
-      if constexpr (KC)
-        off[n] = static_cast<uint32_t>((r < rows ? r : 0) * ld + c * 16);
-      else
-        off[n] = static_cast<uint32_t>(r * ld + (c * 8 < rows ? c : 0) * 16);
-    }
+    int r, c;
+    place(pos(0), &r, &c);
+    // chunks past the matrix's columns: the tile's first one, whose sums are not kept
+    if (!KC && c * 8 >= rows) c = 0;
+    off = static_cast<uint32_t>(r * ld + c * 16);
+    over = static_cast<uint32_t>(c * 16);
   }
   // columns that end inside a chunk of this tile
   __device__ __forceinline__ bool ragged() const { return !KC && rows < BR && rows % 8 != 0; }
   __device__ __forceinline__ const char* at(int32_t k) const { return base + (KC ? int64_t(k) * ES : k * ld); }
 
-  // whole step from k on, asynchronously
-  __device__ __forceinline__ void fetch(int32_t k, uint32_t lds) const {
-    const char* b = uniform(at(k));
+  // Whole step from k on, asynchronously.  A thread's chunks lie kRowsEach rows apart at
+  // one place of their rows (the swizzles repeat after 16 rows).  Rows past the matrix:
+  // the tile's first one again.
+  static constexpr int kRowsEach = KC ? THREADS / 8 : THREADS / (BR / 8);
+  static_assert(kEach == 1 || kRowsEach % 16 == 0, "a thread's chunks are swizzled alike");
+  // nth of the kEach loads of this wave
+  __device__ __forceinline__ void fetch(int n, int32_t k, uint32_t lds) const {
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-    for (int n = 0; n < kEach; ++n)
-      if (whole || n * THREADS + wave * 64 < kChunks) dma16(b, off[n], lds + (n * THREADS + wave * 64) * 16);
+    lds += wave * 1024 + n * THREADS * 16;
+    if (!whole && n * THREADS + wave * 64 >= kChunks) return;
+    if constexpr (!KC) {
+      dma16(at(k) + n * (kRowsEach * ld), off, lds);
+    } else {
+      const int r = (threadIdx.x >> 3) + n * kRowsEach;
+      dma16(at(k), r < rows ? off + static_cast<uint32_t>(n * kRowsEach * ld) : over, lds);
+    }
   }
 
   // step [k, end) through registers
@@ -400,6 +467,13 @@ __device__ __forceinline__ f4 mfma(const Frag<E>& q, const Frag<E>& p, f4 c) {
 // The kernel
 // ---------------------------------------------------------------------------
 
+struct Yes {
+  static constexpr bool value = true;
+};
+struct No {
+  static constexpr bool value = false;
+};
+
 // WI x WJ waves, each with TI x TJ tiles of 16 x 16; NS steps in LDS.
 template <int E, bool PKC, bool QKC, int WI, int WJ, int TI, int TJ, int NS>
 __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
@@ -444,55 +518,47 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
 #pragma unroll
     for (int y = 0; y < TJ; ++y) acc[x][y] = f4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  // the fragments of half a step (h) and their products
+  // the fragments of half a step
   struct Half {
     i4 q[TJ], p[TI];
   };
-  auto read = [&](Half& f, int slot, int h) {
+  auto read_one = [&](Half& f, int slot, int h, int r) {
     lds_char* sp = l3 + slot * kStage;
-    lds_char* sq = sp + OpP::kBytes;
-#pragma unroll
-    for (int y = 0; y < TJ; ++y) f.q[y] = fragment<QKC, BJ>(sq, qb, y, h);
-#pragma unroll
-    for (int x = 0; x < TI; ++x) f.p[x] = fragment<PKC, BI>(sp, pb, x, h);
+    if (r < TJ)
+      f.q[r] = fragment<QKC, BJ>(sp + OpP::kBytes, qb, r, h);
+    else
+      f.p[r - TJ] = fragment<PKC, BI>(sp, pb, r - TJ, h);
   };
-  auto multiply = [&](const Half& f) {
+  auto read = [&](Half& f, int slot, int h) {
 #pragma unroll
-    for (int x = 0; x < TI; ++x) {
-      const Frag<E> fp(f.p[x]);
-#pragma unroll
-      for (int y = 0; y < TJ; ++y) acc[x][y] = mfma<E>(Frag<E>(f.q[y]), fp, acc[x][y]);
-    }
+    for (int r = 0; r < TJ + TI; ++r) read_one(f, slot, h, r);
   };
-  // One half's products while the other half is read: a read or two after every few
-  // products, so that neither unit waits for the other's queue.
-  constexpr int kReads = TI * (PKC ? 1 : 2) + TJ * (QKC ? 1 : 2);
-  constexpr int kProducts = TI * TJ * Frag<E>::kParts;
-  constexpr int kRun = kProducts / kReads > 0 ? kProducts / kReads : 1;
-  auto mix = [] {
+  auto multiply_row = [&](const Half& f, int x) {
+    const Frag<E> fp(f.p[x]);
 #pragma unroll
-    for (int n = 0; n < kReads; ++n) {
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);       // a read of LDS
-      __builtin_amdgcn_sched_group_barrier(0x008, kRun, 0);    // matrix instructions
-    }
-    __builtin_amdgcn_sched_barrier(0);
+    for (int y = 0; y < TJ; ++y) acc[x][y] = mfma<E>(Frag<E>(f.q[y]), fp, acc[x][y]);
   };
 
   const int32_t steps = (k1 - k0 + kStep - 1) / kStep;
   int32_t t = 0;
   if (a.dma && !p.ragged() && !q.ragged()) {
     // Whole steps.  Step t's second half is read while its first is multiplied; then, all
-    // of step t being read and step t + 1 there, one barrier, step t + NS on its way
-    // into t's place, and t + 1's first half is read while t's second is multiplied.
+    // of step t being read and step t + 1 there, one barrier; t + 1's first half is read
+    // while t's second is multiplied, and step t + NS is sent for into t's place.  Reads
+    // and loads are spread over the products, row of tiles by row: a wave issues in order,
+    // and one that waits for the memory unit's queue starts no product (all loads of a
+    // step at once: 1,313 TFLOP/s at 8,192^3 in bf16).
     const int32_t full = (k1 - k0) / kStep;
     // loads of this wave per step: the last one of P may be the other waves'
     constexpr int kMost = OpP::kEach + OpQ::kEach;
     static_assert(OpQ::whole, "every wave moves the same share of Q");
     const bool most = OpP::whole || (OpP::kEach - 1) * THREADS + wave * 64 < OpP::kChunks;
-    auto fetch = [&](int32_t s, int slot) {
+    auto fetch_one = [&](int n, int32_t s, int slot) {
       const uint32_t at = l0 + static_cast<uint32_t>(slot) * kStage;
-      p.fetch(k0 + s * kStep, at);
-      q.fetch(k0 + s * kStep, at + OpP::kBytes);
+      if (n < OpP::kEach)
+        p.fetch(n, k0 + s * kStep, at);
+      else
+        q.fetch(n - OpP::kEach, k0 + s * kStep, at + OpP::kBytes);
     };
     // step s has arrived, with the steps after it up to the newest on their way
     auto arrived = [&](int32_t s, int after) {
@@ -506,27 +572,41 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
         most ? arrive<3 * kMost>() : arrive<3 * (kMost - 1)>();
     };
     static_assert(NS >= 2 && NS <= 4, "the waits are written for two to four steps");
+    Half f[2];
+    int slot = 0;
+    // products of `now`; half h of the step in `from` into `next`; with kFetch step s into `to`
+    auto phase = [&](const Half& now, Half& next, int from, int h, auto fetches, int32_t s, int to) {
+      constexpr bool kFetch = decltype(fetches)::value;
+#pragma unroll
+      for (int x = 0; x < TI; ++x) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int r = x * (TI + TJ) / TI; r < (x + 1) * (TI + TJ) / TI; ++r) read_one(next, from, h, r);
+        if constexpr (kFetch) {
+#pragma unroll
+          for (int n = x * kMost / TI; n < (x + 1) * kMost / TI; ++n) fetch_one(n, s, to);
+        }
+        multiply_row(now, x);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto step = [&](auto fetches) {
+      phase(f[0], f[1], slot, 1, No{}, 0, 0);
+      arrived(t + 1, NS - 2);
+      const int place = slot;
+      slot = slot + 1 == NS ? 0 : slot + 1;
+      phase(f[1], f[0], slot, 0, fetches, t + NS, place);    // (after the last step: bytes that no product uses)
+    };
     if (full > 0) {
 #pragma unroll
       for (int s = 0; s < NS; ++s)
-        if (s < full) fetch(s, s);
+        if (s < full)
+#pragma unroll
+          for (int n = 0; n < kMost; ++n) fetch_one(n, s, s);
       arrived(0, NS - 1);
-      Half f[2];
       read(f[0], 0, 0);
-      int slot = 0;
-      for (; t < full; ++t) {
-        __builtin_amdgcn_sched_barrier(0);
-        read(f[1], slot, 1);
-        multiply(f[0]);
-        mix();
-        arrived(t + 1, NS - 2);
-        if (t + NS < full) fetch(t + NS, slot);
-        slot = slot + 1 == NS ? 0 : slot + 1;
-        __builtin_amdgcn_sched_barrier(0);
-        read(f[0], slot, 0);           // (after the last step: bytes that no product uses)
-        multiply(f[1]);
-        mix();
-      }
+      for (; t < full - NS; ++t) step(Yes{});
+      for (; t < full; ++t) step(No{});
     }
   }
   if (t < steps) {
@@ -545,44 +625,63 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
       for (int h = 0; h < 2; ++h) {
         Half f;
         read(f, slot, h);
-        multiply(f);
+#pragma unroll
+        for (int x = 0; x < TI; ++x) multiply_row(f, x);
       }
     }
   }
 
   // The epilogue by rows: 16 rows of the wave's columns at a time go through its own
   // part of LDS, so that a lane has eight consecutive columns and the wave's reads and
-  // writes of C are whole lines.  (Four floats of padding: the 16 lanes that write a
-  // column of quads start at different banks.)
-  constexpr int kCols = TJ * 16, kPad = kCols + 4, kLanes = kCols / 8, kRows = 64 / kLanes;
-  static_assert(WI * WJ * 16 * kPad * 4 <= NS * kStage, "the rows fit the steps' place");
+  // writes of C are whole lines.  Quads of columns are swizzled by row: the 16 lanes that
+  // write a quad of their rows, and the ones that read two rows, meet no bank twice.
+  // What a row needs from memory is asked for kAhead groups of rows before.
+  constexpr int kCols = TJ * 16, kLanes = kCols / 8, kRows = 64 / kLanes, kGroups = TI * 16 / kRows;
+  constexpr int kAhead = kGroups < 4 ? kGroups : 4;
+  static_assert(WI * WJ * 16 * kCols * 4 <= NS * kStage, "the rows fit the steps' place");
+  static_assert(TJ == 2 || TJ == 4, "8 or 16 quads per row");
   __syncthreads();                     // every wave is done with the steps
   typedef __attribute__((address_space(3))) f4 lds_f4;
-  lds_char* const mine = l3 + wave * (16 * kPad * 4);
+  lds_char* const mine = l3 + wave * (16 * kCols * 4);
   const int lane = threadIdx.x & 63;
-  const int col = lane % kLanes * 8;
-  const int64_t j = j0 + wj * kCols + col;
+  auto quad = [&](int row, int k) {
+    const int sw = TJ == 4 ? row : row >> 1;
+    return reinterpret_cast<lds_f4*>(mine + (row * kCols + ((k ^ sw) & (TJ * 4 - 1)) * 4) * 4);
+  };
+  const int col = lane % kLanes;
+  const int64_t j = j0 + wj * kCols + col * 8;
   const int n = static_cast<int>(min<int64_t>(8, a.J - j));
+  const int64_t first = i0 + wi * TI * 16 + lane / kLanes;      // group g: row first + g * kRows
+  auto inside = [&](int g) { return first + g * kRows < a.I ? n : 0; };
+  ColumnTerms ct;
+  RowTerms rt[kAhead];
+  if (a.splits == 1) {
+    ct = column_terms(a, j, n);
 #pragma unroll
-  for (int x = 0; x < TI; ++x) {
+    for (int g = 0; g < kAhead; ++g) rt[g] = row_terms(a, first + g * kRows, j, inside(g));
+  }
 #pragma unroll
-    for (int y = 0; y < TJ; ++y)
-      *reinterpret_cast<lds_f4*>(mine + ((lane & 15) * kPad + y * 16 + (lane >> 4) * 4) * 4) = acc[x][y];
-    __builtin_amdgcn_wave_barrier();
+  for (int g = 0; g < kGroups; ++g) {
+    constexpr int kPer = 16 / kRows;     // groups per 16 rows
+    const int x = g / kPer;
+    if (g % kPer == 0) {
 #pragma unroll
-    for (int r = lane / kLanes; r < 16; r += kRows) {
-      const f4 lo = *reinterpret_cast<lds_f4*>(mine + (r * kPad + col) * 4);
-      const f4 hi = *reinterpret_cast<lds_f4*>(mine + (r * kPad + col + 4) * 4);
-      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      const int64_t i = i0 + (wi * TI + x) * 16 + r;
-      if (i < a.I && n > 0) {
-        if (a.splits > 1)
-          store8(a.partial + (split * a.I + i) * ((a.J + 7) / 8 * 8) + j, 8, v);
-        else
-          finish8(a, i, j, n, v);
-      }
+      for (int y = 0; y < TJ; ++y) *quad(lane & 15, y * 4 + (lane >> 4)) = acc[x][y];
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_wave_barrier();
+    const int row = g % kPer * kRows + lane / kLanes;
+    const f4 lo = *quad(row, 2 * col), hi = *quad(row, 2 * col + 1);
+    if (g % kPer == kPer - 1) __builtin_amdgcn_wave_barrier();
+    float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    const int64_t i = first + g * kRows;
+    const int m = inside(g);
+    if (a.splits > 1) {
+      if (m > 0) store8(a.partial + (split * a.I + i) * ((a.J + 7) / 8 * 8) + j, 8, v);
+    } else {
+      const RowTerms now = rt[g % kAhead];
+      if (g + kAhead < kGroups) rt[g % kAhead] = row_terms(a, i + kAhead * kRows, j, inside(g + kAhead));
+      if (m > 0) finish8(a, i, j, m, v, ct, now);
+    }
   }
 }
 

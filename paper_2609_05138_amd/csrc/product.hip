@@ -19,7 +19,8 @@ __global__ void __launch_bounds__(256) k_join(const ProductArgs a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += w[e];
   }
-  finish8(a, i, j, static_cast<int>(min<int64_t>(8, a.J - j)), v);
+  const int n = static_cast<int>(min<int64_t>(8, a.J - j));
+  finish8(a, i, j, n, v, column_terms(a, j, n), row_terms(a, i, j, n));
 }
 
 // 512 columns (64 lanes of 8) x every (4 gridDim.y)th row; the four waves' column
