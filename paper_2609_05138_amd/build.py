@@ -22,7 +22,7 @@ ARCH = "gfx950"
 
 SOURCES = ["api.hip", "norms.hip", "plan.hip", "plan_list.hip", "search.hip", "search_f16.hip", "cluster.hip", "update.hip",
            "probe.hip", "api_dense.hip", "rms_norm.hip", "dropout.hip", "product.hip", "product_f16.hip",
-           "product_bf16.hip", "product_e4m3.hip"]
+           "product_bf16.hip", "product_e4m3.hip", "product_few.hip"]
 
 # Packed fp32 instructions are switched off for every device compile.
 CFLAGS = [

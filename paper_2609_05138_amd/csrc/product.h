@@ -54,8 +54,14 @@ struct ProductArgs {
   bool dma;                  // rows of both operands start on 16 bytes
 };
 
-// Tile shapes (rows of C x columns): 256 x 256, 128 x 128, 64 x 128, 32 x 128, 16 x 128.
-enum Shape { kShape256 = 0, kShape128, kShape64, kShape32, kShape16, kShapes };
+// Tile shapes, and the kernel of few rows (product_few.hip).
+enum Shape { kShape256 = 0, kShape128, kShape64, kShape32, kShape16, kShapes, kFew = kShapes };
+struct ShapeInfo {
+  int bi, bj;                // rows and columns of C
+  int wgs;                   // workgroups that a CU holds
+};
+constexpr ShapeInfo kInfo[kShapes] = {{256, 256, 1}, {128, 128, 2}, {64, 128, 3}, {32, 128, 2}, {16, 128, 2}};
+constexpr int64_t kFewRows = 4;
 struct ProductPlan {
   int shape;
   int splits;
@@ -69,6 +75,7 @@ hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream);
 hipError_t launch_product_f16(int shape, const ProductArgs& a, hipStream_t stream);
 hipError_t launch_product_bf16(int shape, const ProductArgs& a, hipStream_t stream);
 hipError_t launch_product_e4m3(int shape, const ProductArgs& a, hipStream_t stream);
+hipError_t launch_product_few(const ProductArgs& a, hipStream_t stream);
 
 // dP = dy act'(pre), rounded to the type, and dP's column sums.
 struct ActGradArgs {
@@ -122,19 +129,22 @@ __device__ __forceinline__ float normal_below(float v, float* e) {
   return v >= 0.0f ? 1.0f - tail : tail;
 }
 
-__device__ __forceinline__ float act_of(int act, float v) {
-  float e;
-  switch (act) {
-    case kActRelu:
-      return v > 0.0f ? v : (v != v ? v : 0.0f);
-    case kActGelu:
-      return v * normal_below(v, &e);
-    case kActGeluTanh:
-      return v * sigmoid(kGeluK * (v + kGeluC * v * v * v));
-    case kActSilu:
-      return v * sigmoid(v);
-    default:
-      return v;
+__device__ __forceinline__ void act8(int act, float (&v)[8]) {
+  if (act == kActNone) return;
+  if (act == kActRelu) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = v[e] > 0.0f ? v[e] : (v[e] != v[e] ? v[e] : 0.0f);
+  } else if (act == kActGelu) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float exponential;
+      v[e] *= normal_below(v[e], &exponential);
+    }
+  } else {
+    // gelu_tanh: v sigmoid(k (v + c v^3)); silu: v sigmoid(v)
+    const float k = act == kActSilu ? 1.0f : kGeluK, c = act == kActSilu ? 0.0f : kGeluK * kGeluC;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= sigmoid(v[e] * (act == kActSilu ? 1.0f : fmaf(c, v[e] * v[e], k)));
   }
 }
 
@@ -161,7 +171,9 @@ __device__ __forceinline__ float act_grad(int act, float v) {
   }
 }
 
+template <bool kWhole>
 __device__ __forceinline__ void store8_as(int type, void* base, int64_t at, int n, const float (&v)[8]) {
+  if (kWhole) n = 8;
   if (type == kF32)
     store8(static_cast<float*>(base) + at, n, v);
   else if (type == kF16)
@@ -223,26 +235,40 @@ __device__ __forceinline__ RowTerms row_terms(const ProductArgs& a, int64_t i, i
   return r;
 }
 
+// The residual's eight values.
+__device__ __forceinline__ void residual8(int type, const RowTerms& r, float (&v)[8]) {
+  typedef f16 h8 __attribute__((ext_vector_type(8)));
+  if (type == kF32) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(r.residual[e / 4][e % 4]);
+  } else if (type == kF16) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += static_cast<float>(__builtin_bit_cast(h8, r.residual[0])[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      v[e] += __uint_as_float(e % 2 ? r.residual[0][e / 2] & 0xffff0000u : r.residual[0][e / 2] << 16);
+  }
+}
+
+template <bool kWhole>
+__device__ __forceinline__ void finish_some(const ProductArgs& a, int64_t i, int64_t j, int n, float (&v)[8],
+                                            const ColumnTerms& c, const RowTerms& r) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e] * r.scale, c.scale[e], c.bias[e]);
+  if (a.pre) store8_as<kWhole>(a.out_type, a.pre, i * a.ldpre + j, n, v);
+  act8(a.act, v);
+  if (a.residual) residual8(a.out_type, r, v);
+  store8_as<kWhole>(a.out_type, a.out, i * a.ldo + j, n, v);
+}
+
 // Columns [j, j + n), n in 1..8, of row i from their sums.
 __device__ __forceinline__ void finish8(const ProductArgs& a, int64_t i, int64_t j, int n, float (&v)[8],
                                         const ColumnTerms& c, const RowTerms& r) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e] * r.scale, c.scale[e], c.bias[e]);
-  if (a.pre) store8_as(a.out_type, a.pre, i * a.ldpre + j, n, v);
-  if (a.act != kActNone) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = act_of(a.act, v[e]);
-  }
-  if (a.residual) {
-    typedef f16 h8 __attribute__((ext_vector_type(8)));
-    typedef bf16 b8 __attribute__((ext_vector_type(8)));
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      v[e] += a.out_type == kF32   ? __uint_as_float(r.residual[e / 4][e % 4])
-              : a.out_type == kF16 ? static_cast<float>(__builtin_bit_cast(h8, r.residual[0])[e])
-                                   : static_cast<float>(__builtin_bit_cast(b8, r.residual[0])[e]);
-  }
-  store8_as(a.out_type, a.out, i * a.ldo + j, n, v);
+  if (n == 8)
+    finish_some<true>(a, i, j, n, v, c, r);
+  else
+    finish_some<false>(a, i, j, n, v, c, r);
 }
 
 // ---------------------------------------------------------------------------
@@ -327,7 +353,7 @@ struct Operand {
   __device__ __forceinline__ bool ragged() const { return !KC && rows < BR && rows % 8 != 0; }
   __device__ __forceinline__ const char* at(int32_t k) const { return base + (KC ? int64_t(k) * ES : k * ld); }
 
-  // Whole step from k on, asynchronously.  A thread's chunks lie kRowsEach rows apart at
+  // Whole step from k on, asynchronously (rows on 16 bytes).  A thread's chunks lie kRowsEach rows apart at
   // one place of their rows (the swizzles repeat after 16 rows).  Rows past the matrix:
   // the tile's first one again.
   static constexpr int kRowsEach = KC ? THREADS / 8 : THREADS / (BR / 8);
@@ -345,28 +371,47 @@ struct Operand {
     }
   }
 
-  // step [k, end) through registers
+  // Steps through registers: 16 bytes at an address of any alignment, and one by one what
+  // is not whole: the columns (KS) that end inside a chunk, and with kLast, in the step
+  // that reaches `end`, what lies beyond it.
+  static __device__ __forceinline__ u4 some(const char* p, int64_t n) {
+    u4 v = {0, 0, 0, 0};
+    if constexpr (ES == 2) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) v[e / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[e]) << (16 * (e % 2));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (e < n) v[e / 4] |= static_cast<uint32_t>(reinterpret_cast<const uint8_t*>(p)[e]) << (8 * (e % 4));
+    }
+    return v;
+  }
+  static __device__ __forceinline__ u4 all(const char* p) {
+    return ES == 2 ? u4(*reinterpret_cast<const u4_at2*>(p)) : u4(*reinterpret_cast<const u4_at1*>(p));
+  }
+  template <bool kLast>
   __device__ __forceinline__ void load(int32_t k, int32_t end, u4 (&v)[kEach]) const {
+    const char* const b = at(k);
+    int r, c;
+    place(pos(0), &r, &c);
+    const int64_t cols = KC ? 8 : rows - c * 8;        // KS: columns of this thread's chunks
 #pragma unroll
     for (int n = 0; n < kEach; ++n) {
-      int r, c;
-      place(pos(n), &r, &c);
-      int64_t left = KC ? (r < rows ? end - (k + c * kPer) : 0) : (k + r < end ? rows - c * 8 : 0);
-      if (!mine(n)) left = 0;
-      const char* p = at(k) + (r * ld + c * 16);
-      if (left >= kPer) {
-        v[n] = ES == 2 ? u4(*reinterpret_cast<const u4_at2*>(p)) : u4(*reinterpret_cast<const u4_at1*>(p));
+      if (!mine(n)) continue;
+      const int row = r + n * kRowsEach;
+      const char* p = b + (KC && row >= rows ? 0 : row) * ld + (KC || c * 8 < rows ? c : 0) * 16;   // 64 bits: any stride
+      if constexpr (KC && kLast) {
+        const int left = end - (k + c * kPer);
+        v[n] = left >= kPer ? all(p) : some(p, left);
+      } else if constexpr (KC) {
+        v[n] = all(p);
       } else {
-        v[n] = u4{0, 0, 0, 0};
-        if constexpr (ES == 2) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (e < left) v[n][e / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[e]) << (16 * (e % 2));
-        } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (e < left) v[n][e / 4] |= static_cast<uint32_t>(reinterpret_cast<const uint8_t*>(p)[e]) << (8 * (e % 4));
-        }
+        const bool in = !kLast || k + row < end;
+        if (cols >= 8 || cols <= 0)                     // (past the columns: the tile's first chunk)
+          v[n] = in && rows >= 8 ? all(p) : u4{0, 0, 0, 0};
+        else
+          v[n] = some(p, in ? cols : 0);
       }
     }
   }
@@ -611,16 +656,22 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
   }
   if (t < steps) {
     u4 vp[OpP::kEach], vq[OpQ::kEach];
-    p.load(k0 + t * kStep, k1, vp);
-    q.load(k0 + t * kStep, k1, vq);
+    auto load = [&](int32_t s) __attribute__((always_inline)) {
+      const int32_t k = k0 + s * kStep;
+      if (k + kStep <= k1) {
+        p.template load<false>(k, k1, vp);
+        q.template load<false>(k, k1, vq);
+      } else {
+        p.template load<true>(k, k1, vp);
+        q.template load<true>(k, k1, vq);
+      }
+    };
+    load(t);
     for (int slot = 0; t < steps; ++t, slot ^= 1) {
       p.store(lds + slot * kStage, vp);
       q.store(lds + slot * kStage + OpP::kBytes, vq);
       __syncthreads();
-      if (t + 1 < steps) {
-        p.load(k0 + (t + 1) * kStep, k1, vp);
-        q.load(k0 + (t + 1) * kStep, k1, vq);
-      }
+      if (t + 1 < steps) load(t + 1);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         Half f;
@@ -631,18 +682,18 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
     }
   }
 
-  // The epilogue by rows: 16 rows of the wave's columns at a time go through its own
+  // The epilogue by rows: up to 64 rows of the wave's columns at a time go through its own
   // part of LDS, so that a lane has eight consecutive columns and the wave's reads and
   // writes of C are whole lines.  Quads of columns are swizzled by row: the 16 lanes that
   // write a quad of their rows, and the ones that read two rows, meet no bank twice.
-  // What a row needs from memory is asked for kAhead groups of rows before.
-  constexpr int kCols = TJ * 16, kLanes = kCols / 8, kRows = 64 / kLanes, kGroups = TI * 16 / kRows;
-  constexpr int kAhead = kGroups < 4 ? kGroups : 4;
-  static_assert(WI * WJ * 16 * kCols * 4 <= NS * kStage, "the rows fit the steps' place");
-  static_assert(TJ == 2 || TJ == 4, "8 or 16 quads per row");
+  // What a row needs from memory is asked for kAhead loads of the wave before.
+  constexpr int kCols = TJ * 16, kLanes = kCols / 8, kRows = 64 / kLanes;    // rows per access of the wave
+  constexpr int kBatch = TI < 4 ? TI : 4, kAhead = 3;
+  static_assert(WI * WJ * kBatch * 16 * kCols * 4 <= NS * kStage, "the rows fit the steps' place");
+  static_assert(TI % kBatch == 0 && TI / kBatch <= 2 && (TJ == 2 || TJ == 4), "see below");
   __syncthreads();                     // every wave is done with the steps
   typedef __attribute__((address_space(3))) f4 lds_f4;
-  lds_char* const mine = l3 + wave * (16 * kCols * 4);
+  lds_char* const mine = l3 + wave * (kBatch * 16 * kCols * 4);
   const int lane = threadIdx.x & 63;
   auto quad = [&](int row, int k) {
     const int sw = TJ == 4 ? row : row >> 1;
@@ -651,37 +702,68 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
   const int col = lane % kLanes;
   const int64_t j = j0 + wj * kCols + col * 8;
   const int n = static_cast<int>(min<int64_t>(8, a.J - j));
-  const int64_t first = i0 + wi * TI * 16 + lane / kLanes;      // group g: row first + g * kRows
-  auto inside = [&](int g) { return first + g * kRows < a.I ? n : 0; };
-  ColumnTerms ct;
-  RowTerms rt[kAhead];
-  if (a.splits == 1) {
-    ct = column_terms(a, j, n);
+  const int64_t first = i0 + wi * TI * 16 + lane / kLanes;
+  constexpr int kGroups = TI * 16 / kRows;                      // accesses of kRows rows
+  const int32_t ld_part = static_cast<int32_t>((a.J + 7) / 8 * 8);
+  // rows [b * kBatch * 16, ...) of the wave's into LDS
+  auto stage = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
-    for (int g = 0; g < kAhead; ++g) rt[g] = row_terms(a, first + g * kRows, j, inside(g));
-  }
+    for (int x = 0; x < kBatch; ++x)
 #pragma unroll
-  for (int g = 0; g < kGroups; ++g) {
-    constexpr int kPer = 16 / kRows;     // groups per 16 rows
-    const int x = g / kPer;
-    if (g % kPer == 0) {
-#pragma unroll
-      for (int y = 0; y < TJ; ++y) *quad(lane & 15, y * 4 + (lane >> 4)) = acc[x][y];
+      for (int y = 0; y < TJ; ++y) {
+        f4 v = acc[x][y];
+        if constexpr (TI > kBatch) v = b ? acc[kBatch + x][y] : v;
+        *quad(x * 16 + (lane & 15), y * 4 + (lane >> 4)) = v;
+      }
+    __builtin_amdgcn_wave_barrier();
+  };
+  // `take`(access, row of C, its eight sums) for every access
+  auto rows = [&](auto take) __attribute__((always_inline)) {
+#pragma unroll 1
+    for (int b = 0; b < TI / kBatch; ++b) {
+      stage(b);
+#pragma unroll 1
+      for (int r = 0; r < kBatch * 16; r += kRows) {
+        const int row = r + lane / kLanes, g = (b * kBatch * 16 + r) / kRows;
+        const f4 lo = *quad(row, 2 * col), hi = *quad(row, 2 * col + 1);
+        float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        take(g, first + g * kRows, v);
+      }
       __builtin_amdgcn_wave_barrier();
     }
-    const int row = g % kPer * kRows + lane / kLanes;
-    const f4 lo = *quad(row, 2 * col), hi = *quad(row, 2 * col + 1);
-    if (g % kPer == kPer - 1) __builtin_amdgcn_wave_barrier();
-    float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  };
+  auto terms = [&](int g) __attribute__((always_inline)) {
     const int64_t i = first + g * kRows;
-    const int m = inside(g);
-    if (a.splits > 1) {
-      if (m > 0) store8(a.partial + (split * a.I + i) * ((a.J + 7) / 8 * 8) + j, 8, v);
-    } else {
-      const RowTerms now = rt[g % kAhead];
-      if (g + kAhead < kGroups) rt[g % kAhead] = row_terms(a, i + kAhead * kRows, j, inside(g + kAhead));
-      if (m > 0) finish8(a, i, j, m, v, ct, now);
-    }
+    return row_terms(a, i, j, g < kGroups && i < a.I ? n : 0);
+  };
+  if (a.splits > 1) {
+    rows([&](int, int64_t i, float (&v)[8]) __attribute__((always_inline)) {
+      if (i < a.I && n > 0) store8(a.partial + (split * a.I + i) * ld_part + j, 8, v);
+    });
+    return;
+  }
+  ColumnTerms ct = column_terms(a, j, n);
+  // (here, and not at their first use: in the loop below that would be a wait for the
+  // stores of the rows before, since loads and stores are counted together)
+#pragma unroll
+  for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(ct.scale[e]), "+v"(ct.bias[e]));
+  if (a.residual || a.p_scale) {
+    RowTerms ahead[kAhead];
+#pragma unroll
+    for (int g = 0; g < kAhead; ++g) ahead[g] = terms(g);
+    rows([&](int g, int64_t i, float (&v)[8]) __attribute__((always_inline)) {
+      const RowTerms now = ahead[0];
+#pragma unroll
+      for (int k = 0; k + 1 < kAhead; ++k) ahead[k] = ahead[k + 1];
+      ahead[kAhead - 1] = terms(g + kAhead);
+      if (i < a.I && n > 0) finish8(a, i, j, n, v, ct, now);
+    });
+  } else {
+    RowTerms none;
+    none.scale = a.alpha;
+    rows([&](int, int64_t i, float (&v)[8]) __attribute__((always_inline)) {
+      if (i < a.I && n > 0) finish8(a, i, j, n, v, ct, none);
+    });
   }
 }
 

@@ -12,12 +12,19 @@ __global__ void __launch_bounds__(256) k_join(const ProductArgs a) {
   if (at >= groups * a.I) return;
   const int64_t i = at / groups, j = at % groups * 8;
   const float* p = a.partial + i * ld + j;
-  float v[8], w[8];
-  load8(p, 8, v);
-  for (int s = 1; s < a.splits; ++s) {
-    load8(p + s * a.I * ld, 8, w);
+  float v[8] = {};
+  constexpr int kDeep = 8;             // parts on their way
+  for (int s0 = 0; s0 < a.splits; s0 += kDeep) {
+    float w[kDeep][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += w[e];
+    for (int s = 0; s < kDeep; ++s)
+      if (s0 + s < a.splits) load8(p + (s0 + s) * a.I * ld, 8, w[s]);
+#pragma unroll
+    for (int s = 0; s < kDeep; ++s)
+      if (s0 + s < a.splits) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += w[s][e];
+      }
   }
   const int n = static_cast<int>(min<int64_t>(8, a.J - j));
   finish8(a, i, j, n, v, column_terms(a, j, n), row_terms(a, i, j, n));
@@ -63,10 +70,6 @@ int64_t act_grad_groups(int64_t M, int64_t N) {
   return g < rows ? g : rows;
 }
 
-struct ShapeInfo {
-  int bi, bj, wgs;           // workgroups a CU holds
-};
-constexpr ShapeInfo kInfo[kShapes] = {{256, 256, 1}, {128, 128, 2}, {64, 128, 3}, {32, 128, 2}, {16, 128, 2}};
 constexpr int kCus = 256;
 
 }  // namespace
@@ -76,6 +79,7 @@ ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc) {
   const int64_t steps = (K + step - 1) / step;
   auto tiles = [&](int s) { return ((I + kInfo[s].bi - 1) / kInfo[s].bi) * ((J + kInfo[s].bj - 1) / kInfo[s].bj); };
   int shape = kShape256;
+  if (p_kc && I <= kFewRows) return {kFew, 1, K, 0};
   if (p_kc && I <= 16)
     shape = kShape16;
   else if (p_kc && I <= 32)
@@ -100,9 +104,10 @@ ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc) {
 
 hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream) {
   const ProductPlan p = plan_product(a.I, a.J, a.K, a.elem, a.p_kc);
+  a.splits = p.splits;
+  if (p.shape == kFew) return launch_product_few(a, stream);
   const ShapeInfo& s = kInfo[p.shape];
   const int64_t es = dtype_bytes(a.elem);
-  a.splits = p.splits;
   a.k_split = p.k_split;
   a.partial = partial;
   a.tiles_i = static_cast<uint32_t>((a.I + s.bi - 1) / s.bi);

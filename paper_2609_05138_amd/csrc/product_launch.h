@@ -5,8 +5,9 @@
 
 namespace som {
 
-template <int E, bool PKC, bool QKC, int WI, int WJ, int TI, int TJ, int NS>
+template <int SHAPE, int E, bool PKC, bool QKC, int WI, int WJ, int TI, int TJ, int NS>
 hipError_t launch_one(const ProductArgs& a, hipStream_t stream) {
+  static_assert(kInfo[SHAPE].bi == WI * TI * 16 && kInfo[SHAPE].bj == WJ * TJ * 16, "the grid is laid out for these tiles");
   constexpr size_t lds = static_cast<size_t>(NS) * (WI * TI + WJ * TJ) * 16 * kStepBytes;
   if constexpr (lds > 64 * 1024) {
     const hipError_t e = allow_lds(k_product<E, PKC, QKC, WI, WJ, TI, TJ, NS>, lds);
@@ -21,16 +22,16 @@ template <int E, bool PKC, bool QKC>
 hipError_t launch_shape(int shape, const ProductArgs& a, hipStream_t stream) {
   switch (shape) {
     case kShape256:
-      return launch_one<E, PKC, QKC, 2, 4, 8, 4, 2>(a, stream);
+      return launch_one<kShape256, E, PKC, QKC, 2, 4, 8, 4, 2>(a, stream);
     case kShape128:
-      return launch_one<E, PKC, QKC, 2, 2, 4, 4, 2>(a, stream);
+      return launch_one<kShape128, E, PKC, QKC, 2, 2, 4, 4, 2>(a, stream);
     case kShape64:
-      return launch_one<E, PKC, QKC, 1, 4, 4, 2, 2>(a, stream);
+      return launch_one<kShape64, E, PKC, QKC, 1, 4, 4, 2, 2>(a, stream);
     default:
       // few rows: their operand has k contiguous in every product that has few
       if constexpr (PKC)
-        return shape == kShape32 ? launch_one<E, PKC, QKC, 1, 4, 2, 2, 4>(a, stream)
-                                 : launch_one<E, PKC, QKC, 1, 4, 1, 2, 4>(a, stream);
+        return shape == kShape32 ? launch_one<kShape32, E, PKC, QKC, 1, 4, 2, 2, 4>(a, stream)
+                                 : launch_one<kShape16, E, PKC, QKC, 1, 4, 1, 2, 4>(a, stream);
       else
         return hipErrorInvalidValue;
   }

@@ -376,7 +376,13 @@ k_column_sums(const float* __restrict__ part, int64_t groups, int64_t ld, int64_
   const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
   float s = 0.0f;
   if (c < cols)
-    for (int64_t g = wave; g < groups; g += 16) s += part[g * ld + c];
+    for (int64_t g0 = wave; g0 < groups; g0 += 16 * 8) {
+      float v[8];                       // eight on their way
+#pragma unroll
+      for (int d = 0; d < 8; ++d) v[d] = g0 + 16 * d < groups ? part[(g0 + 16 * d) * ld + c] : 0.0f;
+#pragma unroll
+      for (int d = 0; d < 8; ++d) s += v[d];
+    }
   sums[wave][lane] = s;
   __syncthreads();
   if (wave == 0 && c < cols) {

@@ -671,27 +671,41 @@ def _rows(t: torch.Tensor, name: str, dtype=None, shape=None):
         raise ValueError(f"{name} must be on a ROCm device (got {t.device})")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
-    if t.dim() != 2:
+    size = t.shape
+    if len(size) != 2:
         raise ValueError(f"{name} must have two dimensions")
-    rows, cols = t.shape
-    if shape is not None and (rows, cols) != shape:
-        raise ValueError(f"{name} must be {shape[0]} x {shape[1]} (got {rows} x {cols})")
+    if shape is not None and size != shape:
+        raise ValueError(f"{name} must be {shape[0]} x {shape[1]} (got {size[0]} x {size[1]})")
+    rows, cols = size
     ld, one = t.stride()
-    if cols > 1 and one != 1:
+    if one != 1 and cols > 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
-    if rows <= 1:
-        ld = max(ld, cols)
-    elif ld < cols:
-        raise ValueError(f"{name}: rows must not overlap")
+    if ld < cols:
+        if rows > 1:
+            raise ValueError(f"{name}: rows must not overlap")
+        ld = cols
     return t.data_ptr(), ld
+
+
+def _stream_of(t: torch.Tensor, stream) -> int:
+    """The given stream, or the current one of the tensor's device (asked for by
+    itself: torch.cuda.current_stream() takes longer than a launch)."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(t.get_device())
+    return stream.cuda_stream
 
 
 def _vector(t: Optional[torch.Tensor], name: str, n: int, dtype=torch.float32):
     if t is None:
         return None
-    _dev(t, dtype, name)
-    if t.numel() != n:
-        raise ValueError(f"{name} must have {n} entries")
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a ROCm device (got {t.device})")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must have {n} contiguous entries")
     return t.data_ptr()
 
 
@@ -722,12 +736,14 @@ def _weights(W: torch.Tensor, name: str, dtype):
 
 
 def _scratch(ws, need: int, device):
+    """(tensor, pointer, bytes) of the workspace: the caller's, or one for this call."""
     if ws is None:
         if need == 0:
-            return None, 0
-        ws = _workspace(need, device)
-    _dev(ws, torch.uint8, "ws")
-    return ws, ws.numel()
+            return None, None, 0
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+    else:
+        _dev(ws, torch.uint8, "ws")
+    return ws, ws.data_ptr(), ws.numel()
 
 
 def som_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -744,7 +760,7 @@ def som_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: fl
     dt = _float_type(x, "x", _FLOATS)
     xp, ldx = _rows(x, "x")
     rows, cols = x.shape
-    shape = (rows, cols)
+    shape = x.shape
     rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", x.dtype, shape)
     wp = _vector(weight, "weight", cols, x.dtype)
     yt = torch.float8_e4m3fn if q8 else x.dtype
@@ -760,7 +776,7 @@ def som_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: fl
         raise ValueError("scale goes with q8")
     sp = _vector(scale, "scale", rows)
     _check(lib.som_rms_norm(xp, ldx, rp, ldr, wp, dt, rows, cols, eps, 1 if q8 else 0, yp, ldy, hp, ldh, sp,
-                            _stream(stream)))
+                            _stream_of(x, stream)))
     return y, h, scale
 
 
@@ -784,9 +800,9 @@ def som_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[to
     if dweight is None:
         dweight = torch.empty(cols, dtype=torch.float32, device=h.device)
     dwp = _vector(dweight, "dweight", cols)
-    ws, n = _scratch(ws, lib.som_rms_norm_backward_workspace_bytes(rows, cols), h.device)
-    _check(lib.som_rms_norm_backward(gp, ldg, hp, ldh, wp, ep, lde, dt, rows, cols, eps, xp, ldx, dwp, _ptr(ws), n,
-                                     _stream(stream)))
+    ws, wsp, n = _scratch(ws, lib.som_rms_norm_backward_workspace_bytes(rows, cols), h.device)
+    _check(lib.som_rms_norm_backward(gp, ldg, hp, ldh, wp, ep, lde, dt, rows, cols, eps, xp, ldx, dwp, wsp, n,
+                                     _stream_of(h, stream)))
     return dx, dweight
 
 
@@ -829,9 +845,9 @@ def som_product(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
     pp, ldp = (None, 0) if pre is None else _rows(pre, "pre", y.dtype, shape)
     e = som_epilogue(ACTIVATIONS[act], 0, alpha, _vector(x_scale, "x_scale", M), _vector(w_scale, "w_scale", N),
                      _vector(bias, "bias", N), rp, ldr, pp, ldp)
-    ws, n = _scratch(ws, lib.som_product_workspace_bytes(M, N, K, xt), x.device)
-    _check(lib.som_product(xp, ldx, Wp, ldw, units, xt, M, N, K, yp, ldy, yt, ctypes.byref(e), _ptr(ws), n,
-                           _stream(stream)))
+    ws, wsp, n = _scratch(ws, lib.som_product_workspace_bytes(M, N, K, xt), x.device)
+    _check(lib.som_product(xp, ldx, Wp, ldw, units, xt, M, N, K, yp, ldy, yt, ctypes.byref(e), wsp, n,
+                           _stream_of(x, stream)))
     return y
 
 
@@ -870,9 +886,9 @@ def som_product_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, act
     if dbias is None:
         dbias = torch.empty(N, dtype=torch.float32, device=x.device)
     dbp = _vector(dbias, "dbias", N)
-    ws, n = _scratch(ws, lib.som_product_backward_workspace_bytes(M, N, K, dt), x.device)
+    ws, wsp, n = _scratch(ws, lib.som_product_backward_workspace_bytes(M, N, K, dt), x.device)
     _check(lib.som_product_backward(gp, ldg, xp, ldx, Wp, ldw, units, dt, M, N, K, ACTIVATIONS[act], pp, ldp, alpha,
-                                    dxp, lddx, dWp, lddw, dbp, _ptr(ws), n, _stream(stream)))
+                                    dxp, lddx, dWp, lddw, dbp, wsp, n, _stream_of(x, stream)))
     return dx, dW, dbias
 
 
@@ -892,5 +908,5 @@ def som_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual:
     if y is None:
         y = torch.empty(shape, dtype=x.dtype, device=x.device)
     yp, ldy = _rows(y, "y", x.dtype, shape)
-    _check(lib.som_dropout(xp, ldx, rp, ldr, dt, rows, cols, p, seed, offset, yp, ldy, _stream(stream)))
+    _check(lib.som_dropout(xp, ldx, rp, ldr, dt, rows, cols, p, seed, offset, yp, ldy, _stream_of(x, stream)))
     return y
