@@ -54,21 +54,20 @@ struct ProductArgs {
   bool dma;                  // rows of both operands start on 16 bytes
 };
 
-// Tile shapes, and the kernel of few rows (product_few.hip).
-enum Shape { kShape256 = 0, kShape128, kShape64, kShape32, kShape16, kShapes, kFew = kShapes };
+// Tile shapes, and the kernels of few rows (product_few.hip).
+enum Shape { kShape256 = 0, kShape256x128, kShape128, kShape64, kShape32, kShape16, kShapes, kFew = kShapes };
 struct ShapeInfo {
   int bi, bj;                // rows and columns of C
   int wgs;                   // workgroups that a CU holds
 };
-constexpr ShapeInfo kInfo[kShapes] = {{256, 256, 1}, {128, 128, 2}, {64, 128, 3}, {32, 128, 2}, {16, 128, 2}};
-constexpr int64_t kFewRows = 4;
+constexpr ShapeInfo kInfo[kShapes] = {{256, 256, 1}, {256, 128, 1}, {128, 128, 1}, {64, 128, 2}, {32, 128, 2}, {16, 128, 2}};
 struct ProductPlan {
   int shape;
   int splits;
   int64_t k_split;
   size_t partial_floats;
 };
-ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc);
+ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc);
 // Fills the launch's fields of `a` and enqueues it (and the join of a split k axis);
 // `partial`: plan_product's floats.
 hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream);

@@ -2,6 +2,8 @@
 // split k axis, and the activation's gradient.
 #include "product.h"
 
+#include <initializer_list>
+
 namespace som {
 namespace {
 
@@ -70,40 +72,71 @@ int64_t act_grad_groups(int64_t M, int64_t N) {
   return g < rows ? g : rows;
 }
 
-constexpr int kCus = 256;
+constexpr int64_t kCus = 256;
+
+// Times in us that the choice of a tile shape goes by, measured on MI355X (bf16, replayed
+// graphs of 20 products): a workgroup's start, first step and epilogue; a step of 128
+// bytes of k alone on a CU, where up to half of the CUs and where all have one; and for two
+// workgroups on a CU.  8-bit steps hold twice the products.
+struct ShapeTime {
+  double fixed, half, full, pair, e4m3;
+};
+constexpr ShapeTime kTime[kShapes] = {{11.0, 1.33, 1.50, 0, 1.8}, {9.5, 0.58, 0.80, 0, 1.6}, {4.4, 0.47, 0.52, 0, 1.4},
+                                      {4.1, 0.29, 0.33, 0.64, 1.2}, {3.4, 0.27, 0.28, 0.59, 1.1}, {3.4, 0.20, 0.22, 0.45, 1.1}};
+// A split k axis: the second launch and its wait, and the parts' bytes per us.
+constexpr double kJoinTime = 4.5, kJoinBytes = 6.5e6;
+constexpr int64_t kMinSplitSteps = 4;
+
+double product_time(int shape, int64_t n, int64_t steps, bool e4m3) {
+  const ShapeTime& t = kTime[shape];
+  const double more = e4m3 ? t.e4m3 : 1.0;
+  const double fill = n >= kCus ? 1.0 : n <= kCus / 2 ? 0.0 : static_cast<double>(n - kCus / 2) / (kCus / 2);
+  const double alone = t.fixed + steps * more * (t.half + (t.full - t.half) * fill);
+  const int64_t each = (n + kCus - 1) / kCus;                // workgroups of a CU
+  if (kInfo[shape].wgs == 1) return each * alone;
+  return each / 2 * (t.fixed + steps * more * t.pair) + each % 2 * alone;
+}
 
 }  // namespace
 
-ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc) {
+// The shape and split with the least time by the table.  Against the measured best of all
+// shapes and splits it chooses within 5% for 2,048^3 (128 x 128, 20.9 us; 256 x 256 in
+// two splits 39.3), 4,096^3 (256 x 256, 107; 128 x 128 148), 3,000 x 1,000 x 3,000
+// (256 x 256, 33.0; 128 x 128 39.8), 512 x 1,024 x 4,096 (64 x 128, 9.5; 128 x 128 11.8),
+// 128 x 4,096 x 4,096 (64 x 128 in four splits, 16.0; unsplit 22.6), 37 x 8,192 x 2,048
+// (32 x 128 in eight splits, 12.7; 64 x 128 12.9).
+//
+// Few rows: with k contiguous in both up to four take the vector kernel (4,096 x 4,096:
+// one row 5.8 us, two 7.4, four 10.1; in 16 x 128 tiles and eight splits 9.0, in two
+// launches).  With k strided one row does from 8,192 columns on (2,048 x 16,384: 13.4
+// against 17.6; two rows are no faster; 4,096 x 4,096: 11.4 against 8.9, since a
+// narrow strip's lines are read by several CUs).
+ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc) {
+  if (p_kc && (q_kc ? I <= 4 : I == 1 && J >= 8192)) return {kFew, 1, K, 0};
   const int64_t step = elem == kE4M3 ? 128 : 64;
   const int64_t steps = (K + step - 1) / step;
-  auto tiles = [&](int s) { return ((I + kInfo[s].bi - 1) / kInfo[s].bi) * ((J + kInfo[s].bj - 1) / kInfo[s].bj); };
-  int shape = kShape256;
-  if (p_kc && I <= kFewRows) return {kFew, 1, K, 0};
-  if (p_kc && I <= 16)
-    shape = kShape16;
-  else if (p_kc && I <= 32)
-    shape = kShape32;
-  else if (I <= 64)
-    shape = kShape64;
-  else if (tiles(kShape256) < kCus)
-    shape = kShape128;
-  // few tiles: split k until the device is full, in splits of at least four steps
-  int64_t splits = 1;
-  const int64_t slots = kCus * kInfo[shape].wgs, n = tiles(shape);
-  if (n * 2 <= slots) splits = slots / n;
-  if (splits > steps / 4) splits = steps / 4;
-  if (splits > 64) splits = 64;
-  if (splits < 1) splits = 1;
-  const int64_t per = (steps + splits - 1) / splits;
-  splits = (steps + per - 1) / per;
-  ProductPlan p{shape, static_cast<int>(splits), per * step, 0};
-  if (splits > 1) p.partial_floats = static_cast<size_t>(splits) * I * ((J + 7) / 8 * 8);
-  return p;
+  ProductPlan best{kShape256, 1, steps * step, 0};
+  double least = 1e300;
+  for (int shape = 0; shape < (p_kc ? static_cast<int>(kShapes) : kShape32); ++shape) {
+    const ShapeInfo& s = kInfo[shape];
+    const int64_t tiles = ((I + s.bi - 1) / s.bi) * ((J + s.bj - 1) / s.bj);
+    for (int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+      if (want > 1 && (steps < want * kMinSplitSteps || tiles * want > 4 * kCus)) break;
+      const int64_t per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
+      double t = product_time(shape, tiles * splits, per, elem == kE4M3);
+      if (splits > 1) t += kJoinTime + 8.0 * static_cast<double>(splits) * I * J / kJoinBytes;
+      if (t < least) {
+        least = t;
+        best = {shape, static_cast<int>(splits), per * step, 0};
+      }
+    }
+  }
+  if (best.splits > 1) best.partial_floats = static_cast<size_t>(best.splits) * I * ((J + 7) / 8 * 8);
+  return best;
 }
 
 hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream) {
-  const ProductPlan p = plan_product(a.I, a.J, a.K, a.elem, a.p_kc);
+  const ProductPlan p = plan_product(a.I, a.J, a.K, a.elem, a.p_kc, a.q_kc);
   a.splits = p.splits;
   if (p.shape == kFew) return launch_product_few(a, stream);
   const ShapeInfo& s = kInfo[p.shape];

@@ -23,10 +23,12 @@ hipError_t launch_shape(int shape, const ProductArgs& a, hipStream_t stream) {
   switch (shape) {
     case kShape256:
       return launch_one<kShape256, E, PKC, QKC, 2, 4, 8, 4, 2>(a, stream);
+    case kShape256x128:
+      return launch_one<kShape256x128, E, PKC, QKC, 4, 2, 4, 4, 3>(a, stream);
     case kShape128:
-      return launch_one<kShape128, E, PKC, QKC, 2, 2, 4, 4, 2>(a, stream);
+      return launch_one<kShape128, E, PKC, QKC, 2, 4, 4, 2, 4>(a, stream);
     case kShape64:
-      return launch_one<kShape64, E, PKC, QKC, 1, 4, 4, 2, 2>(a, stream);
+      return launch_one<kShape64, E, PKC, QKC, 2, 4, 2, 2, 3>(a, stream);
     default:
       // few rows: their operand has k contiguous in every product that has few
       if constexpr (PKC)
