@@ -281,6 +281,9 @@ __device__ __forceinline__ void arrive() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// The same for LDS alone: loads into registers stay on their way.
+__device__ __forceinline__ void arrive_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // 16 bytes per lane from base + off to LDS at `lds` (uniform) + 16 * lane.  A vector
 // instruction may have written the base's scalar registers just before (a lane read
 // into them): a memory instruction may read those five wait states later at the
@@ -370,9 +373,10 @@ struct Operand {
     }
   }
 
-  // Steps through registers: 16 bytes at an address of any alignment, and one by one what
-  // is not whole: the columns (KS) that end inside a chunk, and with kLast, in the step
-  // that reaches `end`, what lies beyond it.
+  // Steps through registers: 16 bytes at an address of any alignment.  Of a chunk that
+  // the row's end cuts (KS: the matrix's last columns; KC, with kLast: `end`), the 16
+  // bytes up to that end, which `store` or `load` shifts into place; the places after it
+  // are zero.  A row shorter than a chunk goes element by element.
   static __device__ __forceinline__ u4 some(const char* p, int64_t n) {
     u4 v = {0, 0, 0, 0};
     if constexpr (ES == 2) {
@@ -389,35 +393,68 @@ struct Operand {
   static __device__ __forceinline__ u4 all(const char* p) {
     return ES == 2 ? u4(*reinterpret_cast<const u4_at2*>(p)) : u4(*reinterpret_cast<const u4_at1*>(p));
   }
+  // the last n (of kPer, 0 < n < kPer) elements moved to the front
+  static __device__ __forceinline__ u4 front(u4 v, int n) {
+    uint64_t lo = static_cast<uint64_t>(v[1]) << 32 | v[0], hi = static_cast<uint64_t>(v[3]) << 32 | v[2];
+    const int bits = (kPer - n) * ES * 8;
+    lo = bits >= 64 ? hi >> (bits - 64) : lo >> bits | hi << (64 - bits);
+    hi = bits >= 64 ? 0 : hi >> bits;
+    return u4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi),
+              static_cast<uint32_t>(hi >> 32)};
+  }
+  // KS: columns in this thread's chunks, where the matrix's end cuts them, else 0
+  __device__ __forceinline__ int cut() const {
+    int r, c;
+    place(pos(0), &r, &c);
+    return !KC && c * 8 < rows && rows - c * 8 < 8 ? static_cast<int>(rows - c * 8) : 0;
+  }
+  // `extent`: columns (KS) or k (KC) of the matrix
   template <bool kLast>
-  __device__ __forceinline__ void load(int32_t k, int32_t end, u4 (&v)[kEach]) const {
+  __device__ __forceinline__ void load(int32_t k, int32_t end, int64_t extent, u4 (&v)[kEach]) const {
     const char* const b = at(k);
     int r, c;
     place(pos(0), &r, &c);
-    const int64_t cols = KC ? 8 : rows - c * 8;        // KS: columns of this thread's chunks
+    const int cols = cut();
+    // KS: past the columns the tile's first chunk (its sums are not kept), where that is whole
+    const bool none = !KC && cols == 0 && rows < 8;
+    const int64_t at_col = KC ? c * 16 : c * 8 >= rows ? 0 : cols && extent >= 8 ? c * 16 - (8 - cols) * 2 : c * 16;
 #pragma unroll
     for (int n = 0; n < kEach; ++n) {
       if (!mine(n)) continue;
       const int row = r + n * kRowsEach;
-      const char* p = b + (KC && row >= rows ? 0 : row) * ld + (KC || c * 8 < rows ? c : 0) * 16;   // 64 bits: any stride
+      const char* p = b + (KC && row >= rows ? 0 : row) * ld + at_col;     // 64 bits: any stride
       if constexpr (KC && kLast) {
         const int left = end - (k + c * kPer);
-        v[n] = left >= kPer ? all(p) : some(p, left);
+        if (left >= kPer)
+          v[n] = all(p);
+        else if (left <= 0)
+          v[n] = u4{0, 0, 0, 0};
+        else
+          v[n] = extent >= kPer ? front(all(p - (kPer - left) * ES), left) : some(p, left);
       } else if constexpr (KC) {
         v[n] = all(p);
       } else {
         const bool in = !kLast || k + row < end;
-        if (cols >= 8 || cols <= 0)                     // (past the columns: the tile's first chunk)
-          v[n] = in && rows >= 8 ? all(p) : u4{0, 0, 0, 0};
+        if (!in || none)
+          v[n] = u4{0, 0, 0, 0};
+        else if (extent >= 8)
+          v[n] = all(p);
         else
-          v[n] = some(p, in ? cols : 0);
+          v[n] = some(p, cols);
       }
     }
   }
-  __device__ __forceinline__ void store(char* lds, const u4 (&v)[kEach]) const {
+  __device__ __forceinline__ void store(char* lds, int64_t extent, const u4 (&v)[kEach]) const {
+    const int cols = cut();
+    if (!KC && cols && extent >= 8) {
 #pragma unroll
-    for (int n = 0; n < kEach; ++n)
-      if (mine(n)) *reinterpret_cast<u4*>(lds + pos(n) * 16) = v[n];
+      for (int n = 0; n < kEach; ++n)
+        if (mine(n)) *reinterpret_cast<u4*>(lds + pos(n) * 16) = front(v[n], cols);
+    } else {
+#pragma unroll
+      for (int n = 0; n < kEach; ++n)
+        if (mine(n)) *reinterpret_cast<u4*>(lds + pos(n) * 16) = v[n];
+    }
   }
 
   // A lane's share of rows [16 t, 16 t + 16) of this wave's: `lane_base` is for
@@ -566,21 +603,36 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
   struct Half {
     i4 q[TJ], p[TI];
   };
-  auto read_one = [&](Half& f, int slot, int h, int r) {
+  auto read_one = [&](Half& f, int slot, int h, int r) __attribute__((always_inline)) {
     lds_char* sp = l3 + slot * kStage;
     if (r < TJ)
       f.q[r] = fragment<QKC, BJ>(sp + OpP::kBytes, qb, r, h);
     else
       f.p[r - TJ] = fragment<PKC, BI>(sp, pb, r - TJ, h);
   };
-  auto read = [&](Half& f, int slot, int h) {
+  auto read = [&](Half& f, int slot, int h) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < TJ + TI; ++r) read_one(f, slot, h, r);
   };
-  auto multiply_row = [&](const Half& f, int x) {
+  auto multiply_row = [&](const Half& f, int x) __attribute__((always_inline)) {
     const Frag<E> fp(f.p[x]);
 #pragma unroll
     for (int y = 0; y < TJ; ++y) acc[x][y] = mfma<E>(Frag<E>(f.q[y]), fp, acc[x][y]);
+  };
+
+  Half f[2];
+  // products of `now`, row of tiles by row; between them half h of the step in `from` is
+  // read into `next`, and `more` of each row is done
+  auto phase = [&](const Half& now, Half& next, int from, int h, auto more) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < TI; ++x) {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int r = x * (TI + TJ) / TI; r < (x + 1) * (TI + TJ) / TI; ++r) read_one(next, from, h, r);
+      more(x);
+      multiply_row(now, x);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   };
 
   const int32_t steps = (k1 - k0 + kStep - 1) / kStep;
@@ -597,7 +649,7 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
     constexpr int kMost = OpP::kEach + OpQ::kEach;
     static_assert(OpQ::whole, "every wave moves the same share of Q");
     const bool most = OpP::whole || (OpP::kEach - 1) * THREADS + wave * 64 < OpP::kChunks;
-    auto fetch_one = [&](int n, int32_t s, int slot) {
+    auto fetch_one = [&](int n, int32_t s, int slot) __attribute__((always_inline)) {
       const uint32_t at = l0 + static_cast<uint32_t>(slot) * kStage;
       if (n < OpP::kEach)
         p.fetch(n, k0 + s * kStep, at);
@@ -605,7 +657,7 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
         q.fetch(n - OpP::kEach, k0 + s * kStep, at + OpP::kBytes);
     };
     // step s has arrived, with the steps after it up to the newest on their way
-    auto arrived = [&](int32_t s, int after) {
+    auto arrived = [&](int32_t s, int after) __attribute__((always_inline)) {
       if (after == 0 || s + after >= full)
         arrive<0>();
       else if (after == 1)
@@ -616,30 +668,18 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
         most ? arrive<3 * kMost>() : arrive<3 * (kMost - 1)>();
     };
     static_assert(NS >= 2 && NS <= 4, "the waits are written for two to four steps");
-    Half f[2];
     int slot = 0;
-    // products of `now`; half h of the step in `from` into `next`; with kFetch step s into `to`
-    auto phase = [&](const Half& now, Half& next, int from, int h, auto fetches, int32_t s, int to) {
-      constexpr bool kFetch = decltype(fetches)::value;
-#pragma unroll
-      for (int x = 0; x < TI; ++x) {
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int r = x * (TI + TJ) / TI; r < (x + 1) * (TI + TJ) / TI; ++r) read_one(next, from, h, r);
-        if constexpr (kFetch) {
-#pragma unroll
-          for (int n = x * kMost / TI; n < (x + 1) * kMost / TI; ++n) fetch_one(n, s, to);
-        }
-        multiply_row(now, x);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    auto step = [&](auto fetches) {
-      phase(f[0], f[1], slot, 1, No{}, 0, 0);
+    auto step = [&](auto fetches) __attribute__((always_inline)) {
+      phase(f[0], f[1], slot, 1, [](int) {});
       arrived(t + 1, NS - 2);
       const int place = slot;
       slot = slot + 1 == NS ? 0 : slot + 1;
-      phase(f[1], f[0], slot, 0, fetches, t + NS, place);    // (after the last step: bytes that no product uses)
+      // (after the last step: bytes that no product uses)
+      phase(f[1], f[0], slot, 0, [&](int x) __attribute__((always_inline)) {
+        if constexpr (decltype(fetches)::value)
+#pragma unroll
+          for (int n = x * kMost / TI; n < (x + 1) * kMost / TI; ++n) fetch_one(n, t + NS, place);
+      });
     };
     if (full > 0) {
 #pragma unroll
@@ -654,29 +694,32 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
     }
   }
   if (t < steps) {
+    // Through registers, one step on its way, two in LDS.  (Two or three on their way, or
+    // the order of reads and products above, gained nothing: 31 us against 37 to 38 for
+    // 1,536 x 2,048 x 1,792 in bf16 with rows off 16 bytes.)
     u4 vp[OpP::kEach], vq[OpQ::kEach];
+    const int64_t p_extent = PKC ? a.K : a.I, q_extent = QKC ? a.K : a.J;
     auto load = [&](int32_t s) __attribute__((always_inline)) {
       const int32_t k = k0 + s * kStep;
       if (k + kStep <= k1) {
-        p.template load<false>(k, k1, vp);
-        q.template load<false>(k, k1, vq);
+        p.template load<false>(k, k1, p_extent, vp);
+        q.template load<false>(k, k1, q_extent, vq);
       } else {
-        p.template load<true>(k, k1, vp);
-        q.template load<true>(k, k1, vq);
+        p.template load<true>(k, k1, p_extent, vp);
+        q.template load<true>(k, k1, q_extent, vq);
       }
     };
     load(t);
     for (int slot = 0; t < steps; ++t, slot ^= 1) {
-      p.store(lds + slot * kStage, vp);
-      q.store(lds + slot * kStage + OpP::kBytes, vq);
-      __syncthreads();
+      p.store(lds + slot * kStage, p_extent, vp);
+      q.store(lds + slot * kStage + OpP::kBytes, q_extent, vq);
+      arrive_lds();
       if (t + 1 < steps) load(t + 1);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        Half f;
-        read(f, slot, h);
+        read(f[0], slot, h);
 #pragma unroll
-        for (int x = 0; x < TI; ++x) multiply_row(f, x);
+        for (int x = 0; x < TI; ++x) multiply_row(f[0], x);
       }
     }
   }

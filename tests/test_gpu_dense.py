@@ -186,7 +186,8 @@ def _weight_layout(W, units, dtype, pad, lead=0):
 # M, N, K: each tile shape, its edges, split k axes, partial steps and chunks
 SIZES = [(1, 1, 1), (1, 8, 64), (1, 130, 300), (3, 257, 65), (16, 128, 128), (17, 100, 1000), (32, 129, 640), (33, 64, 63),
          (64, 300, 2048), (65, 128, 200), (128, 256, 128), (129, 255, 131), (200, 1000, 72), (257, 511, 96),
-         (1, 4096, 4096), (300, 40, 4096), (40, 3001, 520)]
+         (1, 4096, 4096), (300, 40, 4096), (40, 3001, 520), (5, 3, 5), (70, 7, 9), (130, 4, 300), (20, 700, 7), (300, 1001, 203),
+         (1, 20000, 77), (600, 601, 600), (1100, 700, 130)]
 
 
 @pytest.mark.parametrize("units", [False, True])
@@ -277,7 +278,7 @@ def test_scores_of_dense_documents_are_the_units_distances():
 
 
 BACK_SIZES = [(1, 1, 1), (1, 64, 128), (2, 130, 70), (33, 77, 129), (64, 128, 64), (100, 300, 260), (257, 129, 65),
-              (1000, 40, 90), (520, 512, 256)]
+              (1000, 40, 90), (520, 512, 256), (9, 3, 5), (70, 300, 7), (1030, 601, 803)]
 
 
 @pytest.mark.parametrize("units", [False, True])
