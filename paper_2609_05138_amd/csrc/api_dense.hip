@@ -159,9 +159,12 @@ som_status som_rms_norm_backward(const void* dy, int64_t lddy, const void* h, in
 size_t som_product_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t x_dtype) {
   if (M < 1 || M > kI32Max || N < 1 || N > kMaxK || K < 1 || K > kMaxK || x_dtype < SOM_F16 || x_dtype > SOM_E4M3)
     return 0;
-  const size_t strided = som::plan_product(M, N, K, x_dtype, true, false).partial_floats;
-  const size_t contiguous = som::plan_product(M, N, K, x_dtype, true, true).partial_floats;
-  return som::align_up(sizeof(float) * (strided > contiguous ? strided : contiguous), 256);
+  size_t most = 0;
+  for (int i = 0; i < 4; ++i) {        // either layout of W, rows on 16 bytes or not
+    const size_t n = som::plan_product(M, N, K, x_dtype, true, i & 1, i & 2).partial_floats;
+    if (n > most) most = n;
+  }
+  return som::align_up(sizeof(float) * most, 256);
 }
 
 som_status som_product(const void* x, int64_t ldx, const void* W, int64_t ldw, int32_t w_units, int32_t x_dtype,
@@ -230,10 +233,12 @@ static BackwardWs backward_ws(int64_t M, int64_t N, int64_t K, int32_t dtype) {
   o += som::align_up(sizeof(float) * som::act_grad_ws_floats(M, N), 256);
   w.partial = o;
   size_t most = 0;
-  for (int units = 0; units < 2; ++units)
-    for (const size_t n : {som::plan_product(M, K, N, dtype, true, !units).partial_floats,
-                           som::plan_product(units ? N : K, units ? K : N, M, dtype, false, false).partial_floats})
+  for (int i = 0; i < 4; ++i) {        // either layout of W, rows on 16 bytes or not
+    const bool units = i & 1, dma = i & 2;
+    for (const size_t n : {som::plan_product(M, K, N, dtype, true, !units, dma).partial_floats,
+                           som::plan_product(units ? N : K, units ? K : N, M, dtype, false, false, dma).partial_floats})
       if (n > most) most = n;
+  }
   w.total = o + som::align_up(sizeof(float) * most, 256);
   return w;
 }

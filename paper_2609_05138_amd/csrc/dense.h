@@ -36,6 +36,18 @@ __device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
   }
 }
 
+// The same as they lie in memory (zero bits from n on), to be widened where they are
+// used: a load on its way takes half the registers.
+template <typename T>
+__device__ __forceinline__ typename Eight<T>::vec raw8(const T* p, int n) {
+  if (n >= 8) return *reinterpret_cast<const typename Eight<T>::at*>(p);
+  typename Eight<T>::vec r = {};
+#pragma unroll
+  for (int e = 0; e < 7; ++e)
+    if (e < n) r[e] = p[e];
+  return r;
+}
+
 // Rounds to nearest even, once.
 template <typename T>
 __device__ __forceinline__ void store8(T* p, int n, const float (&v)[8]) {

@@ -67,7 +67,8 @@ struct ProductPlan {
   int64_t k_split;
   size_t partial_floats;
 };
-ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc);
+// `dma`: the rows of both operands start on 16 bytes
+ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma);
 // Fills the launch's fields of `a` and enqueues it (and the join of a split k axis);
 // `partial`: plan_product's floats.
 hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream);

@@ -77,19 +77,21 @@ constexpr int64_t kCus = 256;
 // Times in us that the choice of a tile shape goes by, measured on MI355X (bf16, replayed
 // graphs of 20 products): a workgroup's start, first step and epilogue; a step of 128
 // bytes of k alone on a CU, where up to half of the CUs and where all have one; and for two
-// workgroups on a CU.  8-bit steps hold twice the products.
+// workgroups on a CU.  8-bit steps hold twice the products; steps of rows off 16 bytes go
+// through registers.
 struct ShapeTime {
-  double fixed, half, full, pair, e4m3;
+  double fixed, half, full, pair, e4m3, off;
 };
-constexpr ShapeTime kTime[kShapes] = {{11.0, 1.33, 1.50, 0, 1.8}, {9.5, 0.58, 0.80, 0, 1.6}, {4.4, 0.47, 0.52, 0, 1.4},
-                                      {4.1, 0.29, 0.33, 0.64, 1.2}, {3.4, 0.27, 0.28, 0.59, 1.1}, {3.4, 0.20, 0.22, 0.45, 1.1}};
+constexpr ShapeTime kTime[kShapes] = {{11.0, 1.33, 1.50, 0, 1.8, 1.35},   {9.5, 0.58, 0.80, 0, 1.6, 1.6},
+                                      {4.4, 0.47, 0.52, 0, 1.4, 1.8},     {4.1, 0.29, 0.33, 0.64, 1.2, 2.6},
+                                      {3.4, 0.27, 0.28, 0.59, 1.1, 2.8}, {3.4, 0.20, 0.22, 0.45, 1.1, 3.0}};
 // A split k axis: the second launch and its wait, and the parts' bytes per us.
 constexpr double kJoinTime = 4.5, kJoinBytes = 6.5e6;
 constexpr int64_t kMinSplitSteps = 4;
 
-double product_time(int shape, int64_t n, int64_t steps, bool e4m3) {
+double product_time(int shape, int64_t n, int64_t steps, bool e4m3, bool dma) {
   const ShapeTime& t = kTime[shape];
-  const double more = e4m3 ? t.e4m3 : 1.0;
+  const double more = (e4m3 ? t.e4m3 : 1.0) * (dma ? 1.0 : t.off);
   const double fill = n >= kCus ? 1.0 : n <= kCus / 2 ? 0.0 : static_cast<double>(n - kCus / 2) / (kCus / 2);
   const double alone = t.fixed + steps * more * (t.half + (t.full - t.half) * fill);
   const int64_t each = (n + kCus - 1) / kCus;                // workgroups of a CU
@@ -111,7 +113,7 @@ double product_time(int shape, int64_t n, int64_t steps, bool e4m3) {
 // launches).  With k strided one row does from 8,192 columns on (2,048 x 16,384: 13.4
 // against 17.6; two rows are no faster; 4,096 x 4,096: 11.4 against 8.9, since a
 // narrow strip's lines are read by several CUs).
-ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc) {
+ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma) {
   if (p_kc && (q_kc ? I <= 4 : I == 1 && J >= 8192)) return {kFew, 1, K, 0};
   const int64_t step = elem == kE4M3 ? 128 : 64;
   const int64_t steps = (K + step - 1) / step;
@@ -123,7 +125,7 @@ ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, b
     for (int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
       if (want > 1 && (steps < want * kMinSplitSteps || tiles * want > 4 * kCus)) break;
       const int64_t per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
-      double t = product_time(shape, tiles * splits, per, elem == kE4M3);
+      double t = product_time(shape, tiles * splits, per, elem == kE4M3, dma);
       if (splits > 1) t += kJoinTime + 8.0 * static_cast<double>(splits) * I * J / kJoinBytes;
       if (t < least) {
         least = t;
@@ -136,21 +138,21 @@ ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, b
 }
 
 hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream) {
-  const ProductPlan p = plan_product(a.I, a.J, a.K, a.elem, a.p_kc, a.q_kc);
+  const int64_t es = dtype_bytes(a.elem);
+  auto whole = [&](const void* p, int64_t ld) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * es % 16 == 0 && ld <= kDmaMaxLd;
+  };
+  a.dma = whole(a.P, a.ldp) && whole(a.Q, a.ldq);
+  const ProductPlan p = plan_product(a.I, a.J, a.K, a.elem, a.p_kc, a.q_kc, a.dma);
   a.splits = p.splits;
   if (p.shape == kFew) return launch_product_few(a, stream);
   const ShapeInfo& s = kInfo[p.shape];
-  const int64_t es = dtype_bytes(a.elem);
   a.k_split = p.k_split;
   a.partial = partial;
   a.tiles_i = static_cast<uint32_t>((a.I + s.bi - 1) / s.bi);
   a.tiles_j = static_cast<uint32_t>((a.J + s.bj - 1) / s.bj);
   const int64_t wgs = static_cast<int64_t>(a.tiles_i) * a.tiles_j * a.splits;
   a.per_xcd = static_cast<uint32_t>((wgs + kXcds - 1) / kXcds);
-  auto whole = [&](const void* p, int64_t ld) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * es % 16 == 0 && ld <= kDmaMaxLd;
-  };
-  a.dma = whole(a.P, a.ldp) && whole(a.Q, a.ldq);
   hipError_t e = a.elem == kF16 ? launch_product_f16(p.shape, a, stream)
                  : a.elem == kBF16 ? launch_product_bf16(p.shape, a, stream)
                                    : launch_product_e4m3(p.shape, a, stream);

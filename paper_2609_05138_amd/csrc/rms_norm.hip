@@ -143,103 +143,111 @@ __global__ void __launch_bounds__(1024) k_rms_norm_wide(const RmsNormArgs a) {
   }
 }
 
-// Threads per row: the fewest of 64, 256, 1024 that hold it with `most` groups of
-// eight each.  With many rows four groups a thread (fewer threads wait at a row's sums); with
-// few, one, so that a row's reads are all in flight at once.
+// Threads per row: the fewest of 64 to 1024 that hold it with two groups of eight each
+// (16,384 x 8,192 into 8 bits with a residual: 512 threads 170 us, 256 of four groups
+// 195; 65,536 x 2,048: 128 threads 167, 64 of four 180); with few rows, one, so that more
+// of a row's reads are in flight at once.  Wider rows than 1,024 threads hold so, four.
 constexpr int64_t kFewRows = 1024;
 constexpr int64_t kHeldCols = 1024 * 8 * 4;
 
+template <typename T, bool Q8, int G>
+void norm_with(const RmsNormArgs& a, int64_t groups, hipStream_t stream) {
+  constexpr int R = G < 256 ? 256 / G : 1;                 // rows per workgroup
+  const dim3 grid(static_cast<uint32_t>((a.rows + R - 1) / R)), block(G * R);
+  if (groups <= G)
+    hipLaunchKernelGGL((k_rms_norm<T, Q8, G, R, 1>), grid, block, 0, stream, a);
+  else if (groups <= 2 * G)
+    hipLaunchKernelGGL((k_rms_norm<T, Q8, G, R, 2>), grid, block, 0, stream, a);
+  else if constexpr (G == 1024)
+    hipLaunchKernelGGL((k_rms_norm<T, Q8, G, R, 4>), grid, block, 0, stream, a);
+}
+
 template <typename T, bool Q8>
 void norm_of(const RmsNormArgs& a, hipStream_t stream) {
-  const int64_t groups = (a.cols + 7) / 8;
-  const int64_t most = a.rows < kFewRows ? 1 : 4;
-#define SOM_NORM(G, R, U)                                                                                     \
-  hipLaunchKernelGGL((k_rms_norm<T, Q8, G, R, U>), dim3(static_cast<uint32_t>((a.rows + R - 1) / R)), dim3(G* R), 0, \
-                     stream, a)
-  if (a.cols > kHeldCols) {
+  const int64_t groups = (a.cols + 7) / 8, most = a.rows < kFewRows ? 1 : 2;
+  if (a.cols > kHeldCols)
     hipLaunchKernelGGL((k_rms_norm_wide<T, Q8>), dim3(static_cast<uint32_t>(a.rows)), dim3(1024), 0, stream, a);
-  } else if (groups <= 64 * most) {
-    if (groups <= 64)
-      SOM_NORM(64, 4, 1);
-    else if (groups <= 128)
-      SOM_NORM(64, 4, 2);
-    else
-      SOM_NORM(64, 4, 4);
-  } else if (groups <= 256 * most) {
-    if (groups <= 256)
-      SOM_NORM(256, 1, 1);
-    else if (groups <= 512)
-      SOM_NORM(256, 1, 2);
-    else
-      SOM_NORM(256, 1, 4);
-  } else {
-    if (groups <= 1024)
-      SOM_NORM(1024, 1, 1);
-    else if (groups <= 2048)
-      SOM_NORM(1024, 1, 2);
-    else
-      SOM_NORM(1024, 1, 4);
-  }
-#undef SOM_NORM
+  else if (groups <= 64 * most)
+    norm_with<T, Q8, 64>(a, groups, stream);
+  else if (groups <= 128 * most)
+    norm_with<T, Q8, 128>(a, groups, stream);
+  else if (groups <= 256 * most)
+    norm_with<T, Q8, 256>(a, groups, stream);
+  else if (groups <= 512 * most)
+    norm_with<T, Q8, 512>(a, groups, stream);
+  else
+    norm_with<T, Q8, 1024>(a, groups, stream);
 }
 
 // ---------------------------------------------------------------------------
 // Backward
 // ---------------------------------------------------------------------------
 
-// A workgroup of R groups of G threads takes every (gridDim * R)th row; dweight's
+// A workgroup of R groups of G threads takes every (gridDim * R)th row, the next one's
+// reads on their way while it works on one; dweight's
 // terms stay in the threads' registers (U * 8 columns each), and each workgroup
 // writes its sums, groups added in order, as one row of `part`.
-template <typename T, int G, int R, int U>
+template <typename T, int G, int R, int U, bool AHEAD>
 __global__ void __launch_bounds__(G* R) k_rms_norm_back(const RmsNormBackArgs a, float* __restrict__ part_w) {
   __shared__ float part[G * R / 64], part2[G * R / 64];
   extern __shared__ float cols_sum[];     // R > 1: a row of sums
   const int t = threadIdx.x % G, r = threadIdx.x / G;
-  float dw[U][8] = {};
+  using Raw = typename Eight<T>::vec;
+  struct Row {
+    Raw h[U], dy[U], dh[U];
+  };
   const int64_t step = static_cast<int64_t>(gridDim.x) * R;
+  int n[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) n[u] = left(a.cols, (static_cast<int64_t>(u) * G + t) * 8);
+  auto get = [&](int64_t row, Row& x) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t c = (static_cast<int64_t>(u) * G + t) * 8;
+      const int m = row < a.rows ? n[u] : 0;
+      x.h[u] = raw8(static_cast<const T*>(a.h) + row * a.ldh + c, m);
+      x.dy[u] = raw8(static_cast<const T*>(a.dy) + row * a.lddy + c, m);
+      if (a.dh) x.dh[u] = raw8(static_cast<const T*>(a.dh) + row * a.lddh + c, m);
+    }
+  };
+  Raw w[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t c = (static_cast<int64_t>(u) * G + t) * 8;
+    if (a.weight) w[u] = raw8(static_cast<const T*>(a.weight) + c, n[u]);
+  }
+  float dw[U][8] = {};
+  Row next;
+  get(static_cast<int64_t>(blockIdx.x) * R + r, next);
   for (int64_t first = static_cast<int64_t>(blockIdx.x) * R; first < a.rows; first += step) {
     const int64_t row = first + r;
-    const bool live = row < a.rows;
-    float h[U][8], d[U][8], ss = 0.0f, gh = 0.0f;
+    const Row now = next;
+    if (AHEAD) get(row + step, next);    // on its way while this row's sums are made
+    float ss = 0.0f, gh = 0.0f;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t c = (static_cast<int64_t>(u) * G + t) * 8;
-      const int n = live ? left(a.cols, c) : 0;
-      load8(static_cast<const T*>(a.h) + row * a.ldh + c, n, h[u]);
-      load8(static_cast<const T*>(a.dy) + row * a.lddy + c, n, d[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t c = (static_cast<int64_t>(u) * G + t) * 8;
-      float w[8];
-      if (a.weight) load8(static_cast<const T*>(a.weight) + c, left(a.cols, c), w);
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        ss = fmaf(h[u][e], h[u][e], ss);
-        gh = fmaf(a.weight ? d[u][e] * w[e] : d[u][e], h[u][e], gh);
+        const float h = static_cast<float>(now.h[u][e]), d = static_cast<float>(now.dy[u][e]);
+        ss = fmaf(h, h, ss);
+        gh = fmaf(a.weight ? d * static_cast<float>(w[u][e]) : d, h, gh);
       }
-    }
     const float s = rsqrtf(group_sum<G>(ss, part) / static_cast<float>(a.cols) + a.eps);
     const float k = group_sum<G>(gh, part2) / static_cast<float>(a.cols) * s * s;   // times s h: the projection
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int64_t c = (static_cast<int64_t>(u) * G + t) * 8;
-      const int n = live ? left(a.cols, c) : 0;
-      float w[8], o[8];
-      if (a.weight) load8(static_cast<const T*>(a.weight) + c, n, w);
+      float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        dw[u][e] = fmaf(d[u][e] * h[u][e], s, dw[u][e]);
-        o[e] = s * ((a.weight ? d[u][e] * w[e] : d[u][e]) - h[u][e] * k);
+        const float h = static_cast<float>(now.h[u][e]), d = static_cast<float>(now.dy[u][e]);
+        dw[u][e] = fmaf(d * h, s, dw[u][e]);
+        o[e] = s * ((a.weight ? d * static_cast<float>(w[u][e]) : d) - h * k);
+        if (a.dh) o[e] += static_cast<float>(now.dh[u][e]);
       }
-      if (a.dh) {
-        float dh[8];
-        load8(static_cast<const T*>(a.dh) + row * a.lddh + c, n, dh);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] += dh[e];
-      }
-      store8(static_cast<T*>(a.dx) + row * a.lddx + c, n, o);
+      store8(static_cast<T*>(a.dx) + row * a.lddx + c, row < a.rows ? n[u] : 0, o);
     }
+    if (!AHEAD) get(row + step, next);
   }
   if (!a.dweight) return;
   if constexpr (R > 1) {
@@ -336,7 +344,7 @@ struct BackPlan {
 };
 BackPlan back_plan(int64_t rows, int64_t cols) {
   if (cols > kBackHeldCols) return {rows < kWideRowGroups ? rows : kWideRowGroups, 2 * rows};
-  const int64_t per = cols <= 512 ? 8 : cols <= 4096 ? 2 : 1;     // rows per workgroup
+  const int64_t per = cols <= 512 ? 8 : cols <= 2048 ? 2 : 1;     // rows per workgroup
   const int64_t all = (rows + per - 1) / per;
   return {all < kBackGroups ? all : kBackGroups, 0};
 }
@@ -351,19 +359,19 @@ void back_of(const RmsNormBackArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((k_rms_norm_back_wide<T>), grid, dim3(256), 0, stream, a, a.ws, part);
     return;
   }
-#define SOM_BACK(G, R, U)                                                                                        \
-  hipLaunchKernelGGL((k_rms_norm_back<T, G, R, U>), dim3(static_cast<uint32_t>(p.groups)), dim3(G* R),           \
+#define SOM_BACK(G, R, U, AHEAD)                                                                                 \
+  hipLaunchKernelGGL((k_rms_norm_back<T, G, R, U, AHEAD>), dim3(static_cast<uint32_t>(p.groups)), dim3(G* R),    \
                      R > 1 ? G * U * 8 * sizeof(float) : 0, stream, a, part)
   if (a.cols <= 512)
-    SOM_BACK(64, 8, 1);
+    SOM_BACK(64, 8, 1, true);
   else if (a.cols <= 2048)
-    SOM_BACK(256, 2, 1);
+    SOM_BACK(256, 2, 1, true);
   else if (a.cols <= 4096)
-    SOM_BACK(256, 2, 2);
+    SOM_BACK(512, 1, 1, true);
   else if (a.cols <= 8192)
-    SOM_BACK(512, 1, 2);
+    SOM_BACK(512, 1, 2, true);
   else
-    SOM_BACK(1024, 1, 2);
+    SOM_BACK(1024, 1, 2, false);
 #undef SOM_BACK
 }
 
