@@ -84,7 +84,7 @@ struct ShapeTime {
 };
 constexpr ShapeTime kTime[kShapes] = {{11.0, 1.33, 1.50, 0, 1.8, 1.35},   {9.5, 0.58, 0.80, 0, 1.6, 1.6},
                                       {4.4, 0.47, 0.52, 0, 1.4, 1.8},     {4.1, 0.29, 0.33, 0.64, 1.2, 2.6},
-                                      {3.4, 0.27, 0.28, 0.59, 1.1, 2.8}, {3.4, 0.20, 0.22, 0.45, 1.1, 3.0}};
+                                      {3.4, 0.27, 0.28, 0.59, 1.1, 3.3}, {3.4, 0.20, 0.22, 0.45, 1.1, 4.5}};
 // A split k axis: the second launch and its wait, and the parts' bytes per us.
 constexpr double kJoinTime = 4.5, kJoinBytes = 6.5e6;
 constexpr int64_t kMinSplitSteps = 4;
