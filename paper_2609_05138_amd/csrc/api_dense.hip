@@ -159,11 +159,10 @@ som_status som_rms_norm_backward(const void* dy, int64_t lddy, const void* h, in
 size_t som_product_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t x_dtype) {
   if (M < 1 || M > kI32Max || N < 1 || N > kMaxK || K < 1 || K > kMaxK || x_dtype < SOM_F16 || x_dtype > SOM_E4M3)
     return 0;
-  size_t most = 0;
-  for (int i = 0; i < 4; ++i) {        // either layout of W, rows on 16 bytes or not
-    const size_t n = som::plan_product(M, N, K, x_dtype, true, i & 1, i & 2).partial_floats;
-    if (n > most) most = n;
-  }
+  // rows on 16 bytes or not; unit-major weights take the same shapes, or need nothing
+  const size_t on = som::plan_product(M, N, K, x_dtype, true, false, true).partial_floats;
+  const size_t off = som::plan_product(M, N, K, x_dtype, true, false, false).partial_floats;
+  const size_t most = on > off ? on : off;
   return som::align_up(sizeof(float) * most, 256);
 }
 
@@ -233,12 +232,11 @@ static BackwardWs backward_ws(int64_t M, int64_t N, int64_t K, int32_t dtype) {
   o += som::align_up(sizeof(float) * som::act_grad_ws_floats(M, N), 256);
   w.partial = o;
   size_t most = 0;
-  for (int i = 0; i < 4; ++i) {        // either layout of W, rows on 16 bytes or not
-    const bool units = i & 1, dma = i & 2;
-    for (const size_t n : {som::plan_product(M, K, N, dtype, true, !units, dma).partial_floats,
-                           som::plan_product(units ? N : K, units ? K : N, M, dtype, false, false, dma).partial_floats})
+  for (const bool dma : {true, false})   // rows on 16 bytes or not; either layout of W
+    for (const size_t n : {som::plan_product(M, K, N, dtype, true, false, dma).partial_floats,
+                           som::plan_product(K, N, M, dtype, false, false, dma).partial_floats,
+                           som::plan_product(N, K, M, dtype, false, false, dma).partial_floats})
       if (n > most) most = n;
-  }
   w.total = o + som::align_up(sizeof(float) * most, 256);
   return w;
 }

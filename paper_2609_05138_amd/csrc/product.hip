@@ -119,9 +119,13 @@ ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, b
   const int64_t steps = (K + step - 1) / step;
   ProductPlan best{kShape256, 1, steps * step, 0};
   double least = 1e300;
-  for (int shape = 0; shape < (p_kc ? static_cast<int>(kShapes) : kShape32); ++shape) {
+  const int last = p_kc ? kShape16 : kShape64;
+  for (int shape = 0; shape <= last; ++shape) {
     const ShapeInfo& s = kInfo[shape];
+    // not worth the host's time: tiles of four times the rows, or very many of them
+    if (s.bi >= 4 * I && shape < last) continue;
     const int64_t tiles = ((I + s.bi - 1) / s.bi) * ((J + s.bj - 1) / s.bj);
+    if (tiles > 16 * kCus && shape > kShape256) break;
     for (int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
       if (want > 1 && (steps < want * kMinSplitSteps || tiles * want > 4 * kCus)) break;
       const int64_t per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
