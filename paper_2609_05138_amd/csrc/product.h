@@ -17,12 +17,14 @@
 //        64-bit read
 //
 // Where rows do not start on 16 bytes, at columns that end inside a chunk and in the
-// last, partial step the chunks go through registers, element by element at the ends:
-// no element outside the matrices is read, and what lies beyond k counts as zero in both
-// operands (so a NaN there cannot reach a sum).
+// last, partial step the chunks go through registers: a chunk that a row's end cuts is
+// read as the 16 bytes up to that end and shifted, a row shorter than a chunk element
+// by element, so no element outside the matrices is read, and what lies beyond k
+// counts as zero in both operands (a NaN there cannot reach a sum).
 //
 // The matrix instructions take Q as their first operand: a lane then holds four
-// consecutive j of one i, which is how the epilogue reads and writes rows of C.
+// consecutive j of one i, and puts them with one access into the LDS that the operands
+// have left, from which the epilogue reads and writes whole rows of the tile.
 #pragma once
 
 #include "dense.h"
@@ -171,15 +173,26 @@ __device__ __forceinline__ float act_grad(int act, float v) {
   }
 }
 
+// Rows of 16 bits go past the L2, whose lines the operands need (8,192 x 4,096 x 16,384
+// 905 to 886 us); a lane's eight fp32 are two accesses of every other 16 bytes, which
+// the L2 puts together (past it 4,096 x 2,048 x 16,384 took 305 us instead of 279).
+template <typename T>
+__device__ __forceinline__ void store8_stream(T* p, const float (&v)[8]) {
+  typename Eight<T>::vec r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = static_cast<T>(v[e]);
+  __builtin_nontemporal_store(r, reinterpret_cast<typename Eight<T>::at*>(p));
+}
+
 template <bool kWhole>
 __device__ __forceinline__ void store8_as(int type, void* base, int64_t at, int n, const float (&v)[8]) {
   if (kWhole) n = 8;
   if (type == kF32)
     store8(static_cast<float*>(base) + at, n, v);
   else if (type == kF16)
-    store8(static_cast<f16*>(base) + at, n, v);
+    kWhole ? store8_stream(static_cast<f16*>(base) + at, v) : store8(static_cast<f16*>(base) + at, n, v);
   else
-    store8(static_cast<bf16*>(base) + at, n, v);
+    kWhole ? store8_stream(static_cast<bf16*>(base) + at, v) : store8(static_cast<bf16*>(base) + at, n, v);
 }
 
 // What the epilogue takes from memory for eight columns: of all rows, and of one row
