@@ -14,6 +14,9 @@
  * sparse-dense product whose argmin is fused into the product (same
  * section).  Ties go to the lowest neuron index.
  *
+ * Dense documents (rows of 16- or 8-bit states) reach a map through the
+ * section of that name below: norm, product and dropout, with gradients.
+ *
  * Conventions for every entry point:
  *  - Pointers are DEVICE pointers owned by the caller unless stated.  The
  *    library allocates nothing and keeps no pointer after it returns.
@@ -30,7 +33,7 @@
  *    are allowed.  Malformed CSR is undefined behaviour unless
  *    opts->validate is set, in which case it is detected on the device and
  *    reported as SOM_ERR_INVALID_CSR before any search work runs.
- *  - Non-finite weights are undefined behaviour.
+ *  - Non-finite weights are undefined behaviour in the search and the update.
  */
 #ifndef SOM_H
 #define SOM_H
@@ -504,8 +507,9 @@ som_status som_rms_norm_backward(const void* dy, int64_t lddy, const void* h, in
  *
  * x [M][ldx] and W are of type x_dtype (fp16, bf16 or SOM_E4M3).  W is
  * feature-major like a codebook, W[k * ldw + n], or with w_units set unit-major,
- * W[n * ldw + k]; 8-bit weights are unit-major only (the matrix instructions
- * take 16 bytes of one unit at a time).  y, residual and pre are of type y_dtype
+ * W[n * ldw + k]; 8-bit weights are unit-major only (the matrix
+ * instructions take consecutive k of one unit, and no transposing read goes
+ * with 8 bits here).  y, residual and pre are of type y_dtype
  * (x_dtype or fp32; fp32, fp16 or bf16 for 8-bit x).  bias [N], x_scale [M] and
  * w_scale [N] are fp32.  A dense document's scores against a codebook are
  * alpha = -2 with the codebook's norms as bias.

@@ -6,6 +6,7 @@
 // 32: the generator's 20 wide multiplications, which run at a quarter of the vector rate,
 // would take longer than the element's bytes.  The rate p is thus a multiple of 2^-16, and
 // the kept elements' factor is of that multiple, so the expectation is exact.
+// Bound: HBM (16,384 x 8,192 bf16 with a residual 139 us, 5.8 TB/s).
 #include "dense.h"
 
 namespace som {

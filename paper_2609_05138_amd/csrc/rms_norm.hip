@@ -4,7 +4,9 @@
 //   forward   h = x + r;  s = 1 / sqrt(mean h^2 + eps);  y = h s w
 //   backward  g = dy w;  dx = s g - h s^3 mean(g h) + dh;  dw_c = sum_rows dy h s
 //
-// Bound: HBM, a few operations per element.  A row is read once and stays in the
+// Bound: HBM, a few operations per element (16,384 x 8,192 bf16 with a residual into 8
+// bits 172 us, 5.5 TB/s; the gradient of 8,192 x 4,096 53 us, 5.1 TB/s; one row of 4,096
+// 2.6 us, a launch).  A row is read once and stays in the
 // registers of the G threads that share it, 8 elements (16 bytes of a 16-bit type) a
 // thread and read, while its sums are made.  Rows too wide for that are read again.
 #include "dense.h"
@@ -183,10 +185,10 @@ void norm_of(const RmsNormArgs& a, hipStream_t stream) {
 // Backward
 // ---------------------------------------------------------------------------
 
-// A workgroup of R groups of G threads takes every (gridDim * R)th row, the next one's
-// reads on their way while it works on one; dweight's
-// terms stay in the threads' registers (U * 8 columns each), and each workgroup
-// writes its sums, groups added in order, as one row of `part`.
+// A workgroup of R groups of G threads takes every (gridDim * R)th row; dweight's terms
+// stay in the threads' registers (U * 8 columns each), and each workgroup writes its
+// sums, groups added in order, as one row of `part`.  AHEAD: the next row's reads are on
+// their way while it works on one (8,192 x 4,096: 52 us; without, 67).
 template <typename T, int G, int R, int U, bool AHEAD>
 __global__ void __launch_bounds__(G* R) k_rms_norm_back(const RmsNormBackArgs a, float* __restrict__ part_w) {
   __shared__ float part[G * R / 64], part2[G * R / 64];
