@@ -516,7 +516,8 @@ som_status som_rms_norm_backward(const void* dy, int64_t lddy, const void* h, in
  *
  * e may be NULL (alpha 1, nothing else).  residual may be y itself.  pre, if given,
  * receives the activation's argument, which the gradient needs.
- * M in [0, 2^31), N and K in [1, 2^30], M * N up to 2^42.  ws:
+ * M in [0, 2^31), N and K in [1, 2^30], ceil(M / 256) ceil(N / 128) up to
+ * 2^23 - 8 (about 2^38 elements).  ws:
  * som_product_workspace_bytes(M, N, K, x_dtype) bytes, 256-byte aligned (0
  * bytes: ws may be NULL). */
 typedef struct som_epilogue {
@@ -545,7 +546,8 @@ som_status som_product(const void* x, int64_t ldx, const void* W, int64_t ldw, i
  * dx and dW (laid out as W is) are of x's type, dbias is fp32; each may be
  * NULL.  With an activation dP is rounded to x's type for the two products
  * (dbias sums it unrounded).  The residual's gradient is dy.  relu' is 0 at 0.
- * With M == 0 dW and dbias are set to zero.
+ * With M == 0 dW and dbias are set to zero.  M up to 2^30; the limit of a product
+ * holds for dx, dW and dW's transpose.
  * ws: som_product_backward_workspace_bytes, 256-byte aligned. */
 size_t som_product_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype);
 som_status som_product_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* W, int64_t ldw,

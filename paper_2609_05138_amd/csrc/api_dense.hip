@@ -17,7 +17,7 @@ static_assert(som::kActNone == SOM_ACT_NONE && som::kActRelu == SOM_ACT_RELU && 
 
 constexpr int64_t kMaxK = int64_t(1) << 30;       // a step past the end stays an int32
 constexpr int64_t kMaxLd = int64_t(1) << 40;      // row offsets stay inside 64-bit bytes
-constexpr int64_t kMaxTiles = (int64_t(1) << 31) - 16;
+constexpr int64_t kMaxTiles = (int64_t(1) << 23) - 8;   // of 512 threads, under a launch's 2^32
 
 bool is_float(int32_t t) { return t == SOM_F32 || t == SOM_F16 || t == SOM_BF16; }
 
@@ -59,10 +59,9 @@ som_status check_sizes(int64_t M, int64_t N, int64_t K) {
   return SOM_OK;
 }
 
-// Workgroups of C [I][J] in the smallest tiles, and threads of the join.
-bool launchable(int64_t I, int64_t J) {
-  return (I + 15) / 16 <= kMaxTiles / ((J + 127) / 128) && I <= (kMaxTiles * 256) / ((J + 3) / 4);
-}
+// Workgroups of C [I][J]: 256 x 256, or up to 64 rows by 128 columns (then of a strip).
+// Smaller tiles and splits are for launches of a few thousand.
+bool launchable(int64_t I, int64_t J) { return (I + 255) / 256 <= kMaxTiles / ((J + 127) / 128); }
 
 #define SOM_CHECK(call)                 \
   do {                                  \
@@ -256,7 +255,7 @@ som_status som_product_backward(const void* dy, int64_t lddy, const void* x, int
   SOM_CHECK(check_sizes(M, N, K));
   if (M > kMaxK) return fail(SOM_ERR_INVALID_ARG, "M must be in [0, 2^30]");
   if (act < SOM_ACT_NONE || act > SOM_ACT_SILU) return fail(SOM_ERR_INVALID_ARG, "unknown activation");
-  if (!launchable(M, K) || !launchable(K, N)) return fail(SOM_ERR_INVALID_ARG, "a product is too large for one call");
+  if (!launchable(M, K) || !launchable(K, N) || !launchable(N, K)) return fail(SOM_ERR_INVALID_ARG, "a product is too large for one call");
   const int64_t wr = w_units ? N : K, wc = w_units ? K : N;
   if (dW) SOM_CHECK(check_matrix("dW", dW, lddw, wr, wc, dtype));
   SOM_CHECK(check_vector("dbias", dbias));

@@ -15,6 +15,16 @@ typedef _Float16 f16;
 inline int dtype_bytes(int t) { return t == kF32 ? 4 : t == kE4M3 ? 1 : 2; }
 
 // Eight consecutive elements at any address an element may have.
+// A launch holds fewer than 2^32 threads along x: more than 2^21 workgroups (of up to
+// 1,024) lie in several rows of the grid.  The last row may be longer than the work.
+inline dim3 groups_grid(int64_t n) {
+  constexpr int64_t kMost = int64_t(1) << 21;
+  return n <= kMost ? dim3(static_cast<uint32_t>(n)) : dim3(kMost, static_cast<uint32_t>((n + kMost - 1) / kMost));
+}
+__device__ __forceinline__ int64_t group_index() {
+  return static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
+}
+
 template <typename T>
 struct Eight {
   typedef T vec __attribute__((ext_vector_type(8)));

@@ -88,6 +88,7 @@ constexpr ShapeTime kTime[kShapes] = {{11.0, 1.33, 1.50, 0, 1.8, 1.35},   {9.5, 
 // A split k axis: the second launch and its wait, and the parts' bytes per us.
 constexpr double kJoinTime = 4.5, kJoinBytes = 6.5e6;
 constexpr int64_t kMinSplitSteps = 4;
+constexpr int64_t kFewMaxColumns = int64_t(1) << 26;   // 32 threads each at most, of a launch's 2^32
 
 double product_time(int shape, int64_t n, int64_t steps, bool e4m3, bool dma) {
   const ShapeTime& t = kTime[shape];
@@ -114,7 +115,7 @@ double product_time(int shape, int64_t n, int64_t steps, bool e4m3, bool dma) {
 // against 17.6; two rows are no faster; 4,096 x 4,096: 11.4 against 8.9, since a
 // narrow strip's lines are read by several CUs).
 ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma) {
-  if (p_kc && (q_kc ? I <= 4 : I == 1 && J >= 8192)) return {kFew, 1, K, 0};
+  if (p_kc && J <= kFewMaxColumns && (q_kc ? I <= 4 : I == 1 && J >= 8192)) return {kFew, 1, K, 0};
   const int64_t step = elem == kE4M3 ? 128 : 64;
   const int64_t steps = (K + step - 1) / step;
   ProductPlan best{kShape256, 1, steps * step, 0};
@@ -122,10 +123,12 @@ ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, b
   const int last = p_kc ? kShape16 : kShape64;
   for (int shape = 0; shape <= last; ++shape) {
     const ShapeInfo& s = kInfo[shape];
-    // not worth the host's time: tiles of four times the rows, or very many of them
+    // not worth the host's time: tiles of four times the rows, or very many of them unless
+    // they are one row (40 x 512 x 1,048,576: 64 x 128 254 us, 128 x 128 338; 16 x 1,024 x
+    // 1,048,576: 451, 256 x 256 586)
     if (s.bi >= 4 * I && shape < last) continue;
     const int64_t tiles = ((I + s.bi - 1) / s.bi) * ((J + s.bj - 1) / s.bj);
-    if (tiles > 16 * kCus && shape > kShape256) break;
+    if (tiles > 16 * kCus && least < 1e300 && s.bi < I) break;
     for (int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
       if (want > 1 && (steps < want * kMinSplitSteps || tiles * want > 4 * kCus)) break;
       const int64_t per = (steps + want - 1) / want, splits = (steps + per - 1) / per;

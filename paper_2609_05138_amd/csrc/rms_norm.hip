@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(G* R) k_rms_norm(const RmsNormArgs a) {
   __shared__ float part[G * R / 64];
   __shared__ uint32_t tops[G * R / 64];
   const int t = threadIdx.x % G;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * R + threadIdx.x / G;
+  const int64_t row = group_index() * R + threadIdx.x / G;
   const bool live = row < a.rows;
   float v[U][8], ss = 0.0f;
 #pragma unroll
@@ -103,7 +103,8 @@ template <typename T, bool Q8>
 __global__ void __launch_bounds__(1024) k_rms_norm_wide(const RmsNormArgs a) {
   __shared__ float part[16];
   __shared__ uint32_t tops[16];
-  const int64_t row = blockIdx.x;
+  const int64_t row = group_index();
+  if (row >= a.rows) return;
   float v[8], ss = 0.0f;
   for (int64_t c = threadIdx.x * 8; c < a.cols; c += 8192) {
     load_h<T>(a, row, c, left(a.cols, c), v);
@@ -155,7 +156,7 @@ constexpr int64_t kHeldCols = 1024 * 8 * 4;
 template <typename T, bool Q8, int G>
 void norm_with(const RmsNormArgs& a, int64_t groups, hipStream_t stream) {
   constexpr int R = G < 256 ? 256 / G : 1;                 // rows per workgroup
-  const dim3 grid(static_cast<uint32_t>((a.rows + R - 1) / R)), block(G * R);
+  const dim3 grid = groups_grid((a.rows + R - 1) / R), block(G * R);
   if (groups <= G)
     hipLaunchKernelGGL((k_rms_norm<T, Q8, G, R, 1>), grid, block, 0, stream, a);
   else if (groups <= 2 * G)
@@ -168,7 +169,7 @@ template <typename T, bool Q8>
 void norm_of(const RmsNormArgs& a, hipStream_t stream) {
   const int64_t groups = (a.cols + 7) / 8, most = a.rows < kFewRows ? 1 : 2;
   if (a.cols > kHeldCols)
-    hipLaunchKernelGGL((k_rms_norm_wide<T, Q8>), dim3(static_cast<uint32_t>(a.rows)), dim3(1024), 0, stream, a);
+    hipLaunchKernelGGL((k_rms_norm_wide<T, Q8>), groups_grid(a.rows), dim3(1024), 0, stream, a);
   else if (groups <= 64 * most)
     norm_with<T, Q8, 64>(a, groups, stream);
   else if (groups <= 128 * most)
@@ -284,7 +285,8 @@ __global__ void __launch_bounds__(G* R) k_rms_norm_back(const RmsNormBackArgs a,
 template <typename T>
 __global__ void __launch_bounds__(1024) k_rms_norm_back_stats(const RmsNormBackArgs a, float* __restrict__ stats) {
   __shared__ float part[16], part2[16];
-  const int64_t row = blockIdx.x;
+  const int64_t row = group_index();
+  if (row >= a.rows) return;
   float ss = 0.0f, gh = 0.0f;
   for (int64_t c = threadIdx.x * 8; c < a.cols; c += 8192) {
     const int n = left(a.cols, c);
@@ -356,7 +358,7 @@ void back_of(const RmsNormBackArgs& a, hipStream_t stream) {
   const BackPlan p = back_plan(a.rows, a.cols);
   float* part = a.ws + p.stats;
   if (a.cols > kBackHeldCols) {
-    hipLaunchKernelGGL((k_rms_norm_back_stats<T>), dim3(static_cast<uint32_t>(a.rows)), dim3(1024), 0, stream, a, a.ws);
+    hipLaunchKernelGGL((k_rms_norm_back_stats<T>), groups_grid(a.rows), dim3(1024), 0, stream, a, a.ws);
     const dim3 grid(static_cast<uint32_t>((a.cols + 2047) / 2048), static_cast<uint32_t>(p.groups));
     hipLaunchKernelGGL((k_rms_norm_back_wide<T>), grid, dim3(256), 0, stream, a, a.ws, part);
     return;
@@ -383,7 +385,7 @@ __global__ void __launch_bounds__(1024)
 k_column_sums(const float* __restrict__ part, int64_t groups, int64_t ld, int64_t cols, float* __restrict__ out) {
   __shared__ float sums[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+  const int64_t c = group_index() * 64 + lane;
   float s = 0.0f;
   if (c < cols)
     for (int64_t g0 = wave; g0 < groups; g0 += 16 * 8) {
@@ -439,7 +441,7 @@ hipError_t launch_rms_norm_back(const RmsNormBackArgs& a, hipStream_t stream) {
 
 hipError_t launch_column_sums(const float* part, int64_t groups, int64_t ld, int64_t cols, float* out,
                               hipStream_t stream) {
-  hipLaunchKernelGGL(k_column_sums, dim3(static_cast<uint32_t>((cols + 63) / 64)), dim3(1024), 0, stream, part, groups,
+  hipLaunchKernelGGL(k_column_sums, groups_grid((cols + 63) / 64), dim3(1024), 0, stream, part, groups,
                      ld, cols, out);
   return hipGetLastError();
 }

@@ -93,6 +93,14 @@ def test_product_refuses(lib):
     assert size(0, 1, 1, BF16) == 0 and size(1, 0, 1, BF16) == 0 and size(1, 1, 0, BF16) == 0 and size(9, 9, 9, F32) == 0
 
 
+def test_product_refuses_more_than_a_launch_holds(lib):
+    # ceil(M / 256) ceil(N / 128) up to 2^23 - 8
+    args = dict(x=FAKE, ldx=64, W=FAKE, ldw=1 << 30, w_units=0, x_dtype=BF16, M=4, N=32, K=64, y=FAKE, ldy=1 << 30,
+                y_dtype=BF16, e=None, ws=None, ws_bytes=0, stream=None)
+    _refuses(lib, "som_product", args, [dict(M=1, N=1 << 30), dict(M=(1 << 31) - 1, N=128, ldy=128),
+                                        dict(M=1 << 20, N=1 << 19)])
+
+
 def test_product_gradient_refuses(lib):
     args = dict(dy=FAKE, lddy=32, x=FAKE, ldx=64, W=FAKE, ldw=32, w_units=0, dtype=F16, M=4, N=32, K=64, act=4, pre=FAKE,
                 ldp=32, alpha=1.0, dx=FAKE, lddx=64, dW=FAKE, lddw=32, dbias=FAKE, ws=FAKE, ws_bytes=1 << 30, stream=None)

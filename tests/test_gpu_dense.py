@@ -175,6 +175,29 @@ def test_norm_rows_past_32_bits():
     assert dx.shape == (rows, cols) and bool(dx.isfinite().all())
 
 
+def test_norm_of_more_rows_than_one_row_of_a_grid():
+    # 2^26 rows of 64 threads each pass the 2^32 threads that a launch holds along one axis
+    rows, cols = (1 << 26) + 5, 2
+    x = (torch.arange(rows * cols, device=DEV, dtype=torch.int32) % 61 - 30).to(torch.float16).view(rows, cols)
+    y, _, _ = som.som_rms_norm(x, None, 0.5)
+    for at in (0, (1 << 23) - 7, rows - 4000):
+        want, _ = oracle.rms_norm(_np(x[at:at + 4000]), None, 0.5)
+        _near(y[at:at + 4000], want, np.abs(want) * (HALF["f16"] + 2 * CALC) + TINY["f16"])
+    assert bool((y.float().sign() == x.float().sign()).all())
+
+
+def test_norm_gradient_of_more_columns_than_one_row_of_a_grid():
+    # the columns' sums: 16 threads each, 2^28 columns
+    cols = (1 << 28) + 64
+    h = (torch.arange(cols, device=DEV, dtype=torch.int32) % 5 - 2).to(torch.bfloat16).view(1, cols)
+    dweight = torch.full((cols,), 9.0, device=DEV)
+    dx, _ = som.som_rms_norm_backward(h, h, None, 2.0, dx=h.clone(), dweight=dweight)
+    # mean h^2 is 2 but for the last pattern's part: s = 1 / 2
+    want = h[0].float() ** 2 * 0.5
+    assert bool(((dweight - want).abs() <= 1e-3 * want).all())
+    assert bool(dx.isfinite().all())
+
+
 # --------------------------------------------------------------------------- product
 
 def _weight_layout(W, units, dtype, pad, lead=0):
@@ -349,6 +372,17 @@ def test_product_past_32_bits():
     dx, dW, dbias = som.som_product_backward(dy, x, torch.ones((K, 16), dtype=torch.bfloat16, device=DEV))
     assert torch.equal(dW, (x.double().t().contiguous() @ dy.double()).to(torch.bfloat16))
     assert torch.equal(dbias.double(), dy.double().sum(0))
+
+
+@pytest.mark.parametrize("M,N,K,units", [(1, (1 << 26) + 77, 4, True), (1, (1 << 27) + 9, 1, False), (16, 1 << 20, 24, False),
+                                         (3, 600001, 70, False), (9, 530000, 64, True)])
+def test_product_of_few_rows_and_very_many_columns(M, N, K, units):
+    x = torch.randint(-3, 4, (M, K), device=DEV).to(torch.bfloat16)
+    W = torch.randint(-3, 4, (N, K) if units else (K, N), device=DEV, dtype=torch.int8).to(torch.bfloat16)
+    y = som.som_product(x, W.t() if units else W, dtype=torch.float32)
+    for at in (0, N // 2 - 1000, N - 5000):
+        part = W[at:at + 5000].t() if units else W[:, at:at + 5000]
+        assert torch.equal(y[:, at:at + 5000].double(), x.double() @ part.double().contiguous()), at
 
 
 # --------------------------------------------------------------------------- dropout
