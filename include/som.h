@@ -479,7 +479,7 @@ typedef enum som_act {
  * the sum before its rounding to h.  h may be x or residual themselves (same
  * stride), which updates a residual stream in place.  y is of type `dtype`, or
  * with q8 of 8 bits (SOM_E4M3) with an fp32 factor for each row: y = q scale[row], scale
- * = max_c |y_c| / 448 (1 for a row of zeros).  scale is NULL without q8.
+ * = max_c |y_c| / 448, at least 2^-126 (1 for a row of zeros).  scale is NULL without q8.
  * A row holding a NaN or an infinity gives NaNs.  1 <= cols < 2^31. */
 som_status som_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
                         int32_t dtype, int64_t rows, int64_t cols, float eps, int32_t q8, void* y, int64_t ldy,

@@ -110,6 +110,20 @@ def test_norm_special_rows():
     assert bool(y.isnan().all())
 
 
+def test_norm_of_rows_next_to_nothing_in_8_bits():
+    # |y| / 448 below the normal numbers: its inverse would be infinite
+    x = torch.zeros((6, 700), device=DEV)
+    for row, top in enumerate((1e-35, 1e-38, 1e-40, 1e-43, 1e-45, 0.0)):
+        x[row] = torch.linspace(-top, top, 700, device=DEV, dtype=torch.float64).float()
+    for wide in (x, torch.cat([x] * 60, 1)):
+        want, _ = oracle.rms_norm(_np(wide), None, 1e-6)
+        q, _, scale = som.som_rms_norm(wide, None, 1e-6, q8=True)
+        assert bool(q.float().isfinite().all()) and bool((scale > 0).all())
+        # half a step of 4 bits, or of the type's (and fp32's) smallest values
+        _near(q.double() * scale.double()[:, None], want, np.abs(want) * (2.0 ** -4 + CALC)
+              + 2.0 ** -10 * _np(scale)[:, None] + 2.0 ** -148)
+
+
 @pytest.mark.parametrize("cols", [40, 4097, 40000])
 def test_norm_updates_a_residual_stream_in_place(cols):
     rng = np.random.default_rng(cols)
