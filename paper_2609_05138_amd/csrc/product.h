@@ -396,21 +396,25 @@ struct Operand {
   // the row's end cuts (KS: the matrix's last columns; KC, with kLast: `end`), the 16
   // bytes up to that end, which `store` or `load` shifts into place; the places after it
   // are zero.  A row shorter than a chunk goes element by element.
+  // (Pointers into global memory by type: made from `uniform`'s integers they are not known
+  // to be, and a flat load, which may be of LDS, holds up every wait for LDS.)
+  template <typename V>
+  using Global = const __attribute__((address_space(1))) V;
   static __device__ __forceinline__ u4 some(const char* p, int64_t n) {
     u4 v = {0, 0, 0, 0};
     if constexpr (ES == 2) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (e < n) v[e / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[e]) << (16 * (e % 2));
+        if (e < n) v[e / 2] |= static_cast<uint32_t>(((Global<uint16_t>*)p)[e]) << (16 * (e % 2));
     } else {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        if (e < n) v[e / 4] |= static_cast<uint32_t>(reinterpret_cast<const uint8_t*>(p)[e]) << (8 * (e % 4));
+        if (e < n) v[e / 4] |= static_cast<uint32_t>(((Global<uint8_t>*)p)[e]) << (8 * (e % 4));
     }
     return v;
   }
   static __device__ __forceinline__ u4 all(const char* p) {
-    return ES == 2 ? u4(*reinterpret_cast<const u4_at2*>(p)) : u4(*reinterpret_cast<const u4_at1*>(p));
+    return ES == 2 ? u4(*(Global<u4_at2>*)p) : u4(*(Global<u4_at1>*)p);
   }
   // the last n (of kPer, 0 < n < kPer) elements moved to the front
   static __device__ __forceinline__ u4 front(u4 v, int n) {
@@ -461,6 +465,22 @@ struct Operand {
         else
           v[n] = some(p, cols);
       }
+    }
+  }
+  // The same of a whole step, without a branch (KS: 8 columns and more): the number of
+  // loads on their way is then known where one is waited for.  What is not kept is read
+  // too: KS, past the columns, the tile's first 16 bytes or those up to the row's end.
+  __device__ __forceinline__ void load_plain(int32_t k, u4 (&v)[kEach]) const {
+    const char* const b = at(k);
+    int r, c;
+    place(pos(0), &r, &c);
+    const int cols = cut();
+    const int64_t first = rows < 8 ? (rows - 8) * 2 : 0;
+    const int64_t at_col = KC ? c * 16 : c * 8 >= rows ? first : cols ? c * 16 - (8 - cols) * 2 : c * 16;
+#pragma unroll
+    for (int n = 0; n < kEach; ++n) {
+      const int row = r + n * kRowsEach;
+      v[n] = all(b + (KC && row >= rows ? 0 : row) * ld + at_col);
     }
   }
   __device__ __forceinline__ void store(char* lds, int64_t extent, const u4 (&v)[kEach]) const {
@@ -713,32 +733,66 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
     }
   }
   if (t < steps) {
-    // Through registers, one step on its way, two in LDS.  (Two or three on their way, or
-    // the order of reads and products above, gained nothing: 31 us against 37 to 38 for
-    // 1,536 x 2,048 x 1,792 in bf16 with rows off 16 bytes.)
-    u4 vp[OpP::kEach], vq[OpQ::kEach];
+    // Through registers: kDeep steps on their way, two in LDS.  (One on its way costs a
+    // memory latency, 0.8 us, per step: MEASURED.)  A tile of 256 x 256 has the registers
+    // for one.
+    constexpr int kDeep = TI * TJ >= 32 ? 1 : TI * TJ >= 16 ? 2 : 3;
+    u4 vp[kDeep][OpP::kEach], vq[kDeep][OpQ::kEach];
     const int64_t p_extent = PKC ? a.K : a.I, q_extent = QKC ? a.K : a.J;
-    auto load = [&](int32_t s) __attribute__((always_inline)) {
+    const int32_t full = (k1 - k0) / kStep;
+    auto load = [&](int32_t s, int d) __attribute__((always_inline)) {
       const int32_t k = k0 + s * kStep;
-      if (k + kStep <= k1) {
-        p.template load<false>(k, k1, p_extent, vp);
-        q.template load<false>(k, k1, q_extent, vq);
+      if (s < full) {
+        p.template load<false>(k, k1, p_extent, vp[d]);
+        q.template load<false>(k, k1, q_extent, vq[d]);
       } else {
-        p.template load<true>(k, k1, p_extent, vp);
-        q.template load<true>(k, k1, q_extent, vq);
+        p.template load<true>(k, k1, p_extent, vp[d]);
+        q.template load<true>(k, k1, q_extent, vq[d]);
       }
     };
-    load(t);
-    for (int slot = 0; t < steps; ++t, slot ^= 1) {
-      p.store(lds + slot * kStage, p_extent, vp);
-      q.store(lds + slot * kStage + OpP::kBytes, q_extent, vq);
+    auto load_plain = [&](int32_t s, int d) __attribute__((always_inline)) {
+      p.load_plain(k0 + s * kStep, vp[d]);
+      q.load_plain(k0 + s * kStep, vq[d]);
+    };
+    int slot = 0;
+    auto put = [&](int d) __attribute__((always_inline)) {
+      p.store(lds + slot * kStage, p_extent, vp[d]);
+      q.store(lds + slot * kStage + OpP::kBytes, q_extent, vq[d]);
       arrive_lds();
-      if (t + 1 < steps) load(t + 1);
+    };
+    auto multiply = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         read(f[0], slot, h);
 #pragma unroll
         for (int x = 0; x < TI; ++x) multiply_row(f[0], x);
+      }
+      slot ^= 1;
+      ++t;
+    };
+    if (kDeep > 1 && full - t >= 2 * kDeep && (PKC || p_extent >= 8) && (QKC || q_extent >= 8)) {
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d) load_plain(t + d, d);
+      do {
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d) {
+          put(d);
+          load_plain(t + kDeep, d);
+          multiply();
+        }
+      } while (t + 2 * kDeep <= full);
+    } else {
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d)
+        if (t + d < steps) load(t + d, d);
+    }
+    while (t < steps) {
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d) {
+        if (t >= steps) break;
+        put(d);
+        if (t + kDeep < steps) load(t + kDeep, d);
+        multiply();
       }
     }
   }
