@@ -14,7 +14,6 @@ typedef _Float16 f16;
 
 inline int dtype_bytes(int t) { return t == kF32 ? 4 : t == kE4M3 ? 1 : 2; }
 
-// Eight consecutive elements at any address an element may have.
 // A launch holds fewer than 2^32 threads along x: more than 2^21 workgroups (of up to
 // 1,024) lie in several rows of the grid.  The last row may be longer than the work.
 inline dim3 groups_grid(int64_t n) {
@@ -25,6 +24,7 @@ __device__ __forceinline__ int64_t group_index() {
   return static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
 }
 
+// Eight consecutive elements at any address an element may have.
 template <typename T>
 struct Eight {
   typedef T vec __attribute__((ext_vector_type(8)));
