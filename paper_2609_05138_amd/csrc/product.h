@@ -166,6 +166,9 @@ __device__ __forceinline__ float act_grad(int act, float v) {
       return fmaf(v * e, 0.39894228040143268f, below);
     }
     case kActGeluTanh: {
+      // far out s (1 - s) is exactly 0 in fp32, and v^2 must not overflow to 0 times
+      // infinity (bf16 goes up to 3.4e38); NaN stays NaN
+      v = v > 1e4f ? 1e4f : v < -1e4f ? -1e4f : v;
       const float s = sigmoid(kGeluK * (v + kGeluC * v * v * v));
       return s + v * s * (1.0f - s) * kGeluK * (1.0f + 3.0f * kGeluC * v * v);
     }

@@ -529,3 +529,13 @@ def test_the_binding_refuses():
                  lambda: som.som_product(x, W, y=torch.empty((4, 32), dtype=torch.float16, device=DEV))):
         with pytest.raises(som.SomError):
             call()
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_gradients_of_activations_far_out(act):
+    """At arguments whose square overflows fp32 the derivative is 0 or 1, not a NaN."""
+    pre = torch.tensor([[-3e38, -1e30, -1e20, -1e10, 1e10, 1e20, 1e30, 3e38]], dtype=torch.bfloat16, device=DEV)
+    dy, W = torch.ones_like(pre), torch.eye(8, dtype=torch.bfloat16, device=DEV)
+    dx, dW, dbias = som.som_product_backward(dy, torch.ones_like(pre), W, act=act, pre=pre)
+    want = torch.tensor([[0.0] * 4 + [1.0] * 4], device=DEV)
+    assert torch.equal(dx.float(), want) and torch.equal(dbias, want[0]) and torch.equal(dW.float(), want.expand(8, 8))
