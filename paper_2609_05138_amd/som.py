@@ -735,12 +735,29 @@ def _weights(W: torch.Tensor, name: str, dtype):
     return p, ld, int(units)
 
 
-def _scratch(ws, need: int, device):
-    """(tensor, pointer, bytes) of the workspace: the caller's, or one for this call."""
+def _new(shape, dtype, device, stream):
+    """An output.  On a stream that is not the current one it is that stream's memory
+    (nothing earlier on the current one can still use it), which is not handed out
+    again before the current stream, whose caller has it, is done with it either."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _scratch(ws, need: int, device, stream):
+    """(tensor, pointer, bytes) of the workspace: the caller's, or one for this call, of
+    the memory of the stream that uses it: it is free for that stream's next call only."""
     if ws is None:
         if need == 0:
             return None, None, 0
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        if stream is None:
+            ws = torch.empty(need, dtype=torch.uint8, device=device)
+        else:
+            with torch.cuda.stream(stream):
+                ws = torch.empty(need, dtype=torch.uint8, device=device)
     else:
         _dev(ws, torch.uint8, "ws")
     return ws, ws.data_ptr(), ws.numel()
@@ -765,13 +782,13 @@ def som_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: fl
     wp = _vector(weight, "weight", cols, x.dtype)
     yt = torch.float8_e4m3fn if q8 else x.dtype
     if y is None:
-        y = torch.empty(shape, dtype=yt, device=x.device)
+        y = _new(shape, yt, x.device, stream)
     yp, ldy = _rows(y, "y", yt, shape)
     if h is None and residual is not None:
-        h = torch.empty(shape, dtype=x.dtype, device=x.device)
+        h = _new(shape, x.dtype, x.device, stream)
     hp, ldh = (None, 0) if h is None else _rows(h, "h", x.dtype, shape)
     if q8 and scale is None:
-        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+        scale = _new(rows, torch.float32, x.device, stream)
     if scale is not None and not q8:
         raise ValueError("scale goes with q8")
     sp = _vector(scale, "scale", rows)
@@ -795,12 +812,12 @@ def som_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[to
     wp = _vector(weight, "weight", cols, h.dtype)
     ep, lde = (None, 0) if dh is None else _rows(dh, "dh", h.dtype, shape)
     if dx is None:
-        dx = torch.empty(shape, dtype=h.dtype, device=h.device)
+        dx = _new(shape, h.dtype, h.device, stream)
     xp, ldx = _rows(dx, "dx", h.dtype, shape)
     if dweight is None:
-        dweight = torch.empty(cols, dtype=torch.float32, device=h.device)
+        dweight = _new(cols, torch.float32, h.device, stream)
     dwp = _vector(dweight, "dweight", cols)
-    ws, wsp, n = _scratch(ws, lib.som_rms_norm_backward_workspace_bytes(rows, cols), h.device)
+    ws, wsp, n = _scratch(ws, lib.som_rms_norm_backward_workspace_bytes(rows, cols), h.device, stream)
     _check(lib.som_rms_norm_backward(gp, ldg, hp, ldh, wp, ep, lde, dt, rows, cols, eps, xp, ldx, dwp, wsp, n,
                                      _stream_of(h, stream)))
     return dx, dweight
@@ -836,7 +853,7 @@ def som_product(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
         raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}")
     shape = (M, N)
     if y is None:
-        y = torch.empty(shape, dtype=dtype or (torch.bfloat16 if xt == 3 else x.dtype), device=x.device)
+        y = _new(shape, dtype or (torch.bfloat16 if xt == 3 else x.dtype), x.device, stream)
     elif dtype is not None and y.dtype != dtype:
         raise TypeError(f"y must be {dtype} (got {y.dtype})")
     yt = _float_type(y, "y", _FLOATS)
@@ -845,7 +862,7 @@ def som_product(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
     pp, ldp = (None, 0) if pre is None else _rows(pre, "pre", y.dtype, shape)
     e = som_epilogue(ACTIVATIONS[act], 0, alpha, _vector(x_scale, "x_scale", M), _vector(w_scale, "w_scale", N),
                      _vector(bias, "bias", N), rp, ldr, pp, ldp)
-    ws, wsp, n = _scratch(ws, lib.som_product_workspace_bytes(M, N, K, xt), x.device)
+    ws, wsp, n = _scratch(ws, lib.som_product_workspace_bytes(M, N, K, xt), x.device, stream)
     _check(lib.som_product(xp, ldx, Wp, ldw, units, xt, M, N, K, yp, ldy, yt, ctypes.byref(e), wsp, n,
                            _stream_of(x, stream)))
     return y
@@ -877,16 +894,15 @@ def som_product_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, act
         raise ValueError("pre is needed for an activation's gradient")
     pp, ldp = (None, 0) if pre is None else _rows(pre, "pre", x.dtype, (M, N))
     if dx is None:
-        dx = torch.empty((M, K), dtype=x.dtype, device=x.device)
+        dx = _new((M, K), x.dtype, x.device, stream)
     dxp, lddx = _rows(dx, "dx", x.dtype, (M, K))
     if dW is None:
-        dW = torch.empty((N, K), dtype=x.dtype, device=x.device).t() if units else \
-            torch.empty((K, N), dtype=x.dtype, device=x.device)
+        dW = _new((N, K), x.dtype, x.device, stream).t() if units else _new((K, N), x.dtype, x.device, stream)
     dWp, lddw = _rows(dW.t() if units else dW, "dW", x.dtype, (N, K) if units else (K, N))
     if dbias is None:
-        dbias = torch.empty(N, dtype=torch.float32, device=x.device)
+        dbias = _new(N, torch.float32, x.device, stream)
     dbp = _vector(dbias, "dbias", N)
-    ws, wsp, n = _scratch(ws, lib.som_product_backward_workspace_bytes(M, N, K, dt), x.device)
+    ws, wsp, n = _scratch(ws, lib.som_product_backward_workspace_bytes(M, N, K, dt), x.device, stream)
     _check(lib.som_product_backward(gp, ldg, xp, ldx, Wp, ldw, units, dt, M, N, K, ACTIVATIONS[act], pp, ldp, alpha,
                                     dxp, lddx, dWp, lddw, dbp, wsp, n, _stream_of(x, stream)))
     return dx, dW, dbias
@@ -906,7 +922,7 @@ def som_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual:
         raise ValueError("seed and offset must be in [0, 2^64)")
     rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", x.dtype, shape)
     if y is None:
-        y = torch.empty(shape, dtype=x.dtype, device=x.device)
+        y = _new(shape, x.dtype, x.device, stream)
     yp, ldy = _rows(y, "y", x.dtype, shape)
     _check(lib.som_dropout(xp, ldx, rp, ldr, dt, rows, cols, p, seed, offset, yp, ldy, _stream_of(x, stream)))
     return y

@@ -539,3 +539,31 @@ def test_gradients_of_activations_far_out(act):
     dx, dW, dbias = som.som_product_backward(dy, torch.ones_like(pre), W, act=act, pre=pre)
     want = torch.tensor([[0.0] * 4 + [1.0] * 4], device=DEV)
     assert torch.equal(dx.float(), want) and torch.equal(dbias, want[0]) and torch.equal(dW.float(), want.expand(8, 8))
+
+
+def test_memory_of_a_call_is_that_of_its_stream(monkeypatch):
+    """With stream= the workspace that a call makes for itself, free again at its return,
+    is not handed out on the current stream while the call may still use it, and nor is
+    an output that the caller drops."""
+    scratch, seen = som.som._scratch, []
+
+    def keep(*args):
+        made = scratch(*args)
+        seen.append((made[1], made[2]))
+        return made
+
+    monkeypatch.setattr(som.som, "_scratch", keep)
+    x = torch.randn((40, 8192), device=DEV).to(torch.float16)
+    W = torch.randn((8192, 640), device=DEV).to(torch.float16)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream(device=DEV)
+    y = som.som_product(x, W, stream=side)
+    (place, size), = seen
+    assert size > 0
+    out = y.data_ptr()
+    del y
+    others = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in (size, 40 * 640 * 2) for _ in range(4)]
+    assert not {t.data_ptr() for t in others} & {place, out}
+    y = som.som_product(x, W, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(y, som.som_product(x, W))
