@@ -238,7 +238,10 @@ __global__ void __launch_bounds__(G* R) k_rms_norm_back(const RmsNormBackArgs a,
         ss = fmaf(h, h, ss);
         gh = fmaf(a.weight ? d * static_cast<float>(w[u][e]) : d, h, gh);
       }
-    const float s = rsqrtf(group_sum<G>(ss, part) / static_cast<float>(a.cols) + a.eps);
+    // (a group past the last row has zeros: without eps its s would be infinite, and infinity
+    // times zero would go into every column's sum)
+    const float ms = group_sum<G>(ss, part) / static_cast<float>(a.cols) + a.eps;
+    const float s = row < a.rows ? rsqrtf(ms) : 0.0f;
     const float k = group_sum<G>(gh, part2) / static_cast<float>(a.cols) * s * s;   // times s h: the projection
 #pragma unroll
     for (int u = 0; u < U; ++u) {
