@@ -229,7 +229,9 @@ __global__ void __launch_bounds__(G* R) k_rms_norm_back(const RmsNormBackArgs a,
     const int64_t row = first + r;
     const Row now = next;
     if (AHEAD) get(row + step, next);    // on its way while this row's sums are made
-    float ss = 0.0f, gh = 0.0f;
+    // a group past the last row has zeros: without eps its s would be infinite, and infinity
+    // times zero would go into every column's sum
+    float ss = R == 1 || row < a.rows ? 0.0f : 1.0f, gh = 0.0f;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -238,10 +240,7 @@ __global__ void __launch_bounds__(G* R) k_rms_norm_back(const RmsNormBackArgs a,
         ss = fmaf(h, h, ss);
         gh = fmaf(a.weight ? d * static_cast<float>(w[u][e]) : d, h, gh);
       }
-    // (a group past the last row has zeros: without eps its s would be infinite, and infinity
-    // times zero would go into every column's sum)
-    const float ms = group_sum<G>(ss, part) / static_cast<float>(a.cols) + a.eps;
-    const float s = row < a.rows ? rsqrtf(ms) : 0.0f;
+    const float s = rsqrtf(group_sum<G>(ss, part) / static_cast<float>(a.cols) + a.eps);
     const float k = group_sum<G>(gh, part2) / static_cast<float>(a.cols) * s * s;   // times s h: the projection
 #pragma unroll
     for (int u = 0; u < U; ++u) {
