@@ -23,7 +23,8 @@ def rms_norm_backward(dy, h, weight=None, eps=0.0, dh=None):
     return (dx if dh is None else dx + dh), (dy * h * s).sum(axis=0)
 
 
-_erf = np.vectorize(math.erf, otypes=[np.float64])
+# (erfc, and not 1 + erf, which loses the digits of a small share)
+_below = np.vectorize(lambda v: 0.5 * math.erfc(-v / math.sqrt(2.0)), otypes=[np.float64])
 
 
 def activation(name, v):
@@ -32,7 +33,7 @@ def activation(name, v):
     if name == "relu":
         return np.maximum(v, 0.0)
     if name == "gelu":
-        return 0.5 * v * (1.0 + _erf(v / math.sqrt(2.0)))
+        return v * _below(v)
     if name == "gelu_tanh":
         return 0.5 * v * (1.0 + np.tanh(math.sqrt(2.0 / math.pi) * (v + 0.044715 * v ** 3)))
     if name == "silu":
@@ -46,7 +47,7 @@ def activation_grad(name, v):
     if name == "relu":
         return (v > 0).astype(np.float64)
     if name == "gelu":
-        return 0.5 * (1.0 + _erf(v / math.sqrt(2.0))) + v * np.exp(-0.5 * v * v) / math.sqrt(2.0 * math.pi)
+        return _below(v) + v * np.exp(-0.5 * v * v) / math.sqrt(2.0 * math.pi)
     if name == "gelu_tanh":
         t = np.tanh(math.sqrt(2.0 / math.pi) * (v + 0.044715 * v ** 3))
         return 0.5 * (1.0 + t) + 0.5 * v * (1.0 - t * t) * math.sqrt(2.0 / math.pi) * (1.0 + 3 * 0.044715 * v * v)

@@ -113,7 +113,8 @@ constexpr int kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSi
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// 1 / (1 + e^-z), within a few units of fp32; e^-z = infinity gives 0.
+// 1 / (1 + e^-z), within (8 + 2 |z|) 2^-24 of itself for z < 0 (the exponent's roundings), a few
+// units of fp32 for z >= 0; 0 where it is below fp32's normal numbers (z < -87).
 __device__ __forceinline__ float sigmoid(float z) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * z));
 }
@@ -121,19 +122,23 @@ __device__ __forceinline__ float sigmoid(float z) {
 constexpr float kGeluK = 1.5957691216057308f;     // 2 sqrt(2 / pi): 1 + tanh(z) = 2 sigmoid(2 z)
 constexpr float kGeluC = 0.044715f;
 
-// The normal distribution's share below v, and e^(-v^2 / 2): erfc by the rational
-// approximation 7.1.26 of Abramowitz and Stegun (Handbook of Mathematical Functions),
-// within 1.5e-7; the small side is calculated and the large one is its complement, so a
-// negative v does not lose digits.
-__device__ __forceinline__ float normal_below(float v, float* e) {
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(v), 1.0f));
-  float s = fmaf(t, 1.061405429f, -1.453152027f);
-  s = fmaf(t, s, 1.421413741f);
-  s = fmaf(t, s, -0.284496736f);
-  s = fmaf(t, s, 0.254829592f);
+// The normal distribution's share below -|v|, and e = e^(-v^2 / 2): e t q(t) with t =
+// 1 / (1 + 0.3 |v|).  q is the polynomial of degree 7 with the least largest relative error over
+// |v| <= 14 (1.5e-7; fitted to the scaled complementary error function, 4.5e-7 as calculated in
+// fp32), so no digits are lost far out.  e is within 1.5 v^2 2^-24 of itself (its exponent's
+// roundings), the share within 2^-20 + 1.5 v^2 2^-24 of itself until it leaves fp32's normal
+// numbers at -13.  `size`: |v|, or anything from 16 on where that is more.
+__device__ __forceinline__ float normal_tail(float v, float size, float* e) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3f, size, 1.0f));
+  float q = fmaf(t, 0.0356747732f, -0.157203078f);
+  q = fmaf(t, q, 0.2063535f);
+  q = fmaf(t, q, -0.0536836423f);
+  q = fmaf(t, q, 0.128561631f);
+  q = fmaf(t, q, 0.0999134928f);
+  q = fmaf(t, q, 0.120753959f);
+  q = fmaf(t, q, 0.119629301f);
   *e = __builtin_amdgcn_exp2f(-0.5f * kLog2e * v * v);
-  const float tail = 0.5f * t * s * *e;
-  return v >= 0.0f ? 1.0f - tail : tail;
+  return t * q * *e;
 }
 
 __device__ __forceinline__ void act8(int act, float (&v)[8]) {
@@ -144,8 +149,11 @@ __device__ __forceinline__ void act8(int act, float (&v)[8]) {
   } else if (act == kActGelu) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
+      // v minus |v| times the share above v, or v times the share below; from 16 on the tail
+      // is zero, which infinity must not meet (a NaN is one in the exponential)
       float exponential;
-      v[e] *= normal_below(v[e], &exponential);
+      const float size = fminf(fabsf(v[e]), 16.0f), tail = normal_tail(v[e], size, &exponential);
+      v[e] = fmaf(-size, tail, fmaxf(v[e], 0.0f));
     }
   } else {
     // gelu_tanh: v sigmoid(k (v + c v^3)); silu: v sigmoid(v)
@@ -162,7 +170,7 @@ __device__ __forceinline__ float act_grad(int act, float v) {
       return v > 0.0f ? 1.0f : 0.0f;
     case kActGelu: {
       float e;
-      const float below = normal_below(v, &e);
+      const float tail = normal_tail(v, fabsf(v), &e), below = v >= 0.0f ? 1.0f - tail : tail;
       return fmaf(v * e, 0.39894228040143268f, below);
     }
     case kActGeluTanh: {
