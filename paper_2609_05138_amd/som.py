@@ -660,15 +660,20 @@ def som_probe_lds(iters: int, sink: torch.Tensor, stream=None) -> int:
 
 
 # ---------------------------------------------------------------------------
-# Dense documents
+# Dense documents.  All tensors of a call are on one device, and it runs there, whichever
+# device is the current one.
 # ---------------------------------------------------------------------------
 
-def _rows(t: torch.Tensor, name: str, dtype=None, shape=None):
-    """Check a matrix of contiguous rows; return its pointer and row stride."""
+def _rows(t: torch.Tensor, name: str, dtype=None, shape=None, device=None):
+    """Check a matrix of contiguous rows (device: the index of the first tensor's; None: this is
+    it); return its pointer and row stride."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be on a ROCm device (got {t.device})")
+    if device is None:
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be on a ROCm device (got {t.device})")
+    elif t.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device} like the first tensor (got {t.device})")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
     size = t.shape
@@ -687,21 +692,34 @@ def _rows(t: torch.Tensor, name: str, dtype=None, shape=None):
     return t.data_ptr(), ld
 
 
-def _stream_of(t: torch.Tensor, stream) -> int:
-    """The given stream, or the current one of the tensor's device (asked for by
-    itself: torch.cuda.current_stream() takes longer than a launch)."""
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(t.get_device())
-    return stream.cuda_stream
+def _device_of(t: torch.Tensor, stream) -> int:
+    """The index of the device that a call on t works on; the given stream has to be its."""
+    device = t.get_device()
+    if stream is not None and getattr(stream, "device_index", device) != device:
+        raise ValueError(f"stream must be one of cuda:{device}, like the tensors (got cuda:{stream.device_index})")
+    return device
 
 
-def _vector(t: Optional[torch.Tensor], name: str, n: int, dtype=torch.float32):
+def _launch(fn, device: int, stream, *args) -> None:
+    """Call an entry point with the given stream, or the device's current one (asked for by
+    itself: torch.cuda.current_stream() takes longer than a launch).  A launch goes to the
+    current device, so the tensors' is made that where it is another."""
+    raw = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    if torch._C._cuda_getDevice() == device:
+        status = fn(*args, raw)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, raw)
+    _check(status)
+
+
+def _vector(t: Optional[torch.Tensor], name: str, n: int, device: int, dtype=torch.float32):
     if t is None:
         return None
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be on a ROCm device (got {t.device})")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device} like the first tensor (got {t.device})")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
     if t.numel() != n or not t.is_contiguous():
@@ -721,7 +739,7 @@ _FLOATS = (torch.float32, torch.float16, torch.bfloat16)
 _HALVES = (torch.float16, torch.bfloat16)
 
 
-def _weights(W: torch.Tensor, name: str, dtype):
+def _weights(W: torch.Tensor, name: str, dtype, device: int):
     """A K x N weight matrix: (pointer, row stride, 1 if unit-major).
 
     Feature-major rows (W[k, :] contiguous, like a codebook) or, as the
@@ -731,7 +749,7 @@ def _weights(W: torch.Tensor, name: str, dtype):
     if W.dim() != 2:
         raise ValueError(f"{name} must have two dimensions")
     units = W.stride(0) == 1 and (W.stride(1) != 1 or dtype == torch.float8_e4m3fn)
-    p, ld = _rows(W.t() if units else W, name, dtype)
+    p, ld = _rows(W.t() if units else W, name, dtype, None, device)
     return p, ld, int(units)
 
 
@@ -760,6 +778,8 @@ def _scratch(ws, need: int, device, stream):
                 ws = torch.empty(need, dtype=torch.uint8, device=device)
     else:
         _dev(ws, torch.uint8, "ws")
+        if ws.device != device:
+            raise ValueError(f"ws must be on {device} like the first tensor (got {ws.device})")
     return ws, ws.data_ptr(), ws.numel()
 
 
@@ -776,24 +796,25 @@ def som_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: fl
     lib = load()
     dt = _float_type(x, "x", _FLOATS)
     xp, ldx = _rows(x, "x")
+    device = _device_of(x, stream)
     rows, cols = x.shape
     shape = x.shape
-    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", x.dtype, shape)
-    wp = _vector(weight, "weight", cols, x.dtype)
+    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", x.dtype, shape, device)
+    wp = _vector(weight, "weight", cols, device, x.dtype)
     yt = torch.float8_e4m3fn if q8 else x.dtype
     if y is None:
         y = _new(shape, yt, x.device, stream)
-    yp, ldy = _rows(y, "y", yt, shape)
+    yp, ldy = _rows(y, "y", yt, shape, device)
     if h is None and residual is not None:
         h = _new(shape, x.dtype, x.device, stream)
-    hp, ldh = (None, 0) if h is None else _rows(h, "h", x.dtype, shape)
+    hp, ldh = (None, 0) if h is None else _rows(h, "h", x.dtype, shape, device)
     if q8 and scale is None:
         scale = _new(rows, torch.float32, x.device, stream)
     if scale is not None and not q8:
         raise ValueError("scale goes with q8")
-    sp = _vector(scale, "scale", rows)
-    _check(lib.som_rms_norm(xp, ldx, rp, ldr, wp, dt, rows, cols, eps, 1 if q8 else 0, yp, ldy, hp, ldh, sp,
-                            _stream_of(x, stream)))
+    sp = _vector(scale, "scale", rows, device)
+    _launch(lib.som_rms_norm, device, stream, xp, ldx, rp, ldr, wp, dt, rows, cols, eps, 1 if q8 else 0, yp, ldy, hp,
+            ldh, sp)
     return y, h, scale
 
 
@@ -806,20 +827,21 @@ def som_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[to
     lib = load()
     dt = _float_type(h, "h", _FLOATS)
     hp, ldh = _rows(h, "h")
+    device = _device_of(h, stream)
     rows, cols = h.shape
     shape = (rows, cols)
-    gp, ldg = _rows(dy, "dy", h.dtype, shape)
-    wp = _vector(weight, "weight", cols, h.dtype)
-    ep, lde = (None, 0) if dh is None else _rows(dh, "dh", h.dtype, shape)
+    gp, ldg = _rows(dy, "dy", h.dtype, shape, device)
+    wp = _vector(weight, "weight", cols, device, h.dtype)
+    ep, lde = (None, 0) if dh is None else _rows(dh, "dh", h.dtype, shape, device)
     if dx is None:
         dx = _new(shape, h.dtype, h.device, stream)
-    xp, ldx = _rows(dx, "dx", h.dtype, shape)
+    xp, ldx = _rows(dx, "dx", h.dtype, shape, device)
     if dweight is None:
         dweight = _new(cols, torch.float32, h.device, stream)
-    dwp = _vector(dweight, "dweight", cols)
+    dwp = _vector(dweight, "dweight", cols, device)
     ws, wsp, n = _scratch(ws, lib.som_rms_norm_backward_workspace_bytes(rows, cols), h.device, stream)
-    _check(lib.som_rms_norm_backward(gp, ldg, hp, ldh, wp, ep, lde, dt, rows, cols, eps, xp, ldx, dwp, wsp, n,
-                                     _stream_of(h, stream)))
+    _launch(lib.som_rms_norm_backward, device, stream, gp, ldg, hp, ldh, wp, ep, lde, dt, rows, cols, eps, xp, ldx, dwp,
+            wsp, n)
     return dx, dweight
 
 
@@ -844,8 +866,9 @@ def som_product(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
     lib = load()
     xt = _float_type(x, "x", (*_HALVES, torch.float8_e4m3fn))
     xp, ldx = _rows(x, "x")
+    device = _device_of(x, stream)
     M, K = x.shape
-    Wp, ldw, units = _weights(W, "W", x.dtype)
+    Wp, ldw, units = _weights(W, "W", x.dtype, device)
     if W.shape[0] != K:
         raise ValueError(f"x has {K} columns and W {W.shape[0]} rows")
     N = W.shape[1]
@@ -857,14 +880,13 @@ def som_product(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
     elif dtype is not None and y.dtype != dtype:
         raise TypeError(f"y must be {dtype} (got {y.dtype})")
     yt = _float_type(y, "y", _FLOATS)
-    yp, ldy = _rows(y, "y", None, shape)
-    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", y.dtype, shape)
-    pp, ldp = (None, 0) if pre is None else _rows(pre, "pre", y.dtype, shape)
-    e = som_epilogue(ACTIVATIONS[act], 0, alpha, _vector(x_scale, "x_scale", M), _vector(w_scale, "w_scale", N),
-                     _vector(bias, "bias", N), rp, ldr, pp, ldp)
+    yp, ldy = _rows(y, "y", None, shape, device)
+    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", y.dtype, shape, device)
+    pp, ldp = (None, 0) if pre is None else _rows(pre, "pre", y.dtype, shape, device)
+    e = som_epilogue(ACTIVATIONS[act], 0, alpha, _vector(x_scale, "x_scale", M, device),
+                     _vector(w_scale, "w_scale", N, device), _vector(bias, "bias", N, device), rp, ldr, pp, ldp)
     ws, wsp, n = _scratch(ws, lib.som_product_workspace_bytes(M, N, K, xt), x.device, stream)
-    _check(lib.som_product(xp, ldx, Wp, ldw, units, xt, M, N, K, yp, ldy, yt, ctypes.byref(e), wsp, n,
-                           _stream_of(x, stream)))
+    _launch(lib.som_product, device, stream, xp, ldx, Wp, ldw, units, xt, M, N, K, yp, ldy, yt, ctypes.byref(e), wsp, n)
     return y
 
 
@@ -882,29 +904,30 @@ def som_product_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, act
     lib = load()
     dt = _float_type(x, "x", _HALVES)
     xp, ldx = _rows(x, "x")
+    device = _device_of(x, stream)
     M, K = x.shape
-    Wp, ldw, units = _weights(W, "W", x.dtype)
+    Wp, ldw, units = _weights(W, "W", x.dtype, device)
     if W.shape[0] != K:
         raise ValueError(f"x has {K} columns and W {W.shape[0]} rows")
     N = W.shape[1]
-    gp, ldg = _rows(dy, "dy", x.dtype, (M, N))
+    gp, ldg = _rows(dy, "dy", x.dtype, (M, N), device)
     if act not in ACTIVATIONS:
         raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}")
     if pre is None and act != "none":
         raise ValueError("pre is needed for an activation's gradient")
-    pp, ldp = (None, 0) if pre is None else _rows(pre, "pre", x.dtype, (M, N))
+    pp, ldp = (None, 0) if pre is None else _rows(pre, "pre", x.dtype, (M, N), device)
     if dx is None:
         dx = _new((M, K), x.dtype, x.device, stream)
-    dxp, lddx = _rows(dx, "dx", x.dtype, (M, K))
+    dxp, lddx = _rows(dx, "dx", x.dtype, (M, K), device)
     if dW is None:
         dW = _new((N, K), x.dtype, x.device, stream).t() if units else _new((K, N), x.dtype, x.device, stream)
-    dWp, lddw = _rows(dW.t() if units else dW, "dW", x.dtype, (N, K) if units else (K, N))
+    dWp, lddw = _rows(dW.t() if units else dW, "dW", x.dtype, (N, K) if units else (K, N), device)
     if dbias is None:
         dbias = _new(N, torch.float32, x.device, stream)
-    dbp = _vector(dbias, "dbias", N)
+    dbp = _vector(dbias, "dbias", N, device)
     ws, wsp, n = _scratch(ws, lib.som_product_backward_workspace_bytes(M, N, K, dt), x.device, stream)
-    _check(lib.som_product_backward(gp, ldg, xp, ldx, Wp, ldw, units, dt, M, N, K, ACTIVATIONS[act], pp, ldp, alpha,
-                                    dxp, lddx, dWp, lddw, dbp, wsp, n, _stream_of(x, stream)))
+    _launch(lib.som_product_backward, device, stream, gp, ldg, xp, ldx, Wp, ldw, units, dt, M, N, K, ACTIVATIONS[act],
+            pp, ldp, alpha, dxp, lddx, dWp, lddw, dbp, wsp, n)
     return dx, dW, dbias
 
 
@@ -916,13 +939,14 @@ def som_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual:
     lib = load()
     dt = _float_type(x, "x", _FLOATS)
     xp, ldx = _rows(x, "x")
+    device = _device_of(x, stream)
     rows, cols = x.shape
     shape = (rows, cols)
     if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         raise ValueError("seed and offset must be in [0, 2^64)")
-    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", x.dtype, shape)
+    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", x.dtype, shape, device)
     if y is None:
         y = _new(shape, x.dtype, x.device, stream)
-    yp, ldy = _rows(y, "y", x.dtype, shape)
-    _check(lib.som_dropout(xp, ldx, rp, ldr, dt, rows, cols, p, seed, offset, yp, ldy, _stream_of(x, stream)))
+    yp, ldy = _rows(y, "y", x.dtype, shape, device)
+    _launch(lib.som_dropout, device, stream, xp, ldx, rp, ldr, dt, rows, cols, p, seed, offset, yp, ldy)
     return y
