@@ -783,6 +783,11 @@ def _scratch(ws, need: int, device, stream):
     return ws, ws.data_ptr(), ws.numel()
 
 
+def _unwanted(need: bool, given: Optional[torch.Tensor], name: str) -> None:
+    if not need and given is not None:
+        raise ValueError(f"{name} goes with need_{name}")
+
+
 def som_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
                  residual: Optional[torch.Tensor] = None, q8: bool = False, y: Optional[torch.Tensor] = None,
                  h: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, stream=None):
@@ -820,10 +825,12 @@ def som_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: fl
 
 def som_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
                           dh: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
-                          dweight: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+                          dweight: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None,
+                          need_dweight: bool = True):
     """(dx, dweight) of som_rms_norm: from the gradient of y, the h it returned (x
     without a residual) and the gradient ``dh`` that reaches h itself.  dx is the
-    gradient of x and of the residual; dweight is fp32."""
+    gradient of x and of the residual; dweight is fp32, or None (and not calculated)
+    without ``need_dweight``."""
     lib = load()
     dt = _float_type(h, "h", _FLOATS)
     hp, ldh = _rows(h, "h")
@@ -836,8 +843,9 @@ def som_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[to
     if dx is None:
         dx = _new(shape, h.dtype, h.device, stream)
     xp, ldx = _rows(dx, "dx", h.dtype, shape, device)
-    if dweight is None:
+    if need_dweight and dweight is None:
         dweight = _new(cols, torch.float32, h.device, stream)
+    _unwanted(need_dweight, dweight, "dweight")
     dwp = _vector(dweight, "dweight", cols, device)
     ws, wsp, n = _scratch(ws, lib.som_rms_norm_backward_workspace_bytes(rows, cols), h.device, stream)
     _launch(lib.som_rms_norm_backward, device, stream, gp, ldg, hp, ldh, wp, ep, lde, dt, rows, cols, eps, xp, ldx, dwp,
@@ -897,10 +905,12 @@ def som_product_backward_workspace_bytes(M: int, N: int, K: int, dtype=torch.bfl
 def som_product_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, act: str = "none",
                          pre: Optional[torch.Tensor] = None, alpha: float = 1.0, dx: Optional[torch.Tensor] = None,
                          dW: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
-                         ws: Optional[torch.Tensor] = None, stream=None):
+                         ws: Optional[torch.Tensor] = None, stream=None, need_dx: bool = True, need_dW: bool = True,
+                         need_dbias: bool = True):
     """(dx, dW, dbias) of som_product, in x's type (fp16 or bf16), dW laid out as W
     is; dbias is fp32.  ``pre`` is what som_product stored (not needed without an
-    activation).  The residual's gradient is dy."""
+    activation).  The residual's gradient is dy.  One that is not needed is None, and its
+    product or sum is left out."""
     lib = load()
     dt = _float_type(x, "x", _HALVES)
     xp, ldx = _rows(x, "x")
@@ -916,13 +926,16 @@ def som_product_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, act
     if pre is None and act != "none":
         raise ValueError("pre is needed for an activation's gradient")
     pp, ldp = (None, 0) if pre is None else _rows(pre, "pre", x.dtype, (M, N), device)
-    if dx is None:
+    for need, given, name in ((need_dx, dx, "dx"), (need_dW, dW, "dW"), (need_dbias, dbias, "dbias")):
+        _unwanted(need, given, name)
+    if need_dx and dx is None:
         dx = _new((M, K), x.dtype, x.device, stream)
-    dxp, lddx = _rows(dx, "dx", x.dtype, (M, K), device)
-    if dW is None:
+    dxp, lddx = (None, 0) if dx is None else _rows(dx, "dx", x.dtype, (M, K), device)
+    if need_dW and dW is None:
         dW = _new((N, K), x.dtype, x.device, stream).t() if units else _new((K, N), x.dtype, x.device, stream)
-    dWp, lddw = _rows(dW.t() if units else dW, "dW", x.dtype, (N, K) if units else (K, N), device)
-    if dbias is None:
+    dWp, lddw = (None, 0) if dW is None else _rows(dW.t() if units else dW, "dW", x.dtype,
+                                                   (N, K) if units else (K, N), device)
+    if need_dbias and dbias is None:
         dbias = _new(N, torch.float32, x.device, stream)
     dbp = _vector(dbias, "dbias", N, device)
     ws, wsp, n = _scratch(ws, lib.som_product_backward_workspace_bytes(M, N, K, dt), x.device, stream)
