@@ -77,14 +77,17 @@ constexpr int64_t kCus = 256;
 // Times in us that the choice of a tile shape goes by, measured on MI355X (bf16, replayed
 // graphs of 20 products): a workgroup's start, first step and epilogue; a step of 128
 // bytes of k alone on a CU, where up to half of the CUs and where all have one; and for two
-// workgroups on a CU.  8-bit steps hold twice the products; steps of rows off 16 bytes go
-// through registers.
+// workgroups on a CU.  8-bit steps hold twice the products.  Steps of rows off 16 bytes go
+// through registers: 1.3 to 1.8 times a step's time in the four wide shapes; in the narrow ones
+// 1.0 to 1.4 times, but their whole calls, whose weights the many tiles read again and again,
+// are priced right at 1.8 and 2.2 (at 1.4 70 x 5,001 x 3,000 went to 16 x 128, 25.0 us; 64 x
+// 128 in three splits takes 17.5).
 struct ShapeTime {
   double fixed, half, full, pair, e4m3, off;
 };
-constexpr ShapeTime kTime[kShapes] = {{11.0, 1.33, 1.50, 0, 1.8, 1.35},   {9.5, 0.58, 0.80, 0, 1.6, 1.6},
-                                      {4.4, 0.47, 0.52, 0, 1.4, 1.8},     {4.1, 0.29, 0.33, 0.64, 1.2, 2.6},
-                                      {3.4, 0.27, 0.28, 0.59, 1.1, 3.3}, {3.4, 0.20, 0.22, 0.45, 1.1, 4.5}};
+constexpr ShapeTime kTime[kShapes] = {{11.0, 1.33, 1.50, 0, 1.8, 1.5},   {9.5, 0.58, 0.80, 0, 1.6, 1.5},
+                                      {4.4, 0.47, 0.52, 0, 1.4, 1.5},     {4.1, 0.29, 0.33, 0.64, 1.2, 1.5},
+                                      {3.4, 0.27, 0.28, 0.59, 1.1, 1.8}, {3.4, 0.20, 0.22, 0.45, 1.1, 2.2}};
 // A split k axis: the second launch and its wait, and the parts' bytes per us.
 constexpr double kJoinTime = 4.5, kJoinBytes = 6.5e6;
 constexpr int64_t kMinSplitSteps = 4;
@@ -107,7 +110,10 @@ double product_time(int shape, int64_t n, int64_t steps, bool e4m3, bool dma) {
 // two splits 39.3), 4,096^3 (256 x 256, 107; 128 x 128 148), 3,000 x 1,000 x 3,000
 // (256 x 256, 33.0; 128 x 128 39.8), 512 x 1,024 x 4,096 (64 x 128, 9.5; 128 x 128 11.8),
 // 128 x 4,096 x 4,096 (64 x 128 in four splits, 16.0; unsplit 22.6), 37 x 8,192 x 2,048
-// (32 x 128 in eight splits, 12.7; 64 x 128 12.9).
+// (32 x 128 in eight splits, 12.7; 64 x 128 12.9).  With rows off 16 bytes, 38 sizes from 6 x
+// 3,001 x 4,099 to 4,001 x 3,999 x 4,001 in each layout and in 8 bits: 1% off the best in the
+// mean, 15% at the most (2,001 x 1,001 x 2,003 64 x 128, 24.3; 128 x 128 in two splits 29.4.
+// 333 x 1,023 x 5,001 64 x 128 in four splits, 20.2; 128 x 128 in eight 21.9).
 //
 // Few rows: with k contiguous in both up to four take the vector kernel (4,096 x 4,096:
 // one row 5.8 us, two 7.4, four 10.1; in 16 x 128 tiles and eight splits 9.0, in two

@@ -24,7 +24,7 @@ PRODUCTS_8 = {
     (4001, 3999, 700): ("256x256", "256x256"),
     (2500, 2500, 900): ("256x128", "256x128"),
     (2048, 2048, 2000): ("128x128", "128x128"),
-    (3000, 3008, 1000): ("64x128", "256x256"),
+    (3000, 3008, 1000): ("64x128", "64x128"),
 }
 # (M, N, K): the tiles of dx [M x K] and dW [K x N or N x K]
 GRADIENTS = {

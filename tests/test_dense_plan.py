@@ -38,3 +38,19 @@ def test_the_gradients_take_the_large_tiles(lib):
                 rows, cols = (N, K) if units else (K, N)
                 if dW:
                     assert tile(lib, rows, cols, M, BF16, False, False, on16) == dW, (M, N, K, units, on16)
+
+
+# rows off 16 bytes, k contiguous in both: the best of all tiles by measured times (us: this one,
+# and the one that a step through registers priced at twice and more of its time led to)
+RAGGED = {
+    (2001, 1001, 2003): "64x128",     # 24.3; 128x128 in two splits 29.4
+    (129, 4097, 1025): "64x128",      # 13.0 (32x128 12.4); 128x128 in three splits 16.5
+    (333, 1023, 5001): "64x128",      # 20.2; 128x128 in eight splits 21.9
+    (200, 1000, 10001): "64x128",     # 20.1; 128x128 in sixteen splits 22.1
+    (4001, 3999, 4001): "256x256",
+}
+
+
+def test_rows_off_16_bytes_take_the_best_tiles(lib):
+    for (M, N, K), want in RAGGED.items():
+        assert tile(lib, M, N, K, BF16, True, True, False) == want, (M, N, K)
