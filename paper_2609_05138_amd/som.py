@@ -692,25 +692,14 @@ def _rows(t: torch.Tensor, name: str, dtype=None, shape=None, device=None):
     return t.data_ptr(), ld
 
 
-def _device_of(t: torch.Tensor, stream) -> int:
-    """The index of the device that a call on t works on; the given stream has to be its."""
-    device = t.get_device()
-    if stream is not None and getattr(stream, "device_index", device) != device:
+def _raw_stream(device: int, stream) -> int:
+    """The given stream, which has to be the device's, or its current one (asked for by
+    itself: torch.cuda.current_stream() takes longer than a launch)."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    if getattr(stream, "device_index", device) != device:
         raise ValueError(f"stream must be one of cuda:{device}, like the tensors (got cuda:{stream.device_index})")
-    return device
-
-
-def _launch(fn, device: int, stream, *args) -> None:
-    """Call an entry point with the given stream, or the device's current one (asked for by
-    itself: torch.cuda.current_stream() takes longer than a launch).  A launch goes to the
-    current device, so the tensors' is made that where it is another."""
-    raw = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
-    if torch._C._cuda_getDevice() == device:
-        status = fn(*args, raw)
-    else:
-        with torch.cuda.device(device):
-            status = fn(*args, raw)
-    _check(status)
+    return stream.cuda_stream
 
 
 def _vector(t: Optional[torch.Tensor], name: str, n: int, device: int, dtype=torch.float32):
@@ -801,7 +790,10 @@ def som_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: fl
     lib = load()
     dt = _float_type(x, "x", _FLOATS)
     xp, ldx = _rows(x, "x")
-    device = _device_of(x, stream)
+    device = x.get_device()
+    if torch._C._cuda_getDevice() != device:       # a launch goes to the current one
+        with torch.cuda.device(device):
+            return som_rms_norm(x, weight, eps, residual, q8, y, h, scale, stream)
     rows, cols = x.shape
     shape = x.shape
     rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", x.dtype, shape, device)
@@ -818,8 +810,8 @@ def som_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: fl
     if scale is not None and not q8:
         raise ValueError("scale goes with q8")
     sp = _vector(scale, "scale", rows, device)
-    _launch(lib.som_rms_norm, device, stream, xp, ldx, rp, ldr, wp, dt, rows, cols, eps, 1 if q8 else 0, yp, ldy, hp,
-            ldh, sp)
+    _check(lib.som_rms_norm(xp, ldx, rp, ldr, wp, dt, rows, cols, eps, 1 if q8 else 0, yp, ldy, hp, ldh, sp,
+                            _raw_stream(device, stream)))
     return y, h, scale
 
 
@@ -834,7 +826,10 @@ def som_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[to
     lib = load()
     dt = _float_type(h, "h", _FLOATS)
     hp, ldh = _rows(h, "h")
-    device = _device_of(h, stream)
+    device = h.get_device()
+    if torch._C._cuda_getDevice() != device:       # a launch goes to the current one
+        with torch.cuda.device(device):
+            return som_rms_norm_backward(dy, h, weight, eps, dh, dx, dweight, ws, stream, need_dweight)
     rows, cols = h.shape
     shape = (rows, cols)
     gp, ldg = _rows(dy, "dy", h.dtype, shape, device)
@@ -848,8 +843,8 @@ def som_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[to
     _unwanted(need_dweight, dweight, "dweight")
     dwp = _vector(dweight, "dweight", cols, device)
     ws, wsp, n = _scratch(ws, lib.som_rms_norm_backward_workspace_bytes(rows, cols), h.device, stream)
-    _launch(lib.som_rms_norm_backward, device, stream, gp, ldg, hp, ldh, wp, ep, lde, dt, rows, cols, eps, xp, ldx, dwp,
-            wsp, n)
+    _check(lib.som_rms_norm_backward(gp, ldg, hp, ldh, wp, ep, lde, dt, rows, cols, eps, xp, ldx, dwp, wsp, n,
+                                     _raw_stream(device, stream)))
     return dx, dweight
 
 
@@ -874,7 +869,10 @@ def som_product(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
     lib = load()
     xt = _float_type(x, "x", (*_HALVES, torch.float8_e4m3fn))
     xp, ldx = _rows(x, "x")
-    device = _device_of(x, stream)
+    device = x.get_device()
+    if torch._C._cuda_getDevice() != device:       # a launch goes to the current one
+        with torch.cuda.device(device):
+            return som_product(x, W, bias, act, residual, alpha, x_scale, w_scale, y, dtype, pre, ws, stream)
     M, K = x.shape
     Wp, ldw, units = _weights(W, "W", x.dtype, device)
     if W.shape[0] != K:
@@ -894,7 +892,8 @@ def som_product(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] =
     e = som_epilogue(ACTIVATIONS[act], 0, alpha, _vector(x_scale, "x_scale", M, device),
                      _vector(w_scale, "w_scale", N, device), _vector(bias, "bias", N, device), rp, ldr, pp, ldp)
     ws, wsp, n = _scratch(ws, lib.som_product_workspace_bytes(M, N, K, xt), x.device, stream)
-    _launch(lib.som_product, device, stream, xp, ldx, Wp, ldw, units, xt, M, N, K, yp, ldy, yt, ctypes.byref(e), wsp, n)
+    _check(lib.som_product(xp, ldx, Wp, ldw, units, xt, M, N, K, yp, ldy, yt, ctypes.byref(e), wsp, n,
+                           _raw_stream(device, stream)))
     return y
 
 
@@ -914,7 +913,11 @@ def som_product_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, act
     lib = load()
     dt = _float_type(x, "x", _HALVES)
     xp, ldx = _rows(x, "x")
-    device = _device_of(x, stream)
+    device = x.get_device()
+    if torch._C._cuda_getDevice() != device:       # a launch goes to the current one
+        with torch.cuda.device(device):
+            return som_product_backward(dy, x, W, act, pre, alpha, dx, dW, dbias, ws, stream, need_dx, need_dW,
+                                        need_dbias)
     M, K = x.shape
     Wp, ldw, units = _weights(W, "W", x.dtype, device)
     if W.shape[0] != K:
@@ -939,8 +942,8 @@ def som_product_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, act
         dbias = _new(N, torch.float32, x.device, stream)
     dbp = _vector(dbias, "dbias", N, device)
     ws, wsp, n = _scratch(ws, lib.som_product_backward_workspace_bytes(M, N, K, dt), x.device, stream)
-    _launch(lib.som_product_backward, device, stream, gp, ldg, xp, ldx, Wp, ldw, units, dt, M, N, K, ACTIVATIONS[act],
-            pp, ldp, alpha, dxp, lddx, dWp, lddw, dbp, wsp, n)
+    _check(lib.som_product_backward(gp, ldg, xp, ldx, Wp, ldw, units, dt, M, N, K, ACTIVATIONS[act], pp, ldp, alpha,
+                                    dxp, lddx, dWp, lddw, dbp, wsp, n, _raw_stream(device, stream)))
     return dx, dW, dbias
 
 
@@ -952,7 +955,10 @@ def som_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual:
     lib = load()
     dt = _float_type(x, "x", _FLOATS)
     xp, ldx = _rows(x, "x")
-    device = _device_of(x, stream)
+    device = x.get_device()
+    if torch._C._cuda_getDevice() != device:       # a launch goes to the current one
+        with torch.cuda.device(device):
+            return som_dropout(x, p, seed, offset, residual, y, stream)
     rows, cols = x.shape
     shape = (rows, cols)
     if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
@@ -961,5 +967,5 @@ def som_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual:
     if y is None:
         y = _new(shape, x.dtype, x.device, stream)
     yp, ldy = _rows(y, "y", x.dtype, shape, device)
-    _launch(lib.som_dropout, device, stream, xp, ldx, rp, ldr, dt, rows, cols, p, seed, offset, yp, ldy)
+    _check(lib.som_dropout(xp, ldx, rp, ldr, dt, rows, cols, p, seed, offset, yp, ldy, _raw_stream(device, stream)))
     return y
