@@ -479,8 +479,13 @@ typedef enum som_act {
  * the sum before its rounding to h.  h may be x or residual themselves (same
  * stride), which updates a residual stream in place.  y is of type `dtype`, or
  * with q8 of 8 bits (SOM_E4M3) with an fp32 factor for each row: y = q scale[row], scale
- * = max_c |y_c| / 448, at least 2^-126 (1 for a row of zeros).  scale is NULL without q8.
- * A row holding a NaN or an infinity gives NaNs.  1 <= cols < 2^31. */
+ * = max_c |y_c| / 448, at least 2^-126 (1 where every y_c is 0).  scale is NULL without q8.
+ * 1 <= cols < 2^31.
+ *
+ * A NaN in h makes its row's y NaN, an infinity itself NaN and the rest of the row 0; with
+ * q8 either makes the row and its scale NaN.  The squares are summed in fp32: a row whose sum
+ * passes 3.4e38 (elements of about 1.8e19 and more) counts as infinitely long and gives zeros.
+ * A row of zeros gives zeros, without eps NaNs. */
 som_status som_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
                         int32_t dtype, int64_t rows, int64_t cols, float eps, int32_t q8, void* y, int64_t ldy,
                         void* h, int64_t ldh, float* scale, hipStream_t stream);
@@ -492,7 +497,8 @@ som_status som_rms_norm(const void* x, int64_t ldx, const void* residual, int64_
  * dx (of type `dtype`, as dy, h, dh and weight are) is the gradient of x and of the residual
  * alike; dweight [cols] (fp32) may be NULL.  An output in 8 bits is differentiated as
  * if it were not rounded.  dx may be dy or dh (same stride).  With rows == 0
- * dweight is set to zero.  ws: som_rms_norm_backward_workspace_bytes(rows, cols),
+ * dweight is set to zero.  A row that holds a NaN or an infinity, one of zeros without eps, and
+ * one whose squares sum past fp32 give a dx and a part of dweight that say nothing.  ws: som_rms_norm_backward_workspace_bytes(rows, cols),
  * 256-byte aligned. */
 size_t som_rms_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
 som_status som_rms_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, const void* weight,
@@ -547,8 +553,9 @@ som_status som_product(const void* x, int64_t ldx, const void* W, int64_t ldw, i
  * NULL.  With an activation dP is rounded to x's type for the two products
  * (dbias sums it unrounded).  The residual's gradient is dy.  relu' is 0 at 0.
  * With M == 0 dW and dbias are set to zero.  M up to 2^30; the limit of a product
- * holds for dx, dW and dW's transpose.
- * ws: som_product_backward_workspace_bytes, 256-byte aligned. */
+ * holds for dx, dW and dW's transpose.  An input that only absent outputs read may be NULL.
+ * ws: som_product_backward_workspace_bytes, 256-byte aligned (with room for dP whatever the
+ * activation). */
 size_t som_product_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype);
 som_status som_product_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* W, int64_t ldw,
                                 int32_t w_units, int32_t dtype, int64_t M, int64_t N, int64_t K, int32_t act,
