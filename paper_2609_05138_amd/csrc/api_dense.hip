@@ -276,6 +276,8 @@ som_status som_product_backward(const void* dy, int64_t lddy, const void* x, int
   const BackwardWs w = backward_ws(M, N, K, dtype);
   SOM_CHECK(check_ws(ws, ws_bytes, w.total));
 
+  // dP is rounded to x's type because the matrix cores take 16 bits: an fp32 dP would be two
+  // products each (dx is 1.4 times as far from 64 bits so).  Its column sums are not.
   const bool rounded = act != SOM_ACT_NONE && (dx || dW);
   if (rounded || dbias) {
     som::ActGradArgs g{};

@@ -27,9 +27,10 @@
 // have left, from which the epilogue reads and writes whole rows of the tile.
 //
 // Bound, large: the matrix cores, at the clock that the card's power leaves them (8,192^3
-// bf16 763 us, 1,441 TFLOP/s; 8,192 x 4,096 x 16,384 832 us, 1,320; the instructions
-// alone 1,950 to 2,000 on such data), less the tiles' start and epilogue; small: the
-// launch and the latency of a step; few rows: the weights' bytes.
+// bf16 750 to 801 us, 1,370 to 1,470 TFLOP/s, and 8,192 x 4,096 x 16,384 775 to 832, 1,320 to
+// 1,420, over the cards measured on; the instructions alone 1,950 to 2,000 on such data), less
+// the tiles' start and epilogue; small: the launch and the latency of a step; few rows: the
+// weights' bytes.
 #pragma once
 
 #include "dense.h"
@@ -549,10 +550,11 @@ __device__ __forceinline__ i4 fragment(lds_char* step, uint32_t lane_base, int t
 }
 
 // A fragment as the matrix instructions take it: 8 k of 16 bits, or two times 8 of 8
-// bits, widened (exactly) to fp16.  The 8-bit matrix instructions are not used: they
-// line products up before they add them and drop bits that a sum in fp32 keeps (errors
-// of 2^-17 of the sum of magnitudes against the 64-bit oracle, the instructions of
-// 32 k and of 128 k alike).
+// bits, widened (exactly) to fp16.  The 8-bit matrix instructions are not used, a choice of
+// digits over speed: they line products up before they add them and drop bits that a sum in
+// fp32 keeps (errors of 2^-17 of the sum of magnitudes against the 64-bit oracle, the
+// instructions of 32 k and of 128 k alike), but run at twice the 16-bit rate, which bounds this
+// (16,384 x 4,096 x 4,096 378 us, 1,456 TFLOP/s).
 template <int E>
 struct Frag {
   static constexpr int kParts = E == kE4M3 ? 2 : 1;
@@ -745,8 +747,8 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
   }
   if (t < steps) {
     // Through registers: kDeep steps on their way, two in LDS.  (One on its way costs a
-    // memory latency, 0.8 us, per step: MEASURED.)  A tile of 256 x 256 has the registers
-    // for one.
+    // memory latency per step, 0.8 us measured.)  A tile of 256 x 256 has the registers for
+    // one.
     constexpr int kDeep = TI * TJ >= 32 ? 1 : TI * TJ >= 16 ? 2 : 3;
     u4 vp[kDeep][OpP::kEach], vq[kDeep][OpQ::kEach];
     const int64_t p_extent = PKC ? a.K : a.I, q_extent = QKC ? a.K : a.J;

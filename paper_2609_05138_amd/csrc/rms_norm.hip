@@ -5,8 +5,8 @@
 //   backward  g = dy w;  dx = s g - h s^3 mean(g h) + dh;  dw_c = sum_rows dy h s
 //
 // Bound: HBM, a few operations per element (16,384 x 8,192 bf16 with a residual into 8
-// bits 172 us, 5.5 TB/s; the gradient of 8,192 x 4,096 53 us, 5.1 TB/s; one row of 4,096
-// 2.6 us, a launch).  A row is read once and stays in the
+// bits 169 us, 5.5 TB/s; 8,192 x 8,192 fp32 195 us, 5.5 TB/s; the gradient of 8,192 x 4,096 in
+// bf16 46 to 53 us, 5.1 to 5.8 TB/s; one row of 4,096 2.5 us, a launch).  A row is read once and stays in the
 // registers of the G threads that share it, 8 elements (16 bytes of a 16-bit type) a
 // thread and read, while its sums are made.  Rows too wide for that are read again.
 #include "dense.h"
@@ -192,7 +192,9 @@ void norm_of(const RmsNormArgs& a, hipStream_t stream) {
 // A workgroup of R groups of G threads takes every (gridDim * R)th row; dweight's terms
 // stay in the threads' registers (U * 8 columns each), and each workgroup writes its
 // sums, groups added in order, as one row of `part`.  AHEAD: the next row's reads are on
-// their way while it works on one (8,192 x 4,096: 52 us; without, 67).
+// their way while it works on one (8,192 x 4,096: 52 us; without, 67).  The widest form (above
+// 8,192 columns) has no registers for that (4,096 x 16,384 bf16 96 us, 4.2 TB/s), and in fp32
+// too few for the row itself (156 spilled; 214 us, 3.8 TB/s).
 template <typename T, int G, int R, int U, bool AHEAD>
 __global__ void __launch_bounds__(G* R) k_rms_norm_back(const RmsNormBackArgs a, float* __restrict__ part_w) {
   __shared__ float part[G * R / 64], part2[G * R / 64];
