@@ -51,3 +51,19 @@ def test_the_gradient_of_rows_beside_them(cols):
     assert torch.equal(dx[keep], want[keep])
     # the columns of the NaN and the infinity; a NaN's row has no s at all
     assert bool(dweight.isnan().all())
+
+
+@pytest.mark.parametrize("rows", [1, 4, 16, 256])
+def test_every_code_of_8_bits(rows):
+    codes = torch.arange(256, dtype=torch.uint8, device=DEV)
+    values = codes.view(torch.float8_e4m3fn).float()         # +-0, subnormal and normal values, two NaNs
+    x = torch.zeros((256, 48), dtype=torch.uint8, device=DEV)
+    x[:, 33] = codes
+    x = x.view(torch.float8_e4m3fn)
+    W = torch.zeros((20, 48), device=DEV)
+    W[:, 33] = 1.0
+    W = W.to(torch.float8_e4m3fn).t()
+    got = torch.cat([som.som_product(x[a:a + rows], W, dtype=torch.float32) for a in range(0, 256, rows)])
+    want = values[:, None].expand(256, 20)
+    assert int(values.isnan().sum()) == 2
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(), want.nan_to_num())
