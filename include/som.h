@@ -498,8 +498,8 @@ som_status som_rms_norm(const void* x, int64_t ldx, const void* residual, int64_
  * alike; dweight [cols] (fp32) may be NULL.  An output in 8 bits is differentiated as
  * if it were not rounded.  dx may be dy or dh (same stride).  With rows == 0
  * dweight is set to zero.  A row that holds a NaN or an infinity, one of zeros without eps, and
- * one whose squares sum past fp32 give a dx and a part of dweight that say nothing.  ws: som_rms_norm_backward_workspace_bytes(rows, cols),
- * 256-byte aligned. */
+ * one whose squares sum past fp32 have no meaningful dx, nor has dweight with such a row.
+ * ws: som_rms_norm_backward_workspace_bytes(rows, cols), 256-byte aligned. */
 size_t som_rms_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
 som_status som_rms_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, const void* weight,
                                  const void* dh, int64_t lddh, int32_t dtype, int64_t rows, int64_t cols,
