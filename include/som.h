@@ -579,6 +579,63 @@ som_status som_dropout(const void* x, int64_t ldx, const void* residual, int64_t
                        int64_t cols, double p, uint64_t seed, uint64_t offset, void* y, int64_t ldy,
                        hipStream_t stream);
 
+/* Softmax cross entropy of documents against classes (a map's units, an output layer's
+ * tokens) whose scores are a product that is never kept:
+ *
+ *     v[m][n] = alpha sum_k x[m][k] W[k][n] + bias[n],
+ *     lse[m] = log sum_n exp v[m][n],  loss[m] = lse[m] - v[m][labels[m]].
+ *
+ * x and W are as som_product's, fp16 or bf16; with alpha = 2 t and bias = -t |w_n|^2 the scores
+ * are -t times the squared distances to a codebook's units, but for |x|^2, which cancels.  A label outside [0, N)
+ * is none: that document's loss is 0 (its lse is made all the same).  A class whose bias is minus
+ * infinity is left out; a document with no class left has lse minus infinity, and a label
+ * that is left out costs plus infinity.  A NaN or plus infinity among a document's scores makes its lse NaN.
+ * loss and lse are [M], fp32.
+ * M in [0, 2^31), N and K in [1, 2^30], with som_product's limit on their tiles.  ws:
+ * som_cross_entropy_workspace_bytes, 256-byte aligned (8 bytes for 128 scores of up to 65,536
+ * documents, and the scores themselves where a product is small or has up to four rows). */
+size_t som_cross_entropy_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype);
+som_status som_cross_entropy(const void* x, int64_t ldx, const void* W, int64_t ldw, int32_t w_units, int32_t dtype,
+                             int64_t M, int64_t N, int64_t K, const int32_t* labels, const float* bias, float alpha,
+                             float* loss, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Its gradients, from the gradient dloss [M] (fp32) of each document's loss and the lse of the
+ * forward pass:
+ *
+ *     g[m][n] = dloss[m] (exp(v[m][n] - lse[m]) - [n = labels[m]]),
+ *     dx = alpha g W^T,  dW = alpha x^T g,  dbias_n = sum_m g[m][n].
+ *
+ * dx and dW (laid out as W is) are of x's type, dbias is fp32; each may be NULL.  The scores
+ * are calculated again, for a piece of the classes at a time (about 256 MB of g); g is rounded to
+ * x's type for the two products, scaled by a power of two so that fp16 holds a mean's small
+ * values, and dbias sums it unrounded.  A document without a label, with dloss 0 or with no class left
+ * gives zeros to everything, whatever its x holds, NaN too.  lse has no gradient of its own.
+ * With M == 0 dW and dbias are set to zero.  M up to 2^30.  ws:
+ * som_cross_entropy_backward_workspace_bytes, 256-byte aligned. */
+size_t som_cross_entropy_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype);
+som_status som_cross_entropy_backward(const float* dloss, const void* x, int64_t ldx, const void* W, int64_t ldw,
+                                      int32_t w_units, int32_t dtype, int64_t M, int64_t N, int64_t K,
+                                      const int32_t* labels, const float* bias, float alpha, const float* lse, void* dx,
+                                      int64_t lddx, void* dW, int64_t lddw, float* dbias, void* ws, size_t ws_bytes,
+                                      hipStream_t stream);
+
+/* Dense rows or weights into 8 bits (SOM_E4M3) with an fp32 factor for each block: 128
+ * consecutive elements of a row (block_rows 1, the last block of a row shorter), or 128 x
+ * 128 (block_rows 128).  With s the factor of its block,
+ *
+ *     s = max |x| / 448 over the block, at least 2^-126 (1 where every x is 0),  q = x / s.
+ *
+ * q is x, or with transpose set x's transpose ([cols][ldq]), and the blocks are of the matrix
+ * that q is; its factors are scale[r / block_rows * scale_row + c / 128 * scale_block] at
+ * row r and column c of q, with strides that keep them apart.  som_product_blocks reads them
+ * fastest with scale_row 1: the factors of one block of columns next to each other.
+ * x is fp32, fp16 or bf16; q and scale do not overlap x.  A NaN or an infinity in a block makes its factor NaN or
+ * infinite, and none of the block's values can be had from it.
+ * Rows and cols below 2^31; rows == 0 is a no-op. */
+som_status som_quantise(const void* x, int64_t ldx, int32_t dtype, int64_t rows, int64_t cols, int32_t block_rows,
+                        int32_t transpose, void* q, int64_t ldq, float* scale, int64_t scale_row,
+                        int64_t scale_block, hipStream_t stream);
+
 /* ---------------------------------------------------------------------------
  * Measurement aid: read-bandwidth probe.  Reads `bytes` (a multiple of 16) of
  * device memory at `buf` (16-byte aligned) `passes` times with coalesced

@@ -39,4 +39,9 @@ from .som import (  # noqa: F401
     som_product_backward_workspace_bytes,
     som_product_workspace_bytes,
     som_dropout,
+    som_quantise,
+    som_cross_entropy,
+    som_cross_entropy_backward,
+    som_cross_entropy_backward_workspace_bytes,
+    som_cross_entropy_workspace_bytes,
 )

@@ -1,0 +1,172 @@
+// C ABI of what the dense layer is trained by and served with (declared in include/som.h):
+// blocks of 8 bits and their product, cross entropy, orthogonalised updates.
+#include <cmath>
+
+#include "api_dense.h"
+#include "cross_entropy.h"
+
+namespace {
+
+using namespace som::api;
+
+constexpr int64_t kBlock = 128;
+
+int64_t blocks(int64_t n) { return (n + kBlock - 1) / kBlock; }
+
+// Factors [rows][cols] of an output, at strides that keep them apart.
+som_status check_scale_out(const float* p, int64_t rows, int64_t cols, int64_t row, int64_t col) {
+  if (!p) return fail(SOM_ERR_INVALID_ARG, "scale is NULL");
+  SOM_CHECK(check_vector("scale", p));
+  if (row < 1 || col < 1 || row > kMaxLd || col > kMaxLd)
+    return fail(SOM_ERR_INVALID_ARG, "scale's strides must be in [1, 2^40]");
+  if (row / cols < col && col / rows < row && rows > 1 && cols > 1)
+    return fail(SOM_ERR_INVALID_ARG, "scale's strides make its entries overlap");
+  if (row > (int64_t(1) << 58) / rows || col > (int64_t(1) << 58) / cols)
+    return fail(SOM_ERR_INVALID_ARG, "scale exceeds the addressable range");
+  return SOM_OK;
+}
+
+bool is_half(int32_t t) { return t == SOM_F16 || t == SOM_BF16; }
+
+// A vector that has to be there.
+som_status need_vector(const char* name, const void* p) {
+  if (!p) return fail(SOM_ERR_INVALID_ARG, std::string(name) + " is NULL");
+  if (!aligned(p, 4)) return fail(SOM_ERR_INVALID_ARG, std::string(name) + " must be 4-byte aligned");
+  return SOM_OK;
+}
+
+som_status check_scores(int32_t w_units, int32_t dtype, int64_t M, int64_t N, int64_t K, float alpha) {
+  if (!is_half(dtype)) return fail(SOM_ERR_INVALID_ARG, "dtype must be SOM_F16 or SOM_BF16");
+  if (w_units != 0 && w_units != 1) return fail(SOM_ERR_INVALID_ARG, "w_units must be 0 or 1");
+  SOM_CHECK(check_sizes(M, N, K));
+  if (!std::isfinite(alpha)) return fail(SOM_ERR_INVALID_ARG, "alpha must be finite");
+  if (!launchable(M, N)) return fail(SOM_ERR_INVALID_ARG, "M * N is too large for one call");
+  return SOM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t som_cross_entropy_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype) {
+  if (M < 1 || M > kI32Max || N < 1 || N > kMaxK || K < 1 || K > kMaxK || !is_half(dtype)) return 0;
+  return som::loss_ws(M, N, K, dtype).total;
+}
+
+som_status som_cross_entropy(const void* x, int64_t ldx, const void* W, int64_t ldw, int32_t w_units, int32_t dtype,
+                             int64_t M, int64_t N, int64_t K, const int32_t* labels, const float* bias, float alpha,
+                             float* loss, float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+  SOM_CHECK(check_scores(w_units, dtype, M, N, K, alpha));
+  if (M == 0) return ok();
+  SOM_CHECK(check_matrix("x", x, ldx, M, K, dtype));
+  SOM_CHECK(check_matrix("W", W, ldw, w_units ? N : K, w_units ? K : N, dtype));
+  SOM_CHECK(need_vector("labels", labels));
+  SOM_CHECK(check_vector("bias", bias));
+  SOM_CHECK(need_vector("loss", loss));
+  SOM_CHECK(need_vector("lse", lse));
+  SOM_CHECK(check_ws(ws, ws_bytes, som_cross_entropy_workspace_bytes(M, N, K, dtype)));
+  som::LossCall c{};
+  c.x = x;
+  c.ldx = ldx;
+  c.W = W;
+  c.ldw = ldw;
+  c.units = w_units != 0;
+  c.dtype = dtype;
+  c.M = M;
+  c.N = N;
+  c.K = K;
+  c.labels = labels;
+  c.bias = bias;
+  c.alpha = alpha;
+  c.loss = loss;
+  c.lse = lse;
+  const hipError_t e = som::launch_loss(c, ws, stream);
+  return e == hipSuccess ? ok() : hip_fail(e, "cross entropy launch");
+}
+
+size_t som_cross_entropy_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype) {
+  if (M < 1 || M > kMaxK || N < 1 || N > kMaxK || K < 1 || K > kMaxK || !is_half(dtype)) return 0;
+  return som::grad_ws(M, N, K, dtype).total;
+}
+
+som_status som_cross_entropy_backward(const float* dloss, const void* x, int64_t ldx, const void* W, int64_t ldw,
+                                      int32_t w_units, int32_t dtype, int64_t M, int64_t N, int64_t K,
+                                      const int32_t* labels, const float* bias, float alpha, const float* lse, void* dx,
+                                      int64_t lddx, void* dW, int64_t lddw, float* dbias, void* ws, size_t ws_bytes,
+                                      hipStream_t stream) {
+  SOM_CHECK(check_scores(w_units, dtype, M, N, K, alpha));
+  if (M > kMaxK) return fail(SOM_ERR_INVALID_ARG, "M must be in [0, 2^30]");
+  if (!launchable(M, K) || !launchable(K, N) || !launchable(N, K))
+    return fail(SOM_ERR_INVALID_ARG, "a product is too large for one call");
+  const int64_t wr = w_units ? N : K, wc = w_units ? K : N;
+  if (dW) SOM_CHECK(check_matrix("dW", dW, lddw, wr, wc, dtype));
+  SOM_CHECK(check_vector("dbias", dbias));
+  if (M == 0) {
+    hipError_t e = hipSuccess;
+    if (dW) e = som::launch_zero(dW, lddw * 2, wr, wc * 2, stream);
+    if (e == hipSuccess && dbias) e = som::launch_zero(dbias, 0, 1, N * 4, stream);
+    return e == hipSuccess ? ok() : hip_fail(e, "zero launch");
+  }
+  SOM_CHECK(need_vector("dloss", dloss));
+  SOM_CHECK(check_matrix("x", x, ldx, M, K, dtype));
+  SOM_CHECK(check_matrix("W", W, ldw, wr, wc, dtype));
+  SOM_CHECK(need_vector("labels", labels));
+  SOM_CHECK(check_vector("bias", bias));
+  SOM_CHECK(need_vector("lse", lse));
+  if (dx) SOM_CHECK(check_matrix("dx", dx, lddx, M, K, dtype));
+  if (!dx && !dW && !dbias) return ok();
+  SOM_CHECK(check_ws(ws, ws_bytes, som_cross_entropy_backward_workspace_bytes(M, N, K, dtype)));
+  som::GradCall c{};
+  c.dloss = dloss;
+  c.x = x;
+  c.ldx = ldx;
+  c.W = W;
+  c.ldw = ldw;
+  c.units = w_units != 0;
+  c.dtype = dtype;
+  c.M = M;
+  c.N = N;
+  c.K = K;
+  c.labels = labels;
+  c.bias = bias;
+  c.alpha = alpha;
+  c.lse = lse;
+  c.dx = dx;
+  c.lddx = lddx;
+  c.dW = dW;
+  c.lddw = lddw;
+  c.dbias = dbias;
+  const hipError_t e = som::launch_loss_back(c, ws, stream);
+  return e == hipSuccess ? ok() : hip_fail(e, "cross entropy gradient launch");
+}
+
+som_status som_quantise(const void* x, int64_t ldx, int32_t dtype, int64_t rows, int64_t cols, int32_t block_rows,
+                        int32_t transpose, void* q, int64_t ldq, float* scale, int64_t scale_row,
+                        int64_t scale_block, hipStream_t stream) {
+  if (!is_float(dtype)) return fail(SOM_ERR_INVALID_ARG, "dtype must be SOM_F32, SOM_F16 or SOM_BF16");
+  SOM_CHECK(check_rows(rows, cols));
+  if (block_rows != 1 && block_rows != kBlock) return fail(SOM_ERR_INVALID_ARG, "block_rows must be 1 or 128");
+  if (transpose != 0 && transpose != 1) return fail(SOM_ERR_INVALID_ARG, "transpose must be 0 or 1");
+  if (rows == 0) return ok();
+  const int64_t qr = transpose ? cols : rows, qc = transpose ? rows : cols;
+  SOM_CHECK(check_matrix("x", x, ldx, rows, cols, dtype));
+  SOM_CHECK(check_matrix("q", q, ldq, qr, qc, SOM_E4M3));
+  SOM_CHECK(check_scale_out(scale, block_rows == 1 ? qr : blocks(qr), blocks(qc), scale_row, scale_block));
+  som::QuantiseArgs a{};
+  a.x = x;
+  a.q = static_cast<uint8_t*>(q);
+  a.scale = scale;
+  a.ldx = ldx;
+  a.ldq = ldq;
+  a.rows = rows;
+  a.cols = cols;
+  a.scale_row = scale_row;
+  a.scale_block = scale_block;
+  a.dtype = dtype;
+  a.block_rows = block_rows;
+  a.transpose = transpose != 0;
+  const hipError_t e = som::launch_quantise(a, stream);
+  return e == hipSuccess ? ok() : hip_fail(e, "quantise launch");
+}
+
+}  // extern "C"

@@ -1,0 +1,474 @@
+// Softmax cross entropy of rows against classes whose scores are a matrix product, and its
+// gradients; the scores are never kept.
+//
+//   forward   v = alpha x W + b;  lse_m = log sum_n exp v_mn;  loss_m = lse_m - v_m,label
+//   backward  g = dloss_m (exp(v - lse_m) - [n = label]);  dx = alpha g W^T, dW = alpha x^T g, db_n = sum_m g
+//
+// Forward: a tile of the product leaves for each of its rows the largest score m and s = sum
+// exp(v - m) (8 bytes for 256 or 128 scores), and the label's score; k_loss_join puts a row's
+// pairs together.  Where the k axis is split, or the kernels of few rows are faster, the scores go
+// through the workspace, as fp32, to k_loss_scores, which makes the pairs of 2,048 columns.
+//
+// Backward: the product again, a piece of the classes at a time: its epilogue makes g of the
+// piece, in x's type because the matrix cores take 16 bits (as som_product_backward's dP), and
+// its column sums unrounded; two products add the piece to dx (in fp32 until the last piece)
+// and give its part of dW.  g is scaled by a power of two that dloss's largest value sets, so that
+// fp16 holds what a mean over many rows gives (1 / M times a probability).
+//
+// Bound: the matrix cores.
+#include "cross_entropy.h"
+
+#include "product_modes.h"
+
+namespace som {
+namespace {
+
+constexpr int kScoreColumns = 2048;            // of a workgroup of k_loss_scores
+constexpr int64_t kRowsAtOnce = 65536;         // forward: rows of one launch, for the pairs' room
+constexpr int64_t kPieceBytes = int64_t(1) << 28;
+constexpr int64_t kLeastPiece = 2048;
+
+typedef float f2 __attribute__((ext_vector_type(2)));
+
+// One row and 2,048 columns a workgroup, from fp32 sums.
+__global__ void __launch_bounds__(256) k_loss_scores(const LossArgs a, uint32_t chunks) {
+  __shared__ f2 sums[4];
+  const int64_t g = group_index(), i = g / chunks, chunk = g - i * chunks;
+  if (i >= a.I) return;
+  const int64_t j = chunk * kScoreColumns + threadIdx.x * 8;
+  const int n = a.J - j >= 8 ? 8 : a.J > j ? static_cast<int>(a.J - j) : 0;
+  float v[8], bias[8] = {}, m = -INFINITY, s = 0.0f;
+  if (n > 0) {
+    join8(a, i, j, v);
+    if (a.bias) load8(a.bias + j, n, bias);
+    const int64_t label = a.labels[i] - j;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = e >= n || bias[e] == -INFINITY ? -INFINITY : fmaf(v[e], a.alpha, bias[e]);
+      m = fmaxf(m, v[e]);
+      if (e < n && label == e) a.label_score[i] = v[e];
+    }
+  }
+#pragma unroll
+  for (int off = 32; off; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  const float base = m == -INFINITY ? 0.0f : m;
+  if (n > 0) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += __builtin_amdgcn_exp2f(kLog2e * (v[e] - base));
+  }
+#pragma unroll
+  for (int off = 32; off; off >>= 1) s += __shfl_xor(s, off, 64);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = f2{m, s};
+  __syncthreads();
+  if (threadIdx.x) return;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) join_max_sum(m, s, sums[w][0], sums[w][1]);
+  reinterpret_cast<f2*>(a.part)[chunk * a.I + i] = f2{m, s};
+}
+
+// 16 rows a workgroup, 16 threads a row, each every 16th pair.
+__global__ void __launch_bounds__(256) k_loss_join(const f2* __restrict__ part, int64_t parts, int64_t rows,
+                                                   const int32_t* __restrict__ labels, int64_t classes,
+                                                   const float* __restrict__ label_score, float* __restrict__ loss,
+                                                   float* __restrict__ lse) {
+  __shared__ f2 sums[16][17];
+  const int r = threadIdx.x & 15, slice = threadIdx.x >> 4;
+  const int64_t i = group_index() * 16 + r;
+  float m = -INFINITY, s = 0.0f;
+  if (i < rows) {
+    constexpr int kDeep = 4;           // pairs on their way
+    for (int64_t p0 = slice; p0 < parts; p0 += 16 * kDeep) {
+      f2 one[kDeep];
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d) one[d] = p0 + 16 * d < parts ? part[(p0 + 16 * d) * rows + i] : f2{-INFINITY, 0.0f};
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d) join_max_sum(m, s, one[d][0], one[d][1]);
+    }
+  }
+  sums[slice][r] = f2{m, s};
+  __syncthreads();
+  if (slice || i >= rows) return;
+#pragma unroll
+  for (int w = 1; w < 16; ++w) join_max_sum(m, s, sums[w][r][0], sums[w][r][1]);
+  const float all = m + logf(s);       // no score but -infinity: -infinity
+  lse[i] = all;
+  const int32_t label = labels[i];
+  // (a label that cannot be had costs infinitely much, also where nothing can)
+  loss[i] = label < 0 || label >= classes ? 0.0f : all == -INFINITY ? INFINITY : all - label_score[i];
+}
+
+// ---------------------------------------------------------------------------
+// Backward
+// ---------------------------------------------------------------------------
+
+// What the workspace's head holds.
+struct GradHead {
+  float factor, inverse;     // of g as it is stored: a power of two
+  int32_t swap;              // 1: a row that counts for nothing holds a NaN or an infinity
+};
+
+// A row counts for nothing.
+__device__ __forceinline__ bool no_row(const int32_t* labels, const float* lse, const float* dloss, int64_t classes,
+                                       int64_t i) {
+  const int32_t label = labels[i];
+  return label < 0 || label >= classes || lse[i] == -INFINITY || dloss[i] == 0.0f;
+}
+
+// The head, by one workgroup (an order for the whole of it, and M is small beside M K).
+__global__ void __launch_bounds__(1024) k_grad_head(const int32_t* labels, const float* lse, const float* dloss,
+                                                    int64_t rows, int64_t classes, int bits, GradHead* head) {
+  __shared__ uint32_t tops[16];
+  uint32_t top = 0;
+  for (int64_t i = threadIdx.x; i < rows; i += 1024)
+    if (!no_row(labels, lse, dloss, classes, i)) top = max(top, __float_as_uint(dloss[i]) & 0x7fffffffu);
+  top = group_max<1024>(top, tops);
+  if (threadIdx.x) return;
+  const float most = __uint_as_float(top);
+  int e = 0;
+  if (top && most < INFINITY) e = bits - min(max(ilogbf(most), -100), 100);
+  head->factor = ldexpf(1.0f, e);
+  head->inverse = ldexpf(1.0f, -e);
+  head->swap = 0;
+}
+
+// A wave per row: looks through the rows of x that count for nothing.
+template <typename T>
+__global__ void __launch_bounds__(256) k_grad_scan(const T* x, int64_t ldx, int64_t rows, int64_t cols,
+                                                   const int32_t* labels, const float* lse, const float* dloss,
+                                                   int64_t classes, GradHead* head) {
+  const int64_t i = group_index() * 4 + (threadIdx.x >> 6);
+  if (i >= rows || !no_row(labels, lse, dloss, classes, i)) return;
+  bool bad = false;
+  for (int64_t c = (threadIdx.x & 63) * 8; c < cols; c += 512) {
+    const int n = cols - c >= 8 ? 8 : static_cast<int>(cols - c);
+    float v[8];
+    load8(x + i * ldx + c, n, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bad |= !(fabsf(v[e]) < INFINITY);
+  }
+  if (bad) head->swap = 1;             // (the same value, whoever writes it)
+}
+
+// x with zeros in such rows, if there are any.
+template <typename T>
+__global__ void __launch_bounds__(256) k_grad_clean(const T* x, int64_t ldx, int64_t rows, int64_t cols,
+                                                    const int32_t* labels, const float* lse, const float* dloss,
+                                                    int64_t classes, const GradHead* head, T* out, int64_t ldo) {
+  if (head->swap == 0) return;
+  const int lane = threadIdx.x & 63;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); i < rows; i += int64_t(gridDim.x) * 4) {
+    const bool none = no_row(labels, lse, dloss, classes, i);
+    for (int64_t c = lane * 8; c < cols; c += 512) {
+      const int n = cols - c >= 8 ? 8 : static_cast<int>(cols - c);
+      float v[8] = {};
+      if (!none) load8(x + i * ldx + c, n, v);
+      store8(out + i * ldo + c, 8, v);
+    }
+  }
+}
+
+// g and its column sums from a split product's parts: 512 columns a workgroup, every (4
+// gridDim.y)th row, as k_act_grad.
+template <typename T>
+__global__ void __launch_bounds__(256) k_grad_scores(const GradArgs a) {
+  __shared__ float sums[4][512];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t col = (static_cast<int64_t>(blockIdx.x) * 64 + lane) * 8;
+  const int n = a.J - col >= 8 ? 8 : a.J > col ? static_cast<int>(a.J - col) : 0;
+  const float factor = *a.factor;
+  float bias[8] = {}, db[8] = {};
+  if (a.bias) load8(a.bias + col, n, bias);
+  if (n > 0)
+    for (int64_t row = static_cast<int64_t>(blockIdx.y) * 4 + wave; row < a.I; row += int64_t(gridDim.y) * 4) {
+      float v[8];
+      join8(a, row, col, v);
+      grad8(a, grad_row(a, row, col, true), bias, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        db[e] += v[e];
+        v[e] *= factor;
+      }
+      store8(static_cast<T*>(a.out) + row * a.ldo + col, 8, v);
+    }
+  if (!a.column_part) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[wave][lane * 8 + e] = db[e];
+  __syncthreads();
+  for (int c = threadIdx.x; c < 512; c += 256) {
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 512 + c;
+    if (at < a.J)
+      a.column_part[static_cast<int64_t>(blockIdx.y) * a.ld_column + at] = sums[0][c] + sums[1][c] + sums[2][c] + sums[3][c];
+  }
+}
+
+int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
+size_t most(size_t a, size_t b) { return a > b ? a : b; }
+
+int64_t scores_groups(int64_t rows) {
+  const int64_t g = (rows + 3) / 4;
+  return g < 64 ? g : 64;
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------------------
+// Workspaces
+// ---------------------------------------------------------------------------
+
+LossWs loss_ws(int64_t M, int64_t N, int64_t K, int elem) {
+  LossWs w{};
+  const int64_t rows = M < kRowsAtOnce ? M : kRowsAtOnce;
+  w.label_score = 0;
+  size_t o = align_up(sizeof(float) * rows, 256);
+  w.part = o;
+  o += align_up(2 * sizeof(float) * rows * ((N + 127) / 128), 256);
+  w.scores = o;
+  size_t need = 0;
+  for (const bool dma : {true, false})
+    for (const bool units : {true, false})
+      for (const int64_t m : {rows, M % rows}) {          // the last rows may be fewer
+        if (m == 0) continue;
+        const ProductPlan p = plan_product(m, N, K, elem, true, units, dma);
+        need = most(need, p.shape == kFew ? static_cast<size_t>(m) * round8(N) : p.partial_floats);
+      }
+  w.total = o + align_up(sizeof(float) * need, 256);
+  return w;
+}
+
+int64_t grad_piece(int64_t M, int64_t N) {
+  int64_t piece = kPieceBytes / 2 / M / 256 * 256;
+  if (piece < kLeastPiece) piece = kLeastPiece;
+  return piece < N ? piece : N;
+}
+
+GradWs grad_ws(int64_t M, int64_t N, int64_t K, int elem) {
+  GradWs w{};
+  w.piece = grad_piece(M, N);
+  w.ldg = round8(w.piece);
+  w.ldx = round8(K);
+  w.ld_column = round8(w.piece);
+  w.head = 0;
+  size_t o = 256;
+  w.g = o;
+  o += align_up(static_cast<size_t>(M) * w.ldg * 2, 256);
+  w.clean = o;
+  o += align_up(static_cast<size_t>(M) * w.ldx * 2, 256);
+  w.dx = o;
+  if (w.piece < N) o += align_up(sizeof(float) * M * w.ldx, 256);
+  size_t need = 0;
+  int64_t groups = 1;                  // of rows, each with its column sums
+  for (const bool dma : {true, false})
+    for (const int64_t n : {w.piece, N % w.piece}) {
+      if (n == 0) continue;
+      for (const bool units : {true, false}) {
+        const ProductPlan p = plan_extra(M, n, K, elem, true, units, dma);
+        const int64_t g = p.splits > 1 ? scores_groups(M) : (M + kInfo[p.shape].bi - 1) / kInfo[p.shape].bi;
+        if (g > groups) groups = g;
+        need = most(need, p.partial_floats);
+      }
+      for (const ProductPlan& p :
+           {plan_extra(M, K, n, elem, true, false, dma), plan_extra(M, K, n, elem, true, true, dma),
+            plan_extra(K, n, M, elem, false, false, dma), plan_extra(n, K, M, elem, false, false, dma)})
+        need = most(need, p.partial_floats);
+    }
+  w.column = o;
+  o += align_up(sizeof(float) * groups * w.ld_column, 256);
+  w.partial = o;
+  w.total = o + align_up(sizeof(float) * need, 256);
+  return w;
+}
+
+// ---------------------------------------------------------------------------
+// Launches
+// ---------------------------------------------------------------------------
+
+namespace {
+
+template <typename P>
+P* at(void* base, size_t off) {
+  return reinterpret_cast<P*>(static_cast<char*>(base) + off);
+}
+
+}  // namespace
+
+hipError_t launch_loss(const LossCall& c, void* ws, hipStream_t stream) {
+  const LossWs w = loss_ws(c.M, c.N, c.K, c.dtype);
+  for (int64_t m0 = 0; m0 < c.M; m0 += kRowsAtOnce) {
+    const int64_t rows = c.M - m0 < kRowsAtOnce ? c.M - m0 : kRowsAtOnce;
+    LossArgs a{};
+    a.P = static_cast<const char*>(c.x) + m0 * c.ldx * 2;
+    a.ldp = c.ldx;
+    a.p_kc = true;
+    a.Q = c.W;
+    a.ldq = c.ldw;
+    a.q_kc = c.units;
+    a.I = rows;
+    a.J = c.N;
+    a.K = c.K;
+    a.elem = c.dtype;
+    a.alpha = c.alpha;
+    a.bias = c.bias;
+    a.labels = c.labels + m0;
+    a.part = at<float>(ws, w.part);
+    a.label_score = at<float>(ws, w.label_score);
+    a.dma = rows_on_16(a);
+    const ProductPlan p = plan_product(a.I, a.J, a.K, a.elem, true, a.q_kc, a.dma);
+    float* const scores = at<float>(ws, w.scores);
+    int64_t parts;
+    hipError_t e;
+    if (p.shape == kFew) {             // plain sums, which k_loss_scores takes like one split
+      ProductArgs f = a;
+      f.alpha = 1.0f;
+      f.bias = nullptr;
+      f.out = scores;
+      f.ldo = round8(c.N);
+      f.out_type = kF32;
+      f.splits = 1;
+      e = launch_product_few(f, stream);
+      a.partial = scores;
+      a.splits = 1;
+      parts = (c.N + kScoreColumns - 1) / kScoreColumns;
+    } else {
+      set_launch(a, p, scores);
+      e = launch_mode(kLoss, p.shape, a, stream);
+      parts = p.splits > 1 ? (c.N + kScoreColumns - 1) / kScoreColumns : a.tiles_j;
+    }
+    if (e != hipSuccess) return e;
+    if (p.shape == kFew || p.splits > 1) {
+      hipLaunchKernelGGL(k_loss_scores, groups_grid(parts * rows), dim3(256), 0, stream, a, static_cast<uint32_t>(parts));
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(k_loss_join, groups_grid((rows + 15) / 16), dim3(256), 0, stream,
+                       reinterpret_cast<const f2*>(a.part), parts, rows, a.labels, c.N, a.label_score, c.loss + m0,
+                       c.lse + m0);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <typename T>
+static hipError_t prepare_rows(const GradCall& c, const GradWs& w, void* ws, hipStream_t stream) {
+  GradHead* const head = at<GradHead>(ws, w.head);
+  hipLaunchKernelGGL(k_grad_head, dim3(1), dim3(1024), 0, stream, c.labels, c.lse, c.dloss, c.M, c.N,
+                     c.dtype == kF16 ? 14 : 0, head);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !c.dW) return e;
+  const T* const x = static_cast<const T*>(c.x);
+  hipLaunchKernelGGL(k_grad_scan<T>, groups_grid((c.M + 3) / 4), dim3(256), 0, stream, x, c.ldx, c.M, c.K, c.labels,
+                     c.lse, c.dloss, c.N, head);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t groups = (c.M + 3) / 4;
+  hipLaunchKernelGGL(k_grad_clean<T>, dim3(static_cast<uint32_t>(groups < 2048 ? groups : 2048)), dim3(256), 0, stream, x,
+                     c.ldx, c.M, c.K, c.labels, c.lse, c.dloss, c.N, head, at<T>(ws, w.clean), w.ldx);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_back(const GradCall& c, void* ws, hipStream_t stream) {
+  const GradWs w = grad_ws(c.M, c.N, c.K, c.dtype);
+  hipError_t e = c.dtype == kF16 ? prepare_rows<f16>(c, w, ws, stream) : prepare_rows<bf16>(c, w, ws, stream);
+  if (e != hipSuccess) return e;
+  GradHead* const head = at<GradHead>(ws, w.head);
+  float* const partial = at<float>(ws, w.partial);
+  void* const g = at<void>(ws, w.g);
+  for (int64_t n0 = 0; n0 < c.N; n0 += w.piece) {
+    const int64_t n = c.N - n0 < w.piece ? c.N - n0 : w.piece;
+    const int64_t skip = n0 * (c.units ? c.ldw : 1) * 2, dskip = n0 * (c.units ? c.lddw : 1) * 2;
+    const void* const W = static_cast<const char*>(c.W) + skip;
+    GradArgs a{};
+    a.P = c.x;
+    a.ldp = c.ldx;
+    a.p_kc = true;
+    a.Q = W;
+    a.ldq = c.ldw;
+    a.q_kc = c.units;
+    a.I = c.M;
+    a.J = n;
+    a.K = c.K;
+    a.elem = c.dtype;
+    a.alpha = c.alpha;
+    a.bias = c.bias ? c.bias + n0 : nullptr;
+    a.out = g;
+    a.ldo = w.ldg;
+    a.labels = c.labels;
+    a.lse = c.lse;
+    a.dloss = c.dloss;
+    a.factor = &head->factor;
+    a.first = n0;
+    a.classes = c.N;
+    a.column_part = c.dbias ? at<float>(ws, w.column) : nullptr;
+    a.ld_column = w.ld_column;
+    a.dma = rows_on_16(a);
+    const ProductPlan p = plan_extra(a.I, a.J, a.K, a.elem, true, a.q_kc, a.dma);
+    set_launch(a, p, partial);
+    e = launch_mode(kGrad, p.shape, a, stream);
+    if (e != hipSuccess) return e;
+    int64_t groups = a.tiles_i;
+    if (p.splits > 1) {
+      groups = scores_groups(c.M);
+      const dim3 grid(static_cast<uint32_t>((n + 511) / 512), static_cast<uint32_t>(groups));
+      if (c.dtype == kF16)
+        hipLaunchKernelGGL(k_grad_scores<f16>, grid, dim3(256), 0, stream, a);
+      else
+        hipLaunchKernelGGL(k_grad_scores<bf16>, grid, dim3(256), 0, stream, a);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    if (c.dbias) {
+      e = launch_column_sums(a.column_part, groups, w.ld_column, n, c.dbias + n0, stream);
+      if (e != hipSuccess) return e;
+    }
+    ExtraArgs d{};
+    d.elem = c.dtype;
+    d.alpha = c.alpha;
+    d.factor = &head->inverse;
+    d.beta = 1.0f;
+    d.res_type = kF32;
+    if (c.dx) {
+      const bool last = n0 + n == c.N;
+      float* const sum = at<float>(ws, w.dx);
+      d.P = g;
+      d.ldp = w.ldg;
+      d.p_kc = true;
+      d.Q = W;
+      d.ldq = c.ldw;
+      d.q_kc = !c.units;
+      d.I = c.M;
+      d.J = c.K;
+      d.K = n;
+      d.residual = n0 ? sum : nullptr;
+      d.ldr = w.ldx;
+      d.out = last ? c.dx : sum;
+      d.ldo = last ? c.lddx : w.ldx;
+      d.out_type = last ? c.dtype : kF32;
+      e = launch_extra(d, partial, stream);
+      if (e != hipSuccess) return e;
+    }
+    if (c.dW) {
+      d.P = c.units ? g : c.x;
+      d.ldp = c.units ? w.ldg : c.ldx;
+      d.p_kc = false;
+      d.Q = c.units ? c.x : g;
+      d.ldq = c.units ? c.ldx : w.ldg;
+      d.q_kc = false;
+      d.I = c.units ? n : c.K;
+      d.J = c.units ? c.K : n;
+      d.K = c.M;
+      d.residual = nullptr;
+      d.out = static_cast<char*>(c.dW) + dskip;
+      d.ldo = c.lddw;
+      d.out_type = c.dtype;
+      d.swap = &head->swap;
+      d.swapped = at<void>(ws, w.clean);
+      d.ld_swapped = w.ldx;
+      d.swap_p = !c.units;
+      e = launch_extra(d, partial, stream);
+      if (e != hipSuccess) return e;
+    }
+  }
+  return hipSuccess;
+}
+
+}  // namespace som

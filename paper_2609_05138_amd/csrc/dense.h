@@ -92,6 +92,15 @@ __device__ __forceinline__ void store8_e4m3(uint8_t* p, int n, const float (&v)[
   }
 }
 
+// The factor of a row's (or block's) 8-bit values from the bits of the largest magnitude (as unsigned
+// words NaN is above every number, so a NaN anywhere reaches the factor).  At least the
+// smallest normal number, whose inverse is finite.
+__device__ __forceinline__ float q8_scale(uint32_t top) {
+  constexpr float kLeast = 1.17549435e-38f;             // 2^-126
+  const float scale = __uint_as_float(top) / kE4M3Max;
+  return top == 0 ? 1.0f : scale < kLeast ? kLeast : scale;
+}
+
 // Sum (or maximum of unsigned words) over the G = 64, 256, ... consecutive threads
 // that share a row; every one of them gets it.  `part`: a word for each wave of the
 // workgroup.  Each wave's sum is a butterfly, the waves are added in order, so the
@@ -169,5 +178,17 @@ struct DropoutArgs {
   uint64_t seed, offset;
 };
 hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream);
+
+// Factors lie at scale[row / block_rows * scale_row + column / 128 * scale_block], rows and
+// columns being those of q (with `transpose` x's columns and rows).
+struct QuantiseArgs {
+  const void* x;
+  uint8_t* q;
+  float* scale;
+  int64_t ldx, ldq, rows, cols, scale_row, scale_block;
+  int dtype, block_rows;       // 1 or 128
+  bool transpose;
+};
+hipError_t launch_quantise(const QuantiseArgs& a, hipStream_t stream);
 
 }  // namespace som

@@ -75,8 +75,11 @@ struct ProductPlan {
   int64_t k_split;
   size_t partial_floats;
 };
-// `dma`: the rows of both operands start on 16 bytes
-ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma);
+// `dma`: the rows of both operands start on 16 bytes; `few`: the kernels of few rows will do
+ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma, bool few = true);
+// Rows of both operands start on 16 bytes, at strides that a tile's 32-bit offsets span.
+bool rows_on_16(const ProductArgs& a);
+void set_launch(ProductArgs& a, const ProductPlan& p, float* partial);
 // Fills the launch's fields of `a` and enqueues it (and the join of a split k axis);
 // `partial`: plan_product's floats.
 hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream);
@@ -299,6 +302,27 @@ __device__ __forceinline__ void finish8(const ProductArgs& a, int64_t i, int64_t
     finish_some<true>(a, i, j, n, v, c, r);
   else
     finish_some<false>(a, i, j, n, v, c, r);
+}
+
+// Eight columns of row i from their partial sums, added in the order of the splits.
+__device__ __forceinline__ void join8(const ProductArgs& a, int64_t i, int64_t j, float (&v)[8]) {
+  const int64_t ld = (a.J + 7) / 8 * 8;
+  const float* p = a.partial + i * ld + j;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+  constexpr int kDeep = 8;             // parts on their way
+  for (int s0 = 0; s0 < a.splits; s0 += kDeep) {
+    float w[kDeep][8];
+#pragma unroll
+    for (int s = 0; s < kDeep; ++s)
+      if (s0 + s < a.splits) load8(p + (s0 + s) * a.I * ld, 8, w[s]);
+#pragma unroll
+    for (int s = 0; s < kDeep; ++s)
+      if (s0 + s < a.splits) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += w[s][e];
+      }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -600,6 +624,129 @@ __device__ __forceinline__ f4 mfma(const Frag<E>& q, const Frag<E>& p, f4 c) {
 // The kernel
 // ---------------------------------------------------------------------------
 
+// A workgroup's tile of C and its part of the k axis.  XCD x (workgroups are dealt to the
+// XCDs in turn) takes the tiles [x * per_xcd, ...): tiles in bands of kBand rows of tiles, so
+// that the ones it runs at once share both operands' rows in its L2.
+struct TilePlace {
+  uint32_t ti, tj, split;
+  int32_t k0, k1;
+  bool live;
+};
+__device__ __forceinline__ TilePlace tile_place(const ProductArgs& a) {
+  constexpr uint32_t kBand = 4;
+  const uint32_t lin = blockIdx.x % kXcds * a.per_xcd + blockIdx.x / kXcds;
+  const uint32_t tiles = a.tiles_i * a.tiles_j;
+  TilePlace t;
+  t.live = lin < tiles * a.splits;
+  if (!t.live) return t;
+  // (divisions go through the vector unit: back to scalar registers)
+  t.split = __builtin_amdgcn_readfirstlane(lin / tiles);
+  const uint32_t rest = lin - t.split * tiles;
+  const uint32_t band = __builtin_amdgcn_readfirstlane(rest / (kBand * a.tiles_j)), in = rest - band * kBand * a.tiles_j;
+  const uint32_t height = min(kBand, a.tiles_i - band * kBand);
+  t.tj = __builtin_amdgcn_readfirstlane(in / height);
+  t.ti = band * kBand + (in - t.tj * height);
+  t.k0 = static_cast<int32_t>(t.split * a.k_split);
+  t.k1 = static_cast<int32_t>(min(a.K, t.k0 + a.k_split));
+  return t;
+}
+
+// The epilogue by rows: up to 64 rows of the wave's columns at a time go through its own
+// part of LDS, so that a lane has eight consecutive columns and the wave's reads and
+// writes of C are whole lines.  Quads of columns are swizzled by row: the 16 lanes that
+// write a quad of their rows, and the ones that read two rows, meet no bank twice.
+// What a row needs from memory is asked for kAhead loads of the wave before.
+template <int WI, int WJ, int TI, int TJ, int LDS>
+struct Tile {
+  static constexpr int kWI = WI, kWJ = WJ, kTI = TI, kTJ = TJ;
+  static constexpr int kCols = TJ * 16, kLanes = kCols / 8, kRows = 64 / kLanes;    // rows per access of the wave
+  static constexpr int kBatch = TI < 4 ? TI : 4, kAhead = 3;
+  static constexpr int kGroups = TI * 16 / kRows;                                   // accesses of kRows rows
+  static_assert(WI * WJ * kBatch * 16 * kCols * 4 <= LDS, "the rows fit the steps' place");
+  static_assert(TI % kBatch == 0 && TI / kBatch <= 2 && (TJ == 2 || TJ == 4), "see below");
+  typedef __attribute__((address_space(3))) f4 lds_f4;
+
+  lds_char* lds;
+  lds_char* mine;
+  int wave, lane, col, n;       // n: this lane's columns inside C, none if <= 0
+  int64_t i0, j0, j, first;     // j, first: this lane's first column and row
+
+  __device__ __forceinline__ Tile(const ProductArgs& a, lds_char* l3, int w, int64_t i, int64_t jj)
+      : lds(l3), mine(l3 + w * (kBatch * 16 * kCols * 4)), wave(w), lane(threadIdx.x & 63), col(lane % kLanes),
+        i0(i), j0(jj), j(jj + w % WJ * kCols + col * 8), first(i + w / WJ * TI * 16 + lane / kLanes) {
+    n = static_cast<int>(min<int64_t>(8, a.J - j));
+  }
+  __device__ __forceinline__ lds_f4* quad(int row, int k) const {
+    const int sw = TJ == 4 ? row : row >> 1;
+    return reinterpret_cast<lds_f4*>(mine + (row * kCols + ((k ^ sw) & (TJ * 4 - 1)) * 4) * 4);
+  }
+  // rows [b * kBatch * 16, ...) of the wave's into LDS
+  __device__ __forceinline__ void stage(const f4 (&acc)[TI][TJ], int b) const {
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x)
+#pragma unroll
+      for (int y = 0; y < TJ; ++y) {
+        f4 v = acc[x][y];
+        if constexpr (TI > kBatch) v = b ? acc[kBatch + x][y] : v;
+        *quad(x * 16 + (lane & 15), y * 4 + (lane >> 4)) = v;
+      }
+    __builtin_amdgcn_wave_barrier();
+  }
+  // `take`(access, row of C, its eight sums) for every access
+  template <class Take>
+  __device__ __forceinline__ void rows(const f4 (&acc)[TI][TJ], Take take) const {
+#pragma unroll 1
+    for (int b = 0; b < TI / kBatch; ++b) {
+      stage(acc, b);
+#pragma unroll 1
+      for (int r = 0; r < kBatch * 16; r += kRows) {
+        const int row = r + lane / kLanes, g = (b * kBatch * 16 + r) / kRows;
+        const f4 lo = *quad(row, 2 * col), hi = *quad(row, 2 * col + 1);
+        float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        take(g, first + g * kRows, v);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+  // sums of a split k axis
+  __device__ __forceinline__ void part(const ProductArgs& a, const f4 (&acc)[TI][TJ], uint32_t split) const {
+    const int32_t ld_part = static_cast<int32_t>((a.J + 7) / 8 * 8);
+    rows(acc, [&](int, int64_t i, float (&v)[8]) __attribute__((always_inline)) {
+      if (i < a.I && n > 0) store8(a.partial + (split * a.I + i) * ld_part + j, 8, v);
+    });
+  }
+  __device__ __forceinline__ void finish(const ProductArgs& a, const f4 (&acc)[TI][TJ], uint32_t split) const {
+    if (a.splits > 1) return part(a, acc, split);
+    ColumnTerms ct = column_terms(a, j, n);
+    // (here, and not at their first use: in the loop below that would be a wait for the
+    // stores of the rows before, since loads and stores are counted together)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(ct.scale[e]), "+v"(ct.bias[e]));
+    auto terms = [&](int g) __attribute__((always_inline)) {
+      const int64_t i = first + g * kRows;
+      return row_terms(a, i, j, g < kGroups && i < a.I ? n : 0);
+    };
+    if (a.residual || a.p_scale) {
+      RowTerms ahead[kAhead];
+#pragma unroll
+      for (int g = 0; g < kAhead; ++g) ahead[g] = terms(g);
+      rows(acc, [&](int g, int64_t i, float (&v)[8]) __attribute__((always_inline)) {
+        const RowTerms now = ahead[0];
+#pragma unroll
+        for (int k = 0; k + 1 < kAhead; ++k) ahead[k] = ahead[k + 1];
+        ahead[kAhead - 1] = terms(g + kAhead);
+        if (i < a.I && n > 0) finish8(a, i, j, n, v, ct, now);
+      });
+    } else {
+      RowTerms none;
+      none.scale = a.alpha;
+      rows(acc, [&](int, int64_t i, float (&v)[8]) __attribute__((always_inline)) {
+        if (i < a.I && n > 0) finish8(a, i, j, n, v, ct, none);
+      });
+    }
+  }
+};
+
 struct Yes {
   static constexpr bool value = true;
 };
@@ -607,9 +754,22 @@ struct No {
   static constexpr bool value = false;
 };
 
+// What becomes of a tile's sums: the epilogue of som_product, or one of product_modes.h,
+// which take more arguments.
+constexpr int kPlain = 0, kExtra = 1, kLoss = 2, kGrad = 3;
+template <int MODE>
+struct ModeArgs;
+template <>
+struct ModeArgs<kPlain> {
+  typedef ProductArgs type;
+};
+template <int MODE, class TileOf, int TI, int TJ>
+__device__ __forceinline__ void finish_mode(const TileOf& tile, const typename ModeArgs<MODE>::type& a,
+                                            const f4 (&acc)[TI][TJ], const TilePlace& place);
+
 // WI x WJ waves, each with TI x TJ tiles of 16 x 16; NS steps in LDS.
-template <int E, bool PKC, bool QKC, int WI, int WJ, int TI, int TJ, int NS>
-__global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
+template <int E, bool PKC, bool QKC, int WI, int WJ, int TI, int TJ, int NS, int MODE = kPlain>
+__global__ void __launch_bounds__(WI* WJ * 64) k_product(const typename ModeArgs<MODE>::type a) {
   constexpr int ES = E == kE4M3 ? 1 : 2;
   constexpr int BI = WI * TI * 16, BJ = WJ * TJ * 16, THREADS = WI * WJ * 64;
   using OpP = Operand<ES, PKC, BI, THREADS>;
@@ -618,29 +778,23 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
   constexpr int kStep = kStepBytes / ES;
   extern __shared__ __align__(1024) char lds[];
 
-  // XCD x (workgroups are dealt to the XCDs in turn) takes the tiles [x * per_xcd, ...):
-  // tiles in bands of kBand rows of tiles, so that the ones it runs at once share
-  // both operands' rows in its L2
-  constexpr uint32_t kBand = 4;
-  const uint32_t lin = blockIdx.x % kXcds * a.per_xcd + blockIdx.x / kXcds;
-  const uint32_t tiles = a.tiles_i * a.tiles_j;
-  if (lin >= tiles * a.splits) return;
-  // (divisions go through the vector unit: back to scalar registers)
-  const uint32_t split = __builtin_amdgcn_readfirstlane(lin / tiles), rest = lin - split * tiles;
-  const uint32_t band = __builtin_amdgcn_readfirstlane(rest / (kBand * a.tiles_j)), in = rest - band * kBand * a.tiles_j;
-  const uint32_t height = min(kBand, a.tiles_i - band * kBand);
-  const uint32_t across = __builtin_amdgcn_readfirstlane(in / height);
-  const int64_t i0 = static_cast<int64_t>(band * kBand + (in - across * height)) * BI;
-  const int64_t j0 = static_cast<int64_t>(across) * BJ;
-  const int32_t k0 = static_cast<int32_t>(split * a.k_split);
-  const int32_t k1 = static_cast<int32_t>(min(a.K, k0 + a.k_split));
+  const TilePlace place = tile_place(a);
+  if (!place.live) return;
+  const int64_t i0 = static_cast<int64_t>(place.ti) * BI, j0 = static_cast<int64_t>(place.tj) * BJ;
+  const int32_t k0 = place.k0, k1 = place.k1;
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
   OpP p;
   OpQ q;
-  p.init(a.P, a.ldp, i0, a.I);
-  q.init(a.Q, a.ldq, j0, a.J);
+  if constexpr (MODE == kExtra) {
+    const bool swap = a.swap && *a.swap != 0;
+    p.init(swap && a.swap_p ? a.swapped : a.P, swap && a.swap_p ? a.ld_swapped : a.ldp, i0, a.I);
+    q.init(swap && !a.swap_p ? a.swapped : a.Q, swap && !a.swap_p ? a.ld_swapped : a.ldq, j0, a.J);
+  } else {
+    p.init(a.P, a.ldp, i0, a.I);
+    q.init(a.Q, a.ldq, j0, a.J);
+  }
   const uint32_t pb = OpP::lane_base(wi * TI * 16), qb = OpQ::lane_base(wj * TJ * 16);
   lds_char* const l3 = (lds_char*)lds;
   const uint32_t l0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(l3));
@@ -724,13 +878,13 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
     auto step = [&](auto fetches) __attribute__((always_inline)) {
       phase(f[0], f[1], slot, 1, [](int) {});
       arrived(t + 1, NS - 2);
-      const int place = slot;
+      const int freed = slot;
       slot = slot + 1 == NS ? 0 : slot + 1;
       // (after the last step: bytes that no product uses)
       phase(f[1], f[0], slot, 0, [&](int x) __attribute__((always_inline)) {
         if constexpr (decltype(fetches)::value)
 #pragma unroll
-          for (int n = x * kMost / TI; n < (x + 1) * kMost / TI; ++n) fetch_one(n, t + NS, place);
+          for (int n = x * kMost / TI; n < (x + 1) * kMost / TI; ++n) fetch_one(n, t + NS, freed);
       });
     };
     if (full > 0) {
@@ -810,89 +964,12 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const ProductArgs a) {
     }
   }
 
-  // The epilogue by rows: up to 64 rows of the wave's columns at a time go through its own
-  // part of LDS, so that a lane has eight consecutive columns and the wave's reads and
-  // writes of C are whole lines.  Quads of columns are swizzled by row: the 16 lanes that
-  // write a quad of their rows, and the ones that read two rows, meet no bank twice.
-  // What a row needs from memory is asked for kAhead loads of the wave before.
-  constexpr int kCols = TJ * 16, kLanes = kCols / 8, kRows = 64 / kLanes;    // rows per access of the wave
-  constexpr int kBatch = TI < 4 ? TI : 4, kAhead = 3;
-  static_assert(WI * WJ * kBatch * 16 * kCols * 4 <= NS * kStage, "the rows fit the steps' place");
-  static_assert(TI % kBatch == 0 && TI / kBatch <= 2 && (TJ == 2 || TJ == 4), "see below");
   __syncthreads();                     // every wave is done with the steps
-  typedef __attribute__((address_space(3))) f4 lds_f4;
-  lds_char* const mine = l3 + wave * (kBatch * 16 * kCols * 4);
-  const int lane = threadIdx.x & 63;
-  auto quad = [&](int row, int k) {
-    const int sw = TJ == 4 ? row : row >> 1;
-    return reinterpret_cast<lds_f4*>(mine + (row * kCols + ((k ^ sw) & (TJ * 4 - 1)) * 4) * 4);
-  };
-  const int col = lane % kLanes;
-  const int64_t j = j0 + wj * kCols + col * 8;
-  const int n = static_cast<int>(min<int64_t>(8, a.J - j));
-  const int64_t first = i0 + wi * TI * 16 + lane / kLanes;
-  constexpr int kGroups = TI * 16 / kRows;                      // accesses of kRows rows
-  const int32_t ld_part = static_cast<int32_t>((a.J + 7) / 8 * 8);
-  // rows [b * kBatch * 16, ...) of the wave's into LDS
-  auto stage = [&](int b) __attribute__((always_inline)) {
-#pragma unroll
-    for (int x = 0; x < kBatch; ++x)
-#pragma unroll
-      for (int y = 0; y < TJ; ++y) {
-        f4 v = acc[x][y];
-        if constexpr (TI > kBatch) v = b ? acc[kBatch + x][y] : v;
-        *quad(x * 16 + (lane & 15), y * 4 + (lane >> 4)) = v;
-      }
-    __builtin_amdgcn_wave_barrier();
-  };
-  // `take`(access, row of C, its eight sums) for every access
-  auto rows = [&](auto take) __attribute__((always_inline)) {
-#pragma unroll 1
-    for (int b = 0; b < TI / kBatch; ++b) {
-      stage(b);
-#pragma unroll 1
-      for (int r = 0; r < kBatch * 16; r += kRows) {
-        const int row = r + lane / kLanes, g = (b * kBatch * 16 + r) / kRows;
-        const f4 lo = *quad(row, 2 * col), hi = *quad(row, 2 * col + 1);
-        float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        take(g, first + g * kRows, v);
-      }
-      __builtin_amdgcn_wave_barrier();
-    }
-  };
-  auto terms = [&](int g) __attribute__((always_inline)) {
-    const int64_t i = first + g * kRows;
-    return row_terms(a, i, j, g < kGroups && i < a.I ? n : 0);
-  };
-  if (a.splits > 1) {
-    rows([&](int, int64_t i, float (&v)[8]) __attribute__((always_inline)) {
-      if (i < a.I && n > 0) store8(a.partial + (split * a.I + i) * ld_part + j, 8, v);
-    });
-    return;
-  }
-  ColumnTerms ct = column_terms(a, j, n);
-  // (here, and not at their first use: in the loop below that would be a wait for the
-  // stores of the rows before, since loads and stores are counted together)
-#pragma unroll
-  for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(ct.scale[e]), "+v"(ct.bias[e]));
-  if (a.residual || a.p_scale) {
-    RowTerms ahead[kAhead];
-#pragma unroll
-    for (int g = 0; g < kAhead; ++g) ahead[g] = terms(g);
-    rows([&](int g, int64_t i, float (&v)[8]) __attribute__((always_inline)) {
-      const RowTerms now = ahead[0];
-#pragma unroll
-      for (int k = 0; k + 1 < kAhead; ++k) ahead[k] = ahead[k + 1];
-      ahead[kAhead - 1] = terms(g + kAhead);
-      if (i < a.I && n > 0) finish8(a, i, j, n, v, ct, now);
-    });
-  } else {
-    RowTerms none;
-    none.scale = a.alpha;
-    rows([&](int, int64_t i, float (&v)[8]) __attribute__((always_inline)) {
-      if (i < a.I && n > 0) finish8(a, i, j, n, v, ct, none);
-    });
-  }
+  const Tile<WI, WJ, TI, TJ, NS * kStage> tile(a, l3, wave, i0, j0);
+  if constexpr (MODE == kPlain)
+    tile.finish(a, acc, place.split);
+  else
+    finish_mode<MODE>(tile, a, acc, place);
 }
 
 }  // namespace som

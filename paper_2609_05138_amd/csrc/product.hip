@@ -9,25 +9,12 @@ namespace {
 
 // C from its partial sums, added in the order of the splits; eight columns a thread.
 __global__ void __launch_bounds__(256) k_join(const ProductArgs a) {
-  const int64_t ld = (a.J + 7) / 8 * 8, groups = ld / 8;
+  const int64_t groups = (a.J + 7) / 8;
   const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (at >= groups * a.I) return;
   const int64_t i = at / groups, j = at % groups * 8;
-  const float* p = a.partial + i * ld + j;
-  float v[8] = {};
-  constexpr int kDeep = 8;             // parts on their way
-  for (int s0 = 0; s0 < a.splits; s0 += kDeep) {
-    float w[kDeep][8];
-#pragma unroll
-    for (int s = 0; s < kDeep; ++s)
-      if (s0 + s < a.splits) load8(p + (s0 + s) * a.I * ld, 8, w[s]);
-#pragma unroll
-    for (int s = 0; s < kDeep; ++s)
-      if (s0 + s < a.splits) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += w[s][e];
-      }
-  }
+  float v[8];
+  join8(a, i, j, v);
   const int n = static_cast<int>(min<int64_t>(8, a.J - j));
   finish8(a, i, j, n, v, column_terms(a, j, n), row_terms(a, i, j, n));
 }
@@ -120,8 +107,9 @@ double product_time(int shape, int64_t n, int64_t steps, bool e4m3, bool dma) {
 // launches).  With k strided one row does from 8,192 columns on (2,048 x 16,384: 13.4
 // against 17.6; two rows are no faster; 4,096 x 4,096: 11.4 against 8.9, since a
 // narrow strip's lines are read by several CUs).
-ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma) {
-  if (p_kc && J <= kFewMaxColumns && (q_kc ? I <= 4 : I == 1 && J >= 8192)) return {kFew, 1, K, 0};
+ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma,
+                         bool few) {
+  if (few && p_kc && J <= kFewMaxColumns && (q_kc ? I <= 4 : I == 1 && J >= 8192)) return {kFew, 1, K, 0};
   const int64_t step = elem == kE4M3 ? 128 : 64;
   const int64_t steps = (K + step - 1) / step;
   ProductPlan best{kShape256, 1, steps * step, 0};
@@ -150,22 +138,31 @@ ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, b
   return best;
 }
 
-hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream) {
+bool rows_on_16(const ProductArgs& a) {
   const int64_t es = dtype_bytes(a.elem);
   auto whole = [&](const void* p, int64_t ld) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * es % 16 == 0 && ld <= kDmaMaxLd;
   };
-  a.dma = whole(a.P, a.ldp) && whole(a.Q, a.ldq);
-  const ProductPlan p = plan_product(a.I, a.J, a.K, a.elem, a.p_kc, a.q_kc, a.dma);
-  a.splits = p.splits;
-  if (p.shape == kFew) return launch_product_few(a, stream);
+  return whole(a.P, a.ldp) && whole(a.Q, a.ldq);
+}
+
+void set_launch(ProductArgs& a, const ProductPlan& p, float* partial) {
   const ShapeInfo& s = kInfo[p.shape];
+  a.splits = p.splits;
   a.k_split = p.k_split;
   a.partial = partial;
   a.tiles_i = static_cast<uint32_t>((a.I + s.bi - 1) / s.bi);
   a.tiles_j = static_cast<uint32_t>((a.J + s.bj - 1) / s.bj);
   const int64_t wgs = static_cast<int64_t>(a.tiles_i) * a.tiles_j * a.splits;
   a.per_xcd = static_cast<uint32_t>((wgs + kXcds - 1) / kXcds);
+}
+
+hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream) {
+  a.dma = rows_on_16(a);
+  const ProductPlan p = plan_product(a.I, a.J, a.K, a.elem, a.p_kc, a.q_kc, a.dma);
+  a.splits = p.splits;
+  if (p.shape == kFew) return launch_product_few(a, stream);
+  set_launch(a, p, partial);
   hipError_t e = a.elem == kF16 ? launch_product_f16(p.shape, a, stream)
                  : a.elem == kBF16 ? launch_product_bf16(p.shape, a, stream)
                                    : launch_product_e4m3(p.shape, a, stream);

@@ -1,0 +1,320 @@
+// The matrix product's kernel with epilogues of its own: sums and factors that stay on the
+// device (kExtra), and the two passes of cross entropy (kLoss, kGrad).
+#pragma once
+
+#include "product.h"
+
+namespace som {
+
+// out = alpha factor sum + beta residual (of a type of its own), and the same times half_scale
+// in the operands' type.
+struct ExtraArgs : ProductArgs {
+  const float* factor;       // or nullptr
+  float beta;
+  int res_type;
+  void* half;                // [I][ldh] or nullptr
+  int64_t ldh;
+  float half_scale;
+  // where *swap is not 0, P (or Q) is read from `swapped` instead
+  const int32_t* swap;       // or nullptr
+  const void* swapped;
+  int64_t ld_swapped;
+  bool swap_p;
+};
+
+// Scores v = alpha sum + bias of rows against J classes; of each row in each tile the largest and
+// the sum of exponentials below it, and the score of the row's label.
+struct LossArgs : ProductArgs {
+  const int32_t* labels;
+  float* part;               // [tiles_j][I] pairs
+  float* label_score;        // [I]; not written where the label is none of the classes
+};
+
+// g = dloss (exp(v - lse) - [label]) times *factor in the operands' type to out (whose rows are
+// padded to eight columns), and its unscaled sums over the tile's rows.
+struct GradArgs : ProductArgs {
+  const int32_t* labels;
+  const float *lse, *dloss, *factor;
+  int64_t first, classes;    // the first of these columns' classes, and all there are
+  float* column_part;        // [tiles_i][ld_column] or nullptr
+  int64_t ld_column;
+};
+
+template <>
+struct ModeArgs<kExtra> {
+  typedef ExtraArgs type;
+};
+template <>
+struct ModeArgs<kLoss> {
+  typedef LossArgs type;
+};
+template <>
+struct ModeArgs<kGrad> {
+  typedef GradArgs type;
+};
+
+// The plan of a kExtra product (no kernels of few rows), and the product with the join of a split
+// k axis.
+inline ProductPlan plan_extra(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma) {
+  return plan_product(I, J, K, elem, p_kc, q_kc, dma, false);
+}
+hipError_t launch_extra(ExtraArgs a, float* partial, hipStream_t stream);
+// The kernel alone; `a`, the mode's arguments, has its launch's fields.
+hipError_t launch_mode(int mode, int shape, const ProductArgs& a, hipStream_t stream);
+hipError_t launch_modes_f16(int mode, int shape, const ProductArgs& a, hipStream_t stream);
+hipError_t launch_modes_bf16(int mode, int shape, const ProductArgs& a, hipStream_t stream);
+
+// ---------------------------------------------------------------------------
+// kExtra
+// ---------------------------------------------------------------------------
+
+__device__ __forceinline__ RowTerms extra_terms(const ExtraArgs& a, float scale, int64_t i, int64_t j, int n) {
+  RowTerms r;
+  r.scale = scale;
+  r.residual[0] = r.residual[1] = u4{0, 0, 0, 0};
+  if (n <= 0 || !a.residual) return r;
+  float v[8];
+  if (a.res_type == kF32) {
+    load8(static_cast<const float*>(a.residual) + i * a.ldr + j, n, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.residual[e / 4][e % 4] = __float_as_uint(v[e]);
+  } else {
+    const uint16_t* p = static_cast<const uint16_t*>(a.residual) + i * a.ldr + j;
+    if (n == 8) {
+      r.residual[0] = *reinterpret_cast<const u4_at2*>(p);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (e < n) r.residual[0][e / 2] |= static_cast<uint32_t>(p[e]) << (16 * (e % 2));
+    }
+  }
+  return r;
+}
+
+template <bool kWhole>
+__device__ __forceinline__ void finish_extra(const ExtraArgs& a, int64_t i, int64_t j, int n, float (&v)[8],
+                                             const RowTerms& r) {
+  if (a.residual) {
+    float res[8] = {};
+    residual8(a.res_type, r, res);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = fmaf(a.beta, res[e], v[e] * r.scale);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= r.scale;
+  }
+  if (a.out) store8_as<kWhole>(a.out_type, a.out, i * a.ldo + j, n, v);
+  if (a.half) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= a.half_scale;
+    store8_as<false>(a.elem, a.half, i * a.ldh + j, n, v);
+  }
+}
+
+__device__ __forceinline__ void finish8_extra(const ExtraArgs& a, int64_t i, int64_t j, int n, float (&v)[8],
+                                              const RowTerms& r) {
+  if (n == 8)
+    finish_extra<true>(a, i, j, n, v, r);
+  else
+    finish_extra<false>(a, i, j, n, v, r);
+}
+
+__device__ __forceinline__ float extra_scale(const ExtraArgs& a) { return a.factor ? a.alpha * *a.factor : a.alpha; }
+
+template <class TileOf, int TI, int TJ>
+__device__ __forceinline__ void extra_tile(const TileOf& tile, const ExtraArgs& a, const f4 (&acc)[TI][TJ],
+                                           const TilePlace& place) {
+  if (a.splits > 1) return tile.part(a, acc, place.split);
+  constexpr int kAhead = TileOf::kAhead;
+  const float scale = extra_scale(a);
+  auto terms = [&](int g) __attribute__((always_inline)) {
+    const int64_t i = tile.first + g * TileOf::kRows;
+    return extra_terms(a, scale, i, tile.j, g < TileOf::kGroups && i < a.I ? tile.n : 0);
+  };
+  RowTerms ahead[kAhead];
+#pragma unroll
+  for (int g = 0; g < kAhead; ++g) ahead[g] = terms(g);
+  tile.rows(acc, [&](int g, int64_t i, float (&v)[8]) __attribute__((always_inline)) {
+    const RowTerms now = ahead[0];
+#pragma unroll
+    for (int k = 0; k + 1 < kAhead; ++k) ahead[k] = ahead[k + 1];
+    ahead[kAhead - 1] = terms(g + kAhead);
+    if (i < a.I && tile.n > 0) finish8_extra(a, i, tile.j, tile.n, v, now);
+  });
+}
+
+// ---------------------------------------------------------------------------
+// kLoss
+// ---------------------------------------------------------------------------
+
+// The largest m of some scores and s = sum exp(v - m), both pairs' (m = -infinity: none).
+__device__ __forceinline__ void join_max_sum(float& m, float& s, float m2, float s2) {
+  const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.0f : top;
+  s = s * __builtin_amdgcn_exp2f(kLog2e * (m - base)) + s2 * __builtin_amdgcn_exp2f(kLog2e * (m2 - base));
+  m = top;
+}
+
+// Straight from the matrix instructions' registers: a lane has 4 TJ scores of a row, the four lanes
+// 16 apart the wave's 16 TJ.  exp(v - m) as a power of two: its argument's rounding, |v - m| 2^-24,
+// is that of a difference of scores.
+template <class TileOf, int TI, int TJ>
+__device__ __forceinline__ void loss_tile(const TileOf& tile, const LossArgs& a, const f4 (&acc)[TI][TJ],
+                                          const TilePlace& place) {
+  if (a.splits > 1) return tile.part(a, acc, place.split);
+  constexpr int WI = TileOf::kWI, WJ = TileOf::kWJ, BI = WI * TI * 16;
+  const int wi = tile.wave / WJ, wj = tile.wave % WJ, g = tile.lane >> 4;
+  const int64_t j = tile.j0 + wj * TJ * 16 + g * 4;
+  float bias[TJ][4];
+#pragma unroll
+  for (int y = 0; y < TJ; ++y)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t at = j + y * 16 + e;
+      bias[y][e] = at >= a.J ? -INFINITY : a.bias ? a.bias[at] : 0.0f;
+    }
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef __attribute__((address_space(3))) f2 lds_f2;
+  lds_f2* const sums = reinterpret_cast<lds_f2*>(tile.lds);      // [WJ][BI]
+#pragma unroll
+  for (int x = 0; x < TI; ++x) {
+    const int row = (wi * TI + x) * 16 + (tile.lane & 15);
+    const int64_t i = tile.i0 + row;
+    const int64_t label = (i < a.I ? a.labels[i] : -1) - j;     // in this lane's columns: y * 16 + e
+    float v[TJ][4], m = -INFINITY, s = 0.0f;
+#pragma unroll
+    for (int y = 0; y < TJ; ++y)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        // past the classes: -infinity, whatever the sums there (which are of other columns)
+        v[y][e] = bias[y][e] == -INFINITY ? -INFINITY : fmaf(acc[x][y][e], a.alpha, bias[y][e]);
+        m = fmaxf(m, v[y][e]);
+        if (label == y * 16 + e && tile.j0 < a.J) a.label_score[i] = v[y][e];
+      }
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int y = 0; y < TJ; ++y)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f(kLog2e * (v[y][e] - base));
+    s += __shfl_xor(s, 16, 64);
+    s += __shfl_xor(s, 32, 64);
+    if (g == 0) sums[wj * BI + row] = f2{m, s};
+  }
+  __syncthreads();
+  if (threadIdx.x < BI && tile.i0 + threadIdx.x < a.I) {
+    f2 all = sums[threadIdx.x];
+    float m = all[0], s = all[1];
+#pragma unroll
+    for (int w = 1; w < WJ; ++w) {
+      const f2 one = sums[w * BI + threadIdx.x];
+      join_max_sum(m, s, one[0], one[1]);
+    }
+    f2* const part = reinterpret_cast<f2*>(a.part);
+    part[place.tj * a.I + tile.i0 + threadIdx.x] = f2{m, s};
+  }
+}
+
+// ---------------------------------------------------------------------------
+// kGrad
+// ---------------------------------------------------------------------------
+
+struct GradRow {
+  int64_t label;             // among the eight columns' classes, counted from their first
+  float lse, dloss;          // dloss: 0 where the row has no label, or no score to choose from
+};
+
+__device__ __forceinline__ GradRow grad_row(const GradArgs& a, int64_t i, int64_t j, bool in) {
+  GradRow r = {-1, 0.0f, 0.0f};
+  if (!in) return r;
+  const int64_t label = a.labels[i];
+  const float lse = a.lse[i];
+  if (label < 0 || label >= a.classes || lse == -INFINITY) return r;
+  r.label = label - a.first - j;
+  r.lse = lse;
+  r.dloss = a.dloss[i];
+  return r;
+}
+
+// g of eight columns from their sums, in place; a row without a label gives zeros whatever its sums.
+__device__ __forceinline__ void grad8(const GradArgs& a, const GradRow& r, const float (&bias)[8], float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float z = bias[e] == -INFINITY ? -INFINITY : fmaf(v[e], a.alpha, bias[e]);
+    const float p = __builtin_amdgcn_exp2f(kLog2e * (z - r.lse));
+    v[e] = r.dloss == 0.0f ? 0.0f : r.dloss * (r.label == e ? p - 1.0f : p);
+  }
+}
+
+template <class TileOf, int TI, int TJ>
+__device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a, const f4 (&acc)[TI][TJ],
+                                          const TilePlace& place) {
+  if (a.splits > 1) return tile.part(a, acc, place.split);
+  constexpr int kAhead = TileOf::kAhead, kLanes = TileOf::kLanes, WI = TileOf::kWI, WJ = TileOf::kWJ;
+  constexpr int BJ = WJ * TJ * 16;
+  float bias[8], sums[8] = {};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) bias[e] = 0.0f;
+  if (a.bias) load8(a.bias + tile.j, tile.n, bias);
+  const float factor = *a.factor;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(bias[e]));
+  auto terms = [&](int g) __attribute__((always_inline)) {
+    const int64_t i = tile.first + g * TileOf::kRows;
+    return grad_row(a, i, tile.j, g < TileOf::kGroups && i < a.I && tile.n > 0);
+  };
+  GradRow ahead[kAhead];
+#pragma unroll
+  for (int g = 0; g < kAhead; ++g) ahead[g] = terms(g);
+  tile.rows(acc, [&](int g, int64_t i, float (&v)[8]) __attribute__((always_inline)) {
+    const GradRow now = ahead[0];
+#pragma unroll
+    for (int k = 0; k + 1 < kAhead; ++k) ahead[k] = ahead[k + 1];
+    ahead[kAhead - 1] = terms(g + kAhead);
+    if (i >= a.I || tile.n <= 0) return;
+    grad8(a, now, bias, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      sums[e] += v[e];
+      v[e] *= factor;
+    }
+    if (a.elem == kF16)
+      store8(static_cast<f16*>(a.out) + i * a.ldo + tile.j, 8, v);
+    else
+      store8(static_cast<bf16*>(a.out) + i * a.ldo + tile.j, 8, v);
+  });
+  if (!a.column_part) return;
+  // over the lanes that share the columns, then over the waves below each other, in order
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int off = kLanes; off < 64; off <<= 1) sums[e] += __shfl_xor(sums[e], off, 64);
+  __syncthreads();
+  typedef __attribute__((address_space(3))) float lds_float;
+  lds_float* const all = reinterpret_cast<lds_float*>(tile.lds);      // [WI][BJ]
+  if (tile.lane < kLanes) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) all[tile.wave / WJ * BJ + tile.wave % WJ * TJ * 16 + tile.lane * 8 + e] = sums[e];
+  }
+  __syncthreads();
+  const int64_t j = tile.j0 + threadIdx.x;
+  if (threadIdx.x < BJ && j < a.J) {
+    float s = all[threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < WI; ++w) s += all[w * BJ + threadIdx.x];
+    a.column_part[place.ti * a.ld_column + j] = s;
+  }
+}
+
+template <int MODE, class TileOf, int TI, int TJ>
+__device__ __forceinline__ void finish_mode(const TileOf& tile, const typename ModeArgs<MODE>::type& a,
+                                            const f4 (&acc)[TI][TJ], const TilePlace& place) {
+  if constexpr (MODE == kExtra)
+    extra_tile(tile, a, acc, place);
+  else if constexpr (MODE == kLoss)
+    loss_tile(tile, a, acc, place);
+  else
+    grad_tile(tile, a, acc, place);
+}
+
+}  // namespace som

@@ -38,15 +38,6 @@ __device__ __forceinline__ int left(int64_t cols, int64_t c) {
   return cols - c >= 8 ? 8 : cols > c ? static_cast<int>(cols - c) : 0;
 }
 
-// The factor of a row's 8-bit values from the bits of its largest |y| (as unsigned
-// words NaN is above every number, so a NaN anywhere reaches the factor).  At least the
-// smallest normal number, whose inverse is finite.
-__device__ __forceinline__ float q8_scale(uint32_t top) {
-  constexpr float kLeast = 1.17549435e-38f;             // 2^-126
-  const float scale = __uint_as_float(top) / kE4M3Max;
-  return top == 0 ? 1.0f : scale < kLeast ? kLeast : scale;
-}
-
 // G threads per row, R rows per workgroup, U groups of eight columns per thread;
 // G * U * 8 >= cols.
 template <typename T, bool Q8, int G, int R, int U>

@@ -63,6 +63,11 @@ EXPORTS = (
     "som_product_backward_workspace_bytes",
     "som_product_backward",
     "som_dropout",
+    "som_quantise",
+    "som_cross_entropy_workspace_bytes",
+    "som_cross_entropy",
+    "som_cross_entropy_backward_workspace_bytes",
+    "som_cross_entropy_backward",
 )
 
 # som_dtype and som_act
@@ -207,6 +212,18 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.som_dropout.restype = _i32
     lib.som_dropout.argtypes = [_vp, _i64, _vp, _i64, _i32, _i64, _i64, ctypes.c_double, ctypes.c_uint64,
                                 ctypes.c_uint64, _vp, _i64, _vp]
+    lib.som_quantise.restype = _i32
+    lib.som_quantise.argtypes = [_vp, _i64, _i32, _i64, _i64, _i32, _i32, _vp, _i64, _vp, _i64, _i64, _vp]
+    for name in ("som_cross_entropy_workspace_bytes", "som_cross_entropy_backward_workspace_bytes"):
+        fn = getattr(lib, name)
+        fn.restype = _sz
+        fn.argtypes = [_i64, _i64, _i64, _i32]
+    lib.som_cross_entropy.restype = _i32
+    lib.som_cross_entropy.argtypes = [_vp, _i64, _vp, _i64, _i32, _i32, _i64, _i64, _i64, _vp, _vp, ctypes.c_float, _vp,
+                                      _vp, _vp, _sz, _vp]
+    lib.som_cross_entropy_backward.restype = _i32
+    lib.som_cross_entropy_backward.argtypes = [_vp, _vp, _i64, _vp, _i64, _i32, _i32, _i64, _i64, _i64, _vp, _vp,
+                                               ctypes.c_float, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _sz, _vp]
     _lib = lib
     return lib
 
@@ -969,3 +986,131 @@ def som_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual:
     yp, ldy = _rows(y, "y", x.dtype, shape, device)
     _check(lib.som_dropout(xp, ldx, rp, ldr, dt, rows, cols, p, seed, offset, yp, ldy, _raw_stream(device, stream)))
     return y
+
+
+def _blocks(n: int) -> int:
+    return (n + 127) // 128
+
+
+def som_quantise(x: torch.Tensor, block_rows: int = 1, transpose: bool = False, q: Optional[torch.Tensor] = None,
+                 scale: Optional[torch.Tensor] = None, stream=None):
+    """(q, scale): x (or its transpose) in float8_e4m3fn with an fp32 factor for each block of
+    128 elements of a row (block_rows 1) or of 128 x 128 (block_rows 128), for
+    som_product_blocks.  scale [rows of q / block_rows, columns of q / 128], rounded up, has the
+    factors of one block of columns next to each other unless given otherwise."""
+    lib = load()
+    dt = _float_type(x, "x", _FLOATS)
+    xp, ldx = _rows(x, "x")
+    device = x.get_device()
+    if torch._C._cuda_getDevice() != device:       # a launch goes to the current one
+        with torch.cuda.device(device):
+            return som_quantise(x, block_rows, transpose, q, scale, stream)
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows must be 1 or 128")
+    rows, cols = x.shape
+    qr, qc = (cols, rows) if transpose else (rows, cols)
+    if q is None:
+        q = _new((qr, qc), torch.float8_e4m3fn, x.device, stream)
+    qp, ldq = _rows(q, "q", torch.float8_e4m3fn, (qr, qc), device)
+    shape = (qr if block_rows == 1 else _blocks(qr), _blocks(qc))
+    if scale is None:
+        scale = _new((shape[1], shape[0]), torch.float32, x.device, stream).t()
+    sp, sr, sb = _factors(scale, "scale", shape, device)
+    _check(lib.som_quantise(xp, ldx, dt, rows, cols, block_rows, 1 if transpose else 0, qp, ldq, sp, sr, sb,
+                            _raw_stream(device, stream)))
+    return q, scale
+
+
+def _factors(t: torch.Tensor, name: str, shape, device: int):
+    """Check the factors of a matrix in blocks; return their pointer and strides."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device} like the first tensor (got {t.device})")
+    if t.dtype != torch.float32:
+        raise TypeError(f"{name} must be {torch.float32} (got {t.dtype})")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {shape[0]} x {shape[1]} (got {' x '.join(str(n) for n in t.shape)})")
+    row, block = t.stride()
+    return t.data_ptr(), row if shape[0] > 1 else max(row, 1), block if shape[1] > 1 else max(block, 1)
+
+
+def som_cross_entropy_workspace_bytes(M: int, N: int, K: int, dtype=torch.bfloat16) -> int:
+    return int(load().som_cross_entropy_workspace_bytes(M, N, K, DTYPES[dtype]))
+
+
+def som_cross_entropy(x: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                      alpha: float = 1.0, loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                      ws: Optional[torch.Tensor] = None, stream=None):
+    """(loss, lse) of each document: lse = log sum exp of its scores alpha (x @ W) + bias, loss =
+    lse minus the score of its label.
+
+    x [M, K] and W [K, N] in fp16 or bf16, W in either of som_product's layouts; labels [M]
+    int32 (as som_bmu_search gives units), none where outside [0, N): loss 0.  bias [N], loss and
+    lse [M] are fp32.  The scores are not kept; lse is what the gradient needs."""
+    lib = load()
+    dt = _float_type(x, "x", _HALVES)
+    xp, ldx = _rows(x, "x")
+    device = x.get_device()
+    if torch._C._cuda_getDevice() != device:       # a launch goes to the current one
+        with torch.cuda.device(device):
+            return som_cross_entropy(x, W, labels, bias, alpha, loss, lse, ws, stream)
+    M, K = x.shape
+    Wp, ldw, units = _weights(W, "W", x.dtype, device)
+    if W.shape[0] != K:
+        raise ValueError(f"x has {K} columns and W {W.shape[0]} rows")
+    N = W.shape[1]
+    if loss is None:
+        loss = _new(M, torch.float32, x.device, stream)
+    if lse is None:
+        lse = _new(M, torch.float32, x.device, stream)
+    ws, wsp, n = _scratch(ws, lib.som_cross_entropy_workspace_bytes(M, N, K, dt), x.device, stream)
+    _check(lib.som_cross_entropy(xp, ldx, Wp, ldw, units, dt, M, N, K, _vector(labels, "labels", M, device, torch.int32),
+                                 _vector(bias, "bias", N, device), alpha, _vector(loss, "loss", M, device),
+                                 _vector(lse, "lse", M, device), wsp, n, _raw_stream(device, stream)))
+    return loss, lse
+
+
+def som_cross_entropy_backward_workspace_bytes(M: int, N: int, K: int, dtype=torch.bfloat16) -> int:
+    return int(load().som_cross_entropy_backward_workspace_bytes(M, N, K, DTYPES[dtype]))
+
+
+def som_cross_entropy_backward(dloss: torch.Tensor, x: torch.Tensor, W: torch.Tensor, labels: torch.Tensor,
+                               lse: torch.Tensor, bias: Optional[torch.Tensor] = None, alpha: float = 1.0,
+                               dx: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None,
+                               dbias: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None,
+                               need_dx: bool = True, need_dW: bool = True, need_dbias: bool = True):
+    """(dx, dW, dbias) of som_cross_entropy from the gradient ``dloss`` [M] of each loss and the
+    lse that it returned; dx and dW (laid out as W is) in x's type, dbias fp32.  One that is
+    not needed is None, and its product or sum is left out."""
+    lib = load()
+    dt = _float_type(x, "x", _HALVES)
+    xp, ldx = _rows(x, "x")
+    device = x.get_device()
+    if torch._C._cuda_getDevice() != device:       # a launch goes to the current one
+        with torch.cuda.device(device):
+            return som_cross_entropy_backward(dloss, x, W, labels, lse, bias, alpha, dx, dW, dbias, ws, stream, need_dx,
+                                              need_dW, need_dbias)
+    M, K = x.shape
+    Wp, ldw, units = _weights(W, "W", x.dtype, device)
+    if W.shape[0] != K:
+        raise ValueError(f"x has {K} columns and W {W.shape[0]} rows")
+    N = W.shape[1]
+    for need, given, name in ((need_dx, dx, "dx"), (need_dW, dW, "dW"), (need_dbias, dbias, "dbias")):
+        _unwanted(need, given, name)
+    if need_dx and dx is None:
+        dx = _new((M, K), x.dtype, x.device, stream)
+    dxp, lddx = (None, 0) if dx is None else _rows(dx, "dx", x.dtype, (M, K), device)
+    if need_dW and dW is None:
+        dW = _new((N, K), x.dtype, x.device, stream).t() if units else _new((K, N), x.dtype, x.device, stream)
+    dWp, lddw = (None, 0) if dW is None else _rows(dW.t() if units else dW, "dW", x.dtype,
+                                                   (N, K) if units else (K, N), device)
+    if need_dbias and dbias is None:
+        dbias = _new(N, torch.float32, x.device, stream)
+    ws, wsp, n = _scratch(ws, lib.som_cross_entropy_backward_workspace_bytes(M, N, K, dt), x.device, stream)
+    _check(lib.som_cross_entropy_backward(_vector(dloss, "dloss", M, device), xp, ldx, Wp, ldw, units, dt, M, N, K,
+                                          _vector(labels, "labels", M, device, torch.int32),
+                                          _vector(bias, "bias", N, device), alpha, _vector(lse, "lse", M, device), dxp,
+                                          lddx, dWp, lddw, _vector(dbias, "dbias", N, device), wsp, n,
+                                          _raw_stream(device, stream)))
+    return dx, dW, dbias

@@ -1,0 +1,360 @@
+"""Cross entropy and its gradients on the GPU against the fp64 oracle.
+
+Tolerances (u = 2^-24, t = half a unit of x's type):
+  a score, a sum of K fp32 products, is within 2 K u of the sum of their magnitudes (the matrix
+  cores add them) and u of itself and of its bias: dv;
+  lse is within the largest dv of its document, the exponentials' and the logarithm's 2^-18 (a
+  power of two whose argument is off by |v - max| u, weighted by itself, and units of
+  fp32), the sum's depth (N / 16 + 64) u, and 2 u of itself;
+  a probability is within dv + dlse + 2^-18 of itself; g adds t of itself where it is rounded for
+  the products, the products 2 n u of the magnitudes, each output its own t."""
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from oracle import train as oracle  # noqa: E402
+
+if torch.cuda.is_available():
+    import paper_2609_05138_amd as som
+else:  # collected on CPU-only machines, never run there
+    som = None
+
+DEV = "cuda:0"
+T = {"f16": torch.float16, "bf16": torch.bfloat16}
+HALF = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f16": 2.0 ** -24, "bf16": 2.0 ** -126}
+U = 2.0 ** -24
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _view(values, dtype, pad, fill=float("nan")):
+    """values as a view into a wider array whose other columns hold `fill`."""
+    rows, cols = values.shape
+    wide = torch.full((rows, cols + pad), fill, dtype=torch.float32, device=DEV).to(dtype)
+    wide[:, :cols] = torch.as_tensor(values, dtype=torch.float32, device=DEV).to(dtype)
+    return wide[:, :cols]
+
+
+def _near(got, want, tol, what):
+    got = _np(got)
+    with np.errstate(invalid="ignore"):
+        bad = ~((np.abs(got - want) <= tol) | (got == want))
+    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4],
+                           np.broadcast_to(tol, want.shape)[bad][:4])
+
+
+def _inputs(M, N, K, kind, layout, pad=0, seed=0, spread=1.0, ignored=0.2):
+    rng = np.random.default_rng(seed + M * 31 + N * 7 + K)
+    x = _view(rng.normal(size=(M, K)), T[kind], pad)
+    W = rng.normal(size=(N, K)) * spread * K ** -0.5
+    W = _view(W, T[kind], pad).t() if layout == "unit" else _view(W.T, T[kind], pad)
+    labels = rng.integers(0, N, M)
+    labels[rng.random(M) < ignored] = -1
+    if M > 4:
+        labels[1], labels[2] = N, 2 ** 31 - 1              # no classes either
+    bias = torch.as_tensor(rng.normal(size=N) * 0.3, dtype=torch.float32, device=DEV)
+    dloss = torch.as_tensor(rng.uniform(0.5, 1.5, M) / M, dtype=torch.float32, device=DEV)
+    return x, W, torch.as_tensor(labels, dtype=torch.int32, device=DEV), bias, dloss
+
+
+def _dv(x, W, v, bias, alpha):
+    K = x.shape[1]
+    return np.abs(alpha) * 2 * K * U * (np.abs(x) @ np.abs(W)) + 2 * U * (np.abs(v) + (0 if bias is None else np.abs(bias)))
+
+
+def _check(x, W, labels, bias, dloss, alpha, kind):
+    xn, Wn, ln, bn = _np(x), _np(W), labels.cpu().numpy().astype(np.int64), None if bias is None else _np(bias)
+    loss, lse = som.som_cross_entropy(x, W, labels, bias, alpha)
+    want, want_lse = oracle.cross_entropy(xn, Wn, ln, bn, alpha)
+    v = oracle.scores(xn, Wn, bn, alpha)
+    N, K = v.shape[1], xn.shape[1]
+    dv = _dv(xn, Wn, v, bn, alpha)
+    dlse = dv.max(1) + 2.0 ** -18 + (N / 16 + 64) * U + 2 * U * np.abs(want_lse)
+    _near(lse, want_lse, dlse, "lse")
+    has = (ln >= 0) & (ln < N)
+    own = np.where(has, dv[np.arange(len(v)), np.where(has, ln, 0)], 0.0)
+    _near(loss, want, has * (dlse + own + 2 * U * np.abs(want)), "loss")
+
+    dx, dW, dbias = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias, alpha)
+    wx, wW, wb, g = oracle.cross_entropy_backward(_np(dloss), xn, Wn, ln, bn, alpha)
+    assert dx.dtype == x.dtype and dW.dtype == x.dtype and dbias.dtype == torch.float32 and dW.stride(0) == (1 if W.stride(0) == 1 and W.shape[0] > 1 else dW.stride(0))
+    d = _np(dloss)[:, None]
+    p = np.where(has[:, None], np.exp(v - want_lse[:, None]), 0.0) * np.abs(d)
+    dg = p * (np.expm1(dv + dlse[:, None]) + 2.0 ** -18) + 4 * U * np.abs(g)
+    M = len(v)
+    _near(dbias, wb, dg.sum(0) + (M + 8) * U * np.abs(g).sum(0), "dbias")
+    # rounded for the products: the smallest fp16 step of g scaled so that max |dloss| is 2^14 at least
+    dg = dg + HALF[kind] * np.abs(g) + (2.0 ** -25 * np.abs(d).max() / 2.0 ** 13 if kind == "f16" else 0.0)
+    ax, aW = np.abs(xn), np.abs(Wn)
+    _near(dx, wx, abs(alpha) * (dg @ aW.T + 2 * N * U * (np.abs(g) @ aW.T)) * (1 + HALF[kind]) + HALF[kind] * np.abs(wx)
+          + TINY[kind] + 4 * U * np.abs(wx), "dx")
+    _near(dW, wW, abs(alpha) * (ax.T @ dg + 2 * M * U * (ax.T @ np.abs(g))) * (1 + HALF[kind]) + HALF[kind] * np.abs(wW)
+          + TINY[kind] + 4 * U * np.abs(wW), "dW")
+    assert not dx[~torch.as_tensor(has, device=DEV)].any()
+    return loss, lse, dx, dW, dbias
+
+
+SHAPES = [(1, 1, 1), (1, 2, 5), (2, 1, 64), (3, 7, 1), (4, 300, 64), (5, 1000, 72), (17, 129, 200), (33, 257, 129),
+          (64, 1024, 512), (100, 777, 65), (130, 4097, 63), (257, 255, 1030), (300, 3001, 96), (515, 2051, 40),
+          (1001, 777, 500), (2, 9000, 33), (1, 5000, 2100), (20, 520, 6000)]
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("layout", ["feature", "unit"])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_loss_and_gradients(M, N, K, layout, kind):
+    x, W, labels, bias, dloss = _inputs(M, N, K, kind, layout, pad=(M + N) % 3 * 4)
+    _check(x, W, labels, bias, dloss, 1.0, kind)
+
+
+@pytest.mark.parametrize("layout", ["feature", "unit"])
+@pytest.mark.parametrize("alpha,spread,with_bias", [(-2.0, 1.0, True), (0.05, 8.0, False), (1.0, 12.0, True), (0.0, 1.0, True)])
+def test_scales_and_wide_scores(alpha, spread, with_bias, layout):
+    x, W, labels, bias, dloss = _inputs(200, 600, 256, "bf16", layout, spread=spread)
+    _check(x, W, labels, bias if with_bias else None, dloss, alpha, "bf16")
+
+
+def test_large_tiles():
+    # 256 x 256 and 256 x 128 tiles, columns and rows that end inside them
+    for M, N, K in ((1000, 20001, 64), (2049, 6000, 128), (4100, 2056, 64)):
+        x, W, labels, bias, dloss = _inputs(M, N, K, "f16", "unit" if N % 2 else "feature")
+        _check(x, W, labels, bias, dloss, 0.7, "f16")
+
+
+def _double(x, W, labels, bias, alpha, dloss):
+    """The definition in 64 bits on the device."""
+    X, V = x.double(), W.double().contiguous()
+    v = alpha * torch.mm(X, V) + bias.double()
+    lse = torch.logsumexp(v, 1)
+    has = (labels >= 0) & (labels < W.shape[1])
+    rows = torch.arange(len(v), device=DEV)
+    own = v[rows, labels.clamp(0, W.shape[1] - 1).long()]
+    g = torch.exp(v - lse[:, None])
+    g[rows[has], labels[has].long()] -= 1.0
+    g *= (dloss.double() * has)[:, None]
+    return (lse - own) * has, lse, alpha * torch.mm(g, V.t().contiguous()), alpha * torch.mm(X.t().contiguous(), g), g.sum(0)
+
+
+def _far(got, want):
+    return float((got.double() - want).norm() / want.norm())
+
+
+def test_pieces_of_the_classes_and_rows():
+    # more classes than a piece of g holds (2^28 bytes), and more documents than one launch's pairs
+    M, N, K = 66000, 5000, 24
+    x, W, labels, bias, dloss = _inputs(M, N, K, "bf16", "feature")
+    loss, lse = som.som_cross_entropy(x, W, labels, bias)
+    dx, dW, dbias = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias)
+    want = _double(x, W, labels, bias, 1.0, dloss)
+    # norms of many rounded values: each within its half step (2^-8) and a rounded g's (2^-8) at
+    # the most, so the whole within 2^-7; the fp32 outputs within 2^-17
+    for got, w, tol in zip((loss, lse, dx, dW, dbias), want, (2.0 ** -17, 2.0 ** -17, 2.0 ** -7, 2.0 ** -7, 2.0 ** -17)):
+        assert _far(got, w) <= tol
+    assert float((lse.double() - want[1]).abs().max()) < 1e-4
+    # the rows one by one near the seams
+    for i in (0, 65535, 65536, M - 1):
+        one = som.som_cross_entropy(x[i:i + 1], W, labels[i:i + 1], bias)
+        assert abs(float(one[1]) - float(lse[i])) < 1e-5
+    assert bool((dx.float()[labels < 0] == 0).all())
+
+
+def test_gradients_against_differences():
+    M, N, K = 6, 40, 16
+    x, W, labels, bias, dloss = _inputs(M, N, K, "f16", "feature", ignored=0.0)
+    labels = labels.clamp(max=N - 1)
+    dloss = dloss * M
+    _, lse = som.som_cross_entropy(x, W, labels, bias)
+    dx, dW, dbias = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias)
+    xn, Wn, bn, ln, dn = _np(x), _np(W), _np(bias), labels.cpu().numpy(), _np(dloss)
+    f = lambda a, b, c: float((oracle.cross_entropy(a, b, ln, c)[0] * dn).sum())  # noqa: E731
+    h = 1e-5
+    rng = np.random.default_rng(3)
+    for got, which in ((dx, 0), (dW, 1), (dbias, 2)):
+        base = (xn, Wn, bn)
+        for _ in range(12):
+            at = tuple(rng.integers(0, s) for s in base[which].shape)
+            up, down = [a.copy() for a in base], [a.copy() for a in base]
+            up[which][at] += h
+            down[which][at] -= h
+            want = (f(*up) - f(*down)) / (2 * h)
+            # g and the result in fp16, sums of up to 40 terms of about one
+            assert abs(float(got[at]) - want) <= 2.0 ** -9 * (abs(want) + 1.0)
+
+
+def test_classes_left_out_and_rows_without_any():
+    M, N, K = 70, 500, 64
+    for layout in ("feature", "unit"):
+        x, W, labels, bias, dloss = _inputs(M, N, K, "bf16", layout, ignored=0.0)
+        labels = labels.clamp(max=N - 1)
+        out = torch.zeros(N, dtype=torch.bool, device=DEV)
+        out[::3] = True
+        out[256:400] = True                      # a whole tile's columns of some shapes
+        bias[out] = float("-inf")
+        inside = torch.nonzero(~out)[:, 0].int()
+        labels = inside[labels.long() % len(inside)]
+        labels[5] = 0                            # a label that is left out
+        loss, lse = som.som_cross_entropy(x, W, labels, bias)
+        assert float(loss[5]) == float("inf") and bool(lse.isfinite().all())
+        want, want_lse = oracle.cross_entropy(_np(x), _np(W), labels.cpu().numpy(), _np(bias))
+        _near(lse, want_lse, 1e-4, "lse")
+        _near(loss, want, 1e-4, "loss")
+        dx, dW, dbias = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias)
+        wx, wW, wb, _ = oracle.cross_entropy_backward(_np(dloss), _np(x), _np(W), labels.cpu().numpy(), _np(bias))
+        keep = torch.ones(N, dtype=torch.bool, device=DEV)
+        keep[0] = False
+        assert bool((dbias[out & keep] == 0).all()) and bool((dW.float()[:, out & keep] == 0).all())
+        assert _far(dx, torch.as_tensor(wx, device=DEV)) < 2.0 ** -7 and _far(dW, torch.as_tensor(wW, device=DEV)) < 2.0 ** -7
+        assert _far(dbias, torch.as_tensor(wb, device=DEV)) < 2.0 ** -17
+        # no class left at all
+        bias[:] = float("-inf")
+        loss, lse = som.som_cross_entropy(x, W, labels, bias)
+        assert bool((lse == float("-inf")).all()) and bool((loss == float("inf")).all())
+        for t in som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias):
+            assert not t.any()
+        for m in (1, 3, 20):                     # the kernels of few rows
+            loss, lse = som.som_cross_entropy(x[:m], W, labels[:m], bias)
+            assert bool((lse == float("-inf")).all()) and bool((loss == float("inf")).all())
+
+
+@pytest.mark.parametrize("layout", ["feature", "unit"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_rows_that_count_for_nothing_may_hold_anything(bad, layout):
+    M, N, K = 300, 700, 136
+    x, W, labels, bias, dloss = _inputs(M, N, K, "f16", layout, ignored=0.3)
+    has = (labels >= 0) & (labels < N)
+    dloss[has.nonzero()[0, 0]] = 0.0
+    none = ~has | (dloss == 0)
+    _, lse = som.som_cross_entropy(x, W, labels, bias)
+    want = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias)
+    dirty = x.clone()
+    dirty[none, 3] = bad
+    dirty[none.nonzero()[-1, 0]] = bad
+    loss, lse = som.som_cross_entropy(dirty, W, labels, bias)
+    assert bool((loss[~has] == 0).all()) and bool(lse[~none].isfinite().all())
+    got = som.som_cross_entropy_backward(dloss, dirty, W, labels, lse, bias)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    assert not got[0][none].any()
+    # a row that counts makes its own results NaN, and what all rows share
+    i = int((~none).nonzero()[0, 0])
+    dirty = x.clone()
+    dirty[i, 0] = float("nan")
+    loss, lse = som.som_cross_entropy(dirty, W, labels, bias)
+    assert bool(loss[i].isnan()) and int(lse.isnan().sum()) == 1
+    dx, dW, dbias = som.som_cross_entropy_backward(dloss, dirty, W, labels, lse, bias)
+    assert bool(dx[i].isnan().all()) and torch.equal(dx[:i], want[0][:i]) and torch.equal(dx[i + 1:], want[0][i + 1:])
+    assert bool(dbias.isnan().all())
+
+
+def test_small_gradients_reach_fp16():
+    # dloss of 2^-20 and probabilities of 1 / 4096: g is far below fp16's range, x is large
+    M, N, K = 64, 4096, 64
+    x, W, labels, bias, dloss = _inputs(M, N, K, "f16", "unit", ignored=0.0)
+    labels = labels.clamp(max=N - 1)
+    _, lse = som.som_cross_entropy(x, W, labels, None)
+    one = som.som_cross_entropy_backward(torch.full((M,), 1.0, device=DEV), x, W, labels, lse)
+    tiny = som.som_cross_entropy_backward(torch.full((M,), 2.0 ** -20, device=DEV), x, W, labels, lse)
+    assert torch.equal(one[2] * 2.0 ** -20, tiny[2])
+    # the same sums, rounded once to fp16's smallest step (2^-24) here and to 11 bits and then to
+    # that step there: an 11-bit rounding is at most half a step of that size off a tie, so the two
+    # are one step apart at the most
+    for a, b in zip(one[:2], tiny[:2]):
+        assert bool(b.any()) and bool(((a.double() * 2.0 ** -20).half().double() - b.double()).abs().max() <= 2.0 ** -24)
+
+
+def test_only_what_is_needed_and_given_outputs():
+    M, N, K = 90, 333, 200
+    x, W, labels, bias, dloss = _inputs(M, N, K, "bf16", "unit", pad=8)
+    loss, lse = (torch.empty(M, device=DEV) for _ in range(2))
+    got = som.som_cross_entropy(x, W, labels, bias, loss=loss, lse=lse)
+    assert got[0] is loss and got[1] is lse
+    full = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias)
+    for need in ((True, False, False), (False, True, False), (False, False, True), (False, False, False)):
+        part = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias, need_dx=need[0], need_dW=need[1],
+                                              need_dbias=need[2])
+        for a, b, n in zip(part, full, need):
+            assert (a is None) if not n else torch.equal(a, b)
+    wide = torch.full((M, K + 8), 7.0, dtype=torch.bfloat16, device=DEV)
+    wideW = torch.full((N, K + 24), 7.0, dtype=torch.bfloat16, device=DEV)
+    dx, dW, _ = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias, dx=wide[:, :K], dW=wideW[:, :K].t())
+    assert torch.equal(dx, full[0]) and torch.equal(dW, full[1])
+    assert bool((wide[:, K:] == 7).all()) and bool((wideW[:, K:] == 7).all())
+
+
+def test_empty_batches():
+    x, W, labels, bias, dloss = _inputs(8, 50, 32, "f16", "feature")
+    loss, lse = som.som_cross_entropy(x[:0], W, labels[:0], bias)
+    assert loss.shape == lse.shape == (0,)
+    dx, dW, dbias = som.som_cross_entropy_backward(dloss[:0], x[:0], W, labels[:0], lse, bias)
+    assert dx.shape == (0, 32) and not dW.any() and not dbias.any()
+
+
+def test_same_bits_again_and_on_streams_and_in_graphs():
+    M, N, K = 300, 2500, 264
+    x, W, labels, bias, dloss = _inputs(M, N, K, "bf16", "feature")
+    loss, lse = som.som_cross_entropy(x, W, labels, bias)
+    back = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias)
+    again = som.som_cross_entropy(x, W, labels, bias)
+    assert torch.equal(again[0], loss) and torch.equal(again[1], lse)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    a, b = som.som_cross_entropy(x, W, labels, bias, stream=side)
+    c = som.som_cross_entropy_backward(dloss, x, W, labels, b, bias, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(a, loss) and all(torch.equal(p, q) for p, q in zip(c, back))
+    # captured with buffers of its own, replayed on new inputs, eager work between
+    X, D, Lb = x.clone(), dloss.clone(), labels.clone()
+    ws = torch.empty(som.som_cross_entropy_workspace_bytes(M, N, K), dtype=torch.uint8, device=DEV)
+    ws2 = torch.empty(som.som_cross_entropy_backward_workspace_bytes(M, N, K), dtype=torch.uint8, device=DEV)
+    out = [torch.empty(M, device=DEV), torch.empty(M, device=DEV), torch.empty_like(X), torch.empty((K, N), dtype=X.dtype, device=DEV),
+           torch.empty(N, device=DEV)]
+
+    def step():
+        som.som_cross_entropy(X, W, Lb, bias, loss=out[0], lse=out[1], ws=ws)
+        som.som_cross_entropy_backward(D, X, W, Lb, out[1], bias, dx=out[2], dW=out[3], dbias=out[4], ws=ws2)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(3):
+        X.copy_(x * (1.0 + 0.25 * k))
+        D.copy_(dloss * (k + 1))
+        Lb.copy_(labels.roll(k))
+        graph.replay()
+        torch.cuda.synchronize()
+        wl, we = som.som_cross_entropy(X, W, Lb, bias)
+        want = (wl, we, *som.som_cross_entropy_backward(D, X, W, Lb, we, bias))
+        for p, q in zip(out, want):
+            assert torch.equal(p, q), k
+
+
+def test_refusals():
+    x, W, labels, bias, dloss = _inputs(8, 50, 32, "f16", "feature")
+    loss, lse = som.som_cross_entropy(x, W, labels, bias)
+    fails = [(TypeError, lambda: som.som_cross_entropy(x.float(), W, labels)),
+             (TypeError, lambda: som.som_cross_entropy(x, W.bfloat16(), labels)),
+             (TypeError, lambda: som.som_cross_entropy(x, W, labels.long())),
+             (ValueError, lambda: som.som_cross_entropy(x, W, labels[:7])),
+             (ValueError, lambda: som.som_cross_entropy(x[:, :31], W, labels)),
+             (ValueError, lambda: som.som_cross_entropy(x, W, labels, bias[:49])),
+             (ValueError, lambda: som.som_cross_entropy(x, W, labels, lse=lse[:7])),
+             (som.SomError, lambda: som.som_cross_entropy(x, W, labels, alpha=float("nan"))),
+             (som.SomError, lambda: som.som_cross_entropy(x, W, None)),
+             (som.SomError, lambda: som.som_cross_entropy(x, W, labels, ws=torch.empty(8, dtype=torch.uint8, device=DEV))),
+             (ValueError, lambda: som.som_cross_entropy_backward(dloss[:7], x, W, labels, lse)),
+             (ValueError, lambda: som.som_cross_entropy_backward(dloss, x, W, labels, lse[:7])),
+             (TypeError, lambda: som.som_cross_entropy_backward(dloss.double(), x, W, labels, lse)),
+             (TypeError, lambda: som.som_cross_entropy_backward(dloss, x, W, labels, lse, dx=x.float())),
+             (ValueError, lambda: som.som_cross_entropy_backward(dloss, x, W, labels, lse, dx=x, need_dx=False)),
+             (som.SomError, lambda: som.som_cross_entropy_backward(None, x, W, labels, lse))]
+    for error, call in fails:
+        with pytest.raises(error):
+            call()
