@@ -636,6 +636,34 @@ som_status som_quantise(const void* x, int64_t ldx, int32_t dtype, int64_t rows,
                         int32_t transpose, void* q, int64_t ldq, float* scale, int64_t scale_row,
                         int64_t scale_block, hipStream_t stream);
 
+/* Matrix product of operands in 8 bits (SOM_E4M3) with a factor for each block:
+ *
+ *     pre[m][n] = alpha sum_k x[m][k] sx(m, k) W[n][k] sw(n, k) + bias[n],
+ *     y[m][n] = act(pre[m][n]) + residual[m][n].
+ *
+ * x [M][ldx]; W is unit-major, [N][ldw].  sx and sw are x_scale's and w_scale's factors (fp32):
+ * at row r and column k, p[r / rows * row_stride + k / 128 * block_stride], rows being 1 or 128;
+ * strides may be 0 and up.  som_quantise makes such operands: x in blocks of one row and weights in blocks of 128
+ * are the common choice, which is the fastest.  The gradients are products of the same kind: dx's
+ * of dP in blocks along N and the transposed weights (whose blocks of 128 x 128 are the same
+ * ones), dW's of dP and x transposed, both in blocks along M.
+ * e as for som_product, without x_scale and w_scale, which have to be NULL.  y, residual and pre
+ * are fp16, bf16 or fp32.  Sums over a block are rounded to about 16 bits of their size for
+ * y of 16 bits (the 8-bit matrix instructions; errors of 1.4e-5 of their root mean square), to fp32 for
+ * fp32 y, at half the rate; sums of blocks are fp32.
+ * Sizes and workspace (som_product_blocks_workspace_bytes) as for som_product. */
+typedef struct som_block_scale {
+  const float* p;
+  int64_t row_stride, block_stride;
+  int32_t rows;          /* that share a factor: 1 or 128 */
+  int32_t reserved;      /* 0 */
+} som_block_scale;
+
+size_t som_product_blocks_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t y_dtype);
+som_status som_product_blocks(const void* x, int64_t ldx, const som_block_scale* x_scale, const void* W, int64_t ldw,
+                              const som_block_scale* w_scale, int64_t M, int64_t N, int64_t K, void* y, int64_t ldy,
+                              int32_t y_dtype, const som_epilogue* e, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* ---------------------------------------------------------------------------
  * Measurement aid: read-bandwidth probe.  Reads `bytes` (a multiple of 16) of
  * device memory at `buf` (16-byte aligned) `passes` times with coalesced

@@ -44,4 +44,6 @@ from .som import (  # noqa: F401
     som_cross_entropy_backward,
     som_cross_entropy_backward_workspace_bytes,
     som_cross_entropy_workspace_bytes,
+    som_product_blocks,
+    som_product_blocks_workspace_bytes,
 )

@@ -4,6 +4,7 @@
 
 #include "api_dense.h"
 #include "cross_entropy.h"
+#include "product_blocks.h"
 
 namespace {
 
@@ -41,6 +42,21 @@ som_status check_scores(int32_t w_units, int32_t dtype, int64_t M, int64_t N, in
   SOM_CHECK(check_sizes(M, N, K));
   if (!std::isfinite(alpha)) return fail(SOM_ERR_INVALID_ARG, "alpha must be finite");
   if (!launchable(M, N)) return fail(SOM_ERR_INVALID_ARG, "M * N is too large for one call");
+  return SOM_OK;
+}
+
+// Factors [rows / s->rows][k / 128] of an operand.
+som_status check_scale(const char* name, const som_block_scale* s, int64_t rows, int64_t k) {
+  const std::string n(name);
+  if (!s) return fail(SOM_ERR_INVALID_ARG, n + " is NULL");
+  if (s->rows != 1 && s->rows != kBlock) return fail(SOM_ERR_INVALID_ARG, n + ": rows must be 1 or 128");
+  if (s->reserved != 0) return fail(SOM_ERR_INVALID_ARG, n + ": reserved must be 0");
+  if (!s->p) return fail(SOM_ERR_INVALID_ARG, n + ": p is NULL");
+  SOM_CHECK(check_vector(name, s->p));
+  const int64_t r = s->rows == 1 ? rows : blocks(rows);
+  if (s->row_stride < 0 || s->block_stride < 0 || s->row_stride > (int64_t(1) << 58) / r ||
+      s->block_stride > (int64_t(1) << 58) / blocks(k))
+    return fail(SOM_ERR_INVALID_ARG, n + ": the strides must be >= 0, and its entries addressable");
   return SOM_OK;
 }
 
@@ -167,6 +183,69 @@ som_status som_quantise(const void* x, int64_t ldx, int32_t dtype, int64_t rows,
   a.transpose = transpose != 0;
   const hipError_t e = som::launch_quantise(a, stream);
   return e == hipSuccess ? ok() : hip_fail(e, "quantise launch");
+}
+
+size_t som_product_blocks_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t y_dtype) {
+  if (M < 1 || M > kI32Max || N < 1 || N > kMaxK || K < 1 || K > kMaxK || !is_float(y_dtype)) return 0;
+  const bool exact = y_dtype == SOM_F32;
+  const size_t on = som::plan_blocks(M, N, K, true, exact).partial_floats;
+  const size_t off = som::plan_blocks(M, N, K, false, exact).partial_floats;
+  return som::align_up(sizeof(float) * (on > off ? on : off), 256);
+}
+
+som_status som_product_blocks(const void* x, int64_t ldx, const som_block_scale* x_scale, const void* W, int64_t ldw,
+                              const som_block_scale* w_scale, int64_t M, int64_t N, int64_t K, void* y, int64_t ldy,
+                              int32_t y_dtype, const som_epilogue* e, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const som_epilogue plain = {SOM_ACT_NONE, 0, 1.0f, nullptr, nullptr, nullptr, nullptr, 0, nullptr, 0};
+  if (!e) e = &plain;
+  if (!is_float(y_dtype)) return fail(SOM_ERR_INVALID_ARG, "y_dtype must be SOM_F32, SOM_F16 or SOM_BF16");
+  SOM_CHECK(check_sizes(M, N, K));
+  if (e->act < SOM_ACT_NONE || e->act > SOM_ACT_SILU) return fail(SOM_ERR_INVALID_ARG, "unknown activation");
+  if (e->reserved != 0) return fail(SOM_ERR_INVALID_ARG, "reserved must be 0");
+  if (e->x_scale || e->w_scale) return fail(SOM_ERR_INVALID_ARG, "the epilogue's x_scale and w_scale must be NULL: the factors are the blocks'");
+  if (!launchable(M, N)) return fail(SOM_ERR_INVALID_ARG, "M * N is too large for one call");
+  if (M == 0) return ok();
+  SOM_CHECK(check_matrix("x", x, ldx, M, K, SOM_E4M3));
+  SOM_CHECK(check_matrix("W", W, ldw, N, K, SOM_E4M3));
+  SOM_CHECK(check_scale("x_scale", x_scale, M, K));
+  SOM_CHECK(check_scale("w_scale", w_scale, N, K));
+  SOM_CHECK(check_matrix("y", y, ldy, M, N, y_dtype));
+  if (e->residual) SOM_CHECK(check_matrix("residual", e->residual, e->ldr, M, N, y_dtype));
+  if (e->pre) SOM_CHECK(check_matrix("pre", e->pre, e->ldp, M, N, y_dtype));
+  SOM_CHECK(check_vector("bias", e->bias));
+  SOM_CHECK(check_ws(ws, ws_bytes, som_product_blocks_workspace_bytes(M, N, K, y_dtype)));
+  som::BlockArgs a{};
+  a.P = x;
+  a.ldp = ldx;
+  a.p_kc = true;
+  a.Q = W;
+  a.ldq = ldw;
+  a.q_kc = true;
+  a.I = M;
+  a.J = N;
+  a.K = K;
+  a.elem = SOM_E4M3;
+  a.alpha = e->alpha;
+  a.act = e->act;
+  a.bias = e->bias;
+  a.residual = e->residual;
+  a.ldr = e->ldr;
+  a.pre = e->pre;
+  a.ldpre = e->ldp;
+  a.out = y;
+  a.ldo = ldy;
+  a.out_type = y_dtype;
+  a.xs = x_scale->p;
+  a.xs_row = x_scale->row_stride;
+  a.xs_k = x_scale->block_stride;
+  a.xs_shift = x_scale->rows == 1 ? 0 : 7;
+  a.ws = w_scale->p;
+  a.ws_row = w_scale->row_stride;
+  a.ws_k = w_scale->block_stride;
+  a.ws_shift = w_scale->rows == 1 ? 0 : 7;
+  a.exact = y_dtype == SOM_F32;
+  const hipError_t err = som::launch_blocks(a, static_cast<float*>(ws), stream);
+  return err == hipSuccess ? ok() : hip_fail(err, "product launch");
 }
 
 }  // extern "C"

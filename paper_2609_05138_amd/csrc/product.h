@@ -75,8 +75,10 @@ struct ProductPlan {
   int64_t k_split;
   size_t partial_floats;
 };
-// `dma`: the rows of both operands start on 16 bytes; `few`: the kernels of few rows will do
-ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma, bool few = true);
+// `dma`: the rows of both operands start on 16 bytes; `few`: the kernels of few rows will do;
+// `first`: the largest shape that will
+ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma, bool few = true,
+                         int first = kShape256);
 // Rows of both operands start on 16 bytes, at strides that a tile's 32-bit offsets span.
 bool rows_on_16(const ProductArgs& a);
 void set_launch(ProductArgs& a, const ProductPlan& p, float* partial);
@@ -86,6 +88,8 @@ hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream);
 hipError_t launch_product_f16(int shape, const ProductArgs& a, hipStream_t stream);
 hipError_t launch_product_bf16(int shape, const ProductArgs& a, hipStream_t stream);
 hipError_t launch_product_e4m3(int shape, const ProductArgs& a, hipStream_t stream);
+// The join of a split k axis with som_product's epilogue.
+hipError_t launch_join(const ProductArgs& a, hipStream_t stream);
 hipError_t launch_product_few(const ProductArgs& a, hipStream_t stream);
 
 // dP = dy act'(pre), rounded to the type, and dP's column sums.

@@ -108,14 +108,14 @@ double product_time(int shape, int64_t n, int64_t steps, bool e4m3, bool dma) {
 // against 17.6; two rows are no faster; 4,096 x 4,096: 11.4 against 8.9, since a
 // narrow strip's lines are read by several CUs).
 ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma,
-                         bool few) {
+                         bool few, int first) {
   if (few && p_kc && J <= kFewMaxColumns && (q_kc ? I <= 4 : I == 1 && J >= 8192)) return {kFew, 1, K, 0};
   const int64_t step = elem == kE4M3 ? 128 : 64;
   const int64_t steps = (K + step - 1) / step;
-  ProductPlan best{kShape256, 1, steps * step, 0};
+  ProductPlan best{first, 1, steps * step, 0};
   double least = 1e300;
   const int last = p_kc ? kShape16 : kShape64;
-  for (int shape = 0; shape <= last; ++shape) {
+  for (int shape = first; shape <= last; ++shape) {
     const ShapeInfo& s = kInfo[shape];
     // not worth the host's time: tiles of four times the rows, or very many of them unless
     // they are one row (40 x 512 x 1,048,576: 64 x 128 254 us, 128 x 128 338; 16 x 1,024 x
@@ -166,7 +166,10 @@ hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream) {
   hipError_t e = a.elem == kF16 ? launch_product_f16(p.shape, a, stream)
                  : a.elem == kBF16 ? launch_product_bf16(p.shape, a, stream)
                                    : launch_product_e4m3(p.shape, a, stream);
-  if (e != hipSuccess || p.splits == 1) return e;
+  return e != hipSuccess || p.splits == 1 ? e : launch_join(a, stream);
+}
+
+hipError_t launch_join(const ProductArgs& a, hipStream_t stream) {
   const int64_t groups = (a.J + 7) / 8 * a.I;
   hipLaunchKernelGGL(k_join, dim3(static_cast<uint32_t>((groups + 255) / 256)), dim3(256), 0, stream, a);
   return hipGetLastError();

@@ -68,6 +68,8 @@ EXPORTS = (
     "som_cross_entropy",
     "som_cross_entropy_backward_workspace_bytes",
     "som_cross_entropy_backward",
+    "som_product_blocks_workspace_bytes",
+    "som_product_blocks",
 )
 
 # som_dtype and som_act
@@ -109,6 +111,16 @@ class som_epilogue(ctypes.Structure):
         ("ldr", ctypes.c_int64),
         ("pre", ctypes.c_void_p),
         ("ldp", ctypes.c_int64),
+    ]
+
+
+class som_block_scale(ctypes.Structure):
+    _fields_ = [
+        ("p", ctypes.c_void_p),
+        ("row_stride", ctypes.c_int64),
+        ("block_stride", ctypes.c_int64),
+        ("rows", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
     ]
 
 
@@ -224,6 +236,12 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.som_cross_entropy_backward.restype = _i32
     lib.som_cross_entropy_backward.argtypes = [_vp, _vp, _i64, _vp, _i64, _i32, _i32, _i64, _i64, _i64, _vp, _vp,
                                                ctypes.c_float, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _sz, _vp]
+    lib.som_product_blocks_workspace_bytes.restype = _sz
+    lib.som_product_blocks_workspace_bytes.argtypes = [_i64, _i64, _i64, _i32]
+    lib.som_product_blocks.restype = _i32
+    lib.som_product_blocks.argtypes = [_vp, _i64, ctypes.POINTER(som_block_scale), _vp, _i64,
+                                       ctypes.POINTER(som_block_scale), _i64, _i64, _i64, _vp, _i64, _i32,
+                                       ctypes.POINTER(som_epilogue), _vp, _sz, _vp]
     _lib = lib
     return lib
 
@@ -1114,3 +1132,63 @@ def som_cross_entropy_backward(dloss: torch.Tensor, x: torch.Tensor, W: torch.Te
                                           lddx, dWp, lddw, _vector(dbias, "dbias", N, device), wsp, n,
                                           _raw_stream(device, stream)))
     return dx, dW, dbias
+
+
+def som_product_blocks_workspace_bytes(M: int, N: int, K: int, dtype=torch.bfloat16) -> int:
+    return int(load().som_product_blocks_workspace_bytes(M, N, K, DTYPES[dtype]))
+
+
+def _block_scale(t: torch.Tensor, name: str, rows: int, k: int, device: int) -> som_block_scale:
+    """The factors of a rows x k operand: one for each row and block of k, or for 128 rows."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dim() != 2 or t.shape[0] not in (rows, _blocks(rows)):
+        raise ValueError(f"{name} must be {rows} or {_blocks(rows)} x {_blocks(k)} (got "
+                         f"{' x '.join(str(n) for n in t.shape)})")
+    p, row, block = _factors(t, name, (t.shape[0], _blocks(k)), device)
+    return som_block_scale(p, row, block, 1 if t.shape[0] == rows else 128, 0)
+
+
+def som_product_blocks(x: torch.Tensor, x_scale: torch.Tensor, W: torch.Tensor, w_scale: torch.Tensor,
+                       bias: Optional[torch.Tensor] = None, act: str = "none", residual: Optional[torch.Tensor] = None,
+                       alpha: float = 1.0, y: Optional[torch.Tensor] = None, dtype=None,
+                       pre: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """act(alpha (x x_scale) @ (W w_scale) + bias) + residual of operands in blocks of 8 bits.
+
+    x [M, K] and W [K, N] in float8_e4m3fn, W the transposed view of an N x K matrix.  x_scale
+    [M, K / 128] and w_scale [N / 128, K / 128] (rounded up) are som_quantise's factors, of blocks
+    of one row or of 128 either; w_scale's rows are those of the N x K matrix.  y in bf16, fp16 or
+    fp32 (``dtype``; bf16 unless given).  Everything else as for som_product."""
+    lib = load()
+    _float_type(x, "x", (torch.float8_e4m3fn,))
+    xp, ldx = _rows(x, "x")
+    device = x.get_device()
+    if torch._C._cuda_getDevice() != device:       # a launch goes to the current one
+        with torch.cuda.device(device):
+            return som_product_blocks(x, x_scale, W, w_scale, bias, act, residual, alpha, y, dtype, pre, ws, stream)
+    M, K = x.shape
+    Wp, ldw, units = _weights(W, "W", x.dtype, device)
+    if not units and K > 1:
+        raise ValueError("W must be the transposed view of an N x K matrix (unit-major)")
+    if W.shape[0] != K:
+        raise ValueError(f"x has {K} columns and W {W.shape[0]} rows")
+    N = W.shape[1]
+    if not units:                                  # one element of each unit
+        ldw = max(W.stride(1), 1)
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}")
+    xs, wsc = _block_scale(x_scale, "x_scale", M, K, device), _block_scale(w_scale, "w_scale", N, K, device)
+    shape = (M, N)
+    if y is None:
+        y = _new(shape, dtype or torch.bfloat16, x.device, stream)
+    elif dtype is not None and y.dtype != dtype:
+        raise TypeError(f"y must be {dtype} (got {y.dtype})")
+    yt = _float_type(y, "y", _FLOATS)
+    yp, ldy = _rows(y, "y", None, shape, device)
+    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", y.dtype, shape, device)
+    pp, ldp = (None, 0) if pre is None else _rows(pre, "pre", y.dtype, shape, device)
+    e = som_epilogue(ACTIVATIONS[act], 0, alpha, None, None, _vector(bias, "bias", N, device), rp, ldr, pp, ldp)
+    ws, wsp, n = _scratch(ws, lib.som_product_blocks_workspace_bytes(M, N, K, yt), x.device, stream)
+    _check(lib.som_product_blocks(xp, ldx, ctypes.byref(xs), Wp, ldw, ctypes.byref(wsc), M, N, K, yp, ldy, yt,
+                                  ctypes.byref(e), wsp, n, _raw_stream(device, stream)))
+    return y
