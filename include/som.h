@@ -664,6 +664,25 @@ som_status som_product_blocks(const void* x, int64_t ldx, const som_block_scale*
                               const som_block_scale* w_scale, int64_t M, int64_t N, int64_t K, void* y, int64_t ldy,
                               int32_t y_dtype, const som_epilogue* e, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* A gradient or momentum of a weight matrix orthogonalised by Newton-Schulz steps, the update that
+ * moves all directions of the weights alike:
+ *
+ *     X = G / |G|_F;  `steps` times:  A = X X^T,  X = a X + (b A + c A A) X;  y = X
+ *
+ * (tall matrices: of the transpose, which is the same).  (3.4445, -4.7750, 2.0315) and 5 steps bring
+ * singular values from 1 / 100 of the norm on to between 0.7 and 1.2; (1.5, -0.5, 0) and more steps to 1.
+ * G [rows][ldg] is fp32, fp16 or bf16; y [rows][ldy] is bf16 and may be G.  X is kept in fp32, the
+ * products take it and A in fp16: y is within 2e-3 (2-norm, relative) of the formula's beside its own rounding.  A
+ * matrix of zeros gives zeros; a NaN or an infinity makes all of y NaN.  Singular values of X have to stay
+ * below 3.9 and |a|, |b| and |c| are at most 64: coefficients for which they do not give infinities and NaN.
+ * rows and cols in [1, 2^24], the smaller one up to 2^15, with som_product's limit on tiles;
+ * steps in [1, 64].  ws: som_orthogonalise_workspace_bytes, 256-byte aligned (8 bytes for an
+ * element of G and 4 for one of A, and more for small products). */
+size_t som_orthogonalise_workspace_bytes(int64_t rows, int64_t cols);
+som_status som_orthogonalise(const void* G, int64_t ldg, int32_t dtype, int64_t rows, int64_t cols, int32_t steps,
+                             float a, float b, float c, void* y, int64_t ldy, void* ws, size_t ws_bytes,
+                             hipStream_t stream);
+
 /* ---------------------------------------------------------------------------
  * Measurement aid: read-bandwidth probe.  Reads `bytes` (a multiple of 16) of
  * device memory at `buf` (16-byte aligned) `passes` times with coalesced

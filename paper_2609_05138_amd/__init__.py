@@ -46,4 +46,6 @@ from .som import (  # noqa: F401
     som_cross_entropy_workspace_bytes,
     som_product_blocks,
     som_product_blocks_workspace_bytes,
+    som_orthogonalise,
+    som_orthogonalise_workspace_bytes,
 )

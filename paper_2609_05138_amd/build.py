@@ -23,7 +23,8 @@ ARCH = "gfx950"
 SOURCES = ["api.hip", "norms.hip", "plan.hip", "plan_list.hip", "search.hip", "search_f16.hip", "cluster.hip", "update.hip",
            "probe.hip", "api_dense.hip", "rms_norm.hip", "dropout.hip", "product.hip", "product_f16.hip",
            "product_bf16.hip", "product_e4m3.hip", "product_few.hip", "api_train.hip", "quantise.hip",
-           "product_modes.hip", "product_modes_f16.hip", "product_modes_bf16.hip", "cross_entropy.hip", "product_blocks.hip"]
+           "product_modes.hip", "product_modes_f16.hip", "product_modes_bf16.hip", "cross_entropy.hip", "product_blocks.hip",
+           "orthogonalise.hip"]
 
 # Packed fp32 instructions are switched off for every device compile.
 CFLAGS = [

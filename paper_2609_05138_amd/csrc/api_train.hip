@@ -4,6 +4,7 @@
 
 #include "api_dense.h"
 #include "cross_entropy.h"
+#include "orthogonalise.h"
 #include "product_blocks.h"
 
 namespace {
@@ -58,6 +59,13 @@ som_status check_scale(const char* name, const som_block_scale* s, int64_t rows,
       s->block_stride > (int64_t(1) << 58) / blocks(k))
     return fail(SOM_ERR_INVALID_ARG, n + ": the strides must be >= 0, and its entries addressable");
   return SOM_OK;
+}
+
+constexpr int64_t kMaxSide = int64_t(1) << 24, kMaxShort = int64_t(1) << 15;
+
+bool ortho_sizes(int64_t rows, int64_t cols) {
+  return rows >= 1 && cols >= 1 && rows <= kMaxSide && cols <= kMaxSide && (rows <= kMaxShort || cols <= kMaxShort) &&
+         launchable(rows, cols);
 }
 
 }  // namespace
@@ -246,6 +254,38 @@ som_status som_product_blocks(const void* x, int64_t ldx, const som_block_scale*
   a.exact = y_dtype == SOM_F32;
   const hipError_t err = som::launch_blocks(a, static_cast<float*>(ws), stream);
   return err == hipSuccess ? ok() : hip_fail(err, "product launch");
+}
+
+size_t som_orthogonalise_workspace_bytes(int64_t rows, int64_t cols) {
+  return ortho_sizes(rows, cols) ? som::ortho_ws(rows, cols).total : 0;
+}
+
+som_status som_orthogonalise(const void* G, int64_t ldg, int32_t dtype, int64_t rows, int64_t cols, int32_t steps,
+                             float a, float b, float c, void* y, int64_t ldy, void* ws, size_t ws_bytes,
+                             hipStream_t stream) {
+  if (!is_float(dtype)) return fail(SOM_ERR_INVALID_ARG, "dtype must be SOM_F32, SOM_F16 or SOM_BF16");
+  if (!ortho_sizes(rows, cols))
+    return fail(SOM_ERR_INVALID_ARG, "rows and cols must be in [1, 2^24], one of them up to 2^15, and launchable");
+  if (steps < 1 || steps > 64) return fail(SOM_ERR_INVALID_ARG, "steps must be in [1, 64]");
+  for (const float v : {a, b, c})
+    if (!(std::fabs(v) <= 64.0f)) return fail(SOM_ERR_INVALID_ARG, "the coefficients must be in [-64, 64]");
+  SOM_CHECK(check_matrix("G", G, ldg, rows, cols, dtype));
+  SOM_CHECK(check_matrix("y", y, ldy, rows, cols, SOM_BF16));
+  SOM_CHECK(check_ws(ws, ws_bytes, som_orthogonalise_workspace_bytes(rows, cols)));
+  som::OrthoCall o{};
+  o.G = G;
+  o.y = y;
+  o.ldg = ldg;
+  o.ldy = ldy;
+  o.rows = rows;
+  o.cols = cols;
+  o.dtype = dtype;
+  o.steps = steps;
+  o.a = a;
+  o.b = b;
+  o.c = c;
+  const hipError_t e = som::launch_orthogonalise(o, ws, stream);
+  return e == hipSuccess ? ok() : hip_fail(e, "orthogonalise launch");
 }
 
 }  // extern "C"

@@ -70,6 +70,8 @@ EXPORTS = (
     "som_cross_entropy_backward",
     "som_product_blocks_workspace_bytes",
     "som_product_blocks",
+    "som_orthogonalise_workspace_bytes",
+    "som_orthogonalise",
 )
 
 # som_dtype and som_act
@@ -242,6 +244,11 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.som_product_blocks.argtypes = [_vp, _i64, ctypes.POINTER(som_block_scale), _vp, _i64,
                                        ctypes.POINTER(som_block_scale), _i64, _i64, _i64, _vp, _i64, _i32,
                                        ctypes.POINTER(som_epilogue), _vp, _sz, _vp]
+    lib.som_orthogonalise_workspace_bytes.restype = _sz
+    lib.som_orthogonalise_workspace_bytes.argtypes = [_i64, _i64]
+    lib.som_orthogonalise.restype = _i32
+    lib.som_orthogonalise.argtypes = [_vp, _i64, _i32, _i64, _i64, _i32, ctypes.c_float, ctypes.c_float, ctypes.c_float,
+                                      _vp, _i64, _vp, _sz, _vp]
     _lib = lib
     return lib
 
@@ -1191,4 +1198,30 @@ def som_product_blocks(x: torch.Tensor, x_scale: torch.Tensor, W: torch.Tensor, 
     ws, wsp, n = _scratch(ws, lib.som_product_blocks_workspace_bytes(M, N, K, yt), x.device, stream)
     _check(lib.som_product_blocks(xp, ldx, ctypes.byref(xs), Wp, ldw, ctypes.byref(wsc), M, N, K, yp, ldy, yt,
                                   ctypes.byref(e), wsp, n, _raw_stream(device, stream)))
+    return y
+
+
+def som_orthogonalise_workspace_bytes(rows: int, cols: int) -> int:
+    return int(load().som_orthogonalise_workspace_bytes(rows, cols))
+
+
+def som_orthogonalise(G: torch.Tensor, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315),
+                      y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """G / |G| after ``steps`` Newton-Schulz steps X = a X + (b A + c A A) X, A = X X^T, in bf16: a
+    matrix near G whose singular values are all about one.  G in fp32, fp16 or bf16; y may be
+    G where that is bf16."""
+    lib = load()
+    dt = _float_type(G, "G", _FLOATS)
+    Gp, ldg = _rows(G, "G")
+    device = G.get_device()
+    if torch._C._cuda_getDevice() != device:       # a launch goes to the current one
+        with torch.cuda.device(device):
+            return som_orthogonalise(G, steps, coefficients, y, ws, stream)
+    rows, cols = G.shape
+    a, b, c = coefficients
+    if y is None:
+        y = _new((rows, cols), torch.bfloat16, G.device, stream)
+    yp, ldy = _rows(y, "y", torch.bfloat16, (rows, cols), device)
+    ws, wsp, n = _scratch(ws, lib.som_orthogonalise_workspace_bytes(rows, cols), G.device, stream)
+    _check(lib.som_orthogonalise(Gp, ldg, dt, rows, cols, steps, a, b, c, yp, ldy, wsp, n, _raw_stream(device, stream)))
     return y

@@ -1,0 +1,153 @@
+"""Orthogonalised updates on the GPU against the fp64 oracle.
+
+Tolerance.  Every element of X, A and B that a product reads is rounded to 11 bits, uniformly:
+r = 2^-11 / sqrt(3) of itself at the most (a rounding's root mean square is at most half a
+step over sqrt 3).  Of a step's terms a X is exact, (b A + c A A) X carries the roundings of A, twice in
+A A, of B and of X: their norms are at most |b| s^3 and c s^5 for singular values s up to 1.2, which
+for (3.4445, -4.775, 2.0315) are 8.3 and 5.1, but cancel in X, so for directions of s = 1 the
+terms are 4.8 and 2.0, their roundings r sqrt((4.8 + 2 * 2.0)^2 + 2.8^2 * 2) = 9.7 r, damped by the next
+step's slope (a + 3 b s^2 + 5 c s^4 = -0.7 at s = 1, at most 1.5 between 0.7 and 1.2 in size): a
+geometric sum of at most 2 of them in root mean square, 20 r = 5.6e-3 of the result in the worst
+case that all directions are there; the result's own rounding is 2^-8 of each element.  Every test asks for
+that; the typical error is a fifth (2e-3)."""
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from oracle import train as oracle  # noqa: E402
+
+if torch.cuda.is_available():
+    import paper_2609_05138_amd as som
+else:  # collected on CPU-only machines, never run there
+    som = None
+
+DEV = "cuda:0"
+T = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+QUINTIC, CUBIC = (3.4445, -4.7750, 2.0315), (1.5, -0.5, 0.0)
+WITHIN = 5.6e-3 + 2.0 ** -8 / 3 ** 0.5
+
+
+def _view(values, dtype, pad):
+    rows, cols = values.shape
+    wide = torch.full((rows, cols + pad), float("nan"), device=DEV).to(dtype)
+    wide[:, :cols] = torch.as_tensor(values, device=DEV).to(dtype)
+    return wide[:, :cols]
+
+
+def _far(got, want):
+    return np.linalg.norm(got.double().cpu().numpy() - want) / np.linalg.norm(want)
+
+
+SHAPES = [(1, 1), (1, 7), (9, 1), (2, 3), (5, 64), (64, 64), (65, 63), (63, 200), (100, 100), (128, 512), (300, 129),
+          (257, 1000), (1030, 255), (520, 520)]
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_orthogonalise(rows, cols, kind):
+    rng = np.random.default_rng(rows * 100 + cols)
+    pad = (rows + cols) % 3 * 3
+    G = _view(rng.normal(size=(rows, cols)) * 1e-2, T[kind], pad)
+    wide = torch.full((rows, cols + 5), 7.0, dtype=torch.bfloat16, device=DEV)
+    for coefficients, steps in ((QUINTIC, 5), (QUINTIC, 1), (CUBIC, 3)):
+        y = som.som_orthogonalise(G, steps, coefficients, y=wide[:, :cols])
+        assert _far(y, oracle.orthogonalise(G.double().cpu().numpy(), steps, coefficients)) <= WITHIN
+        assert bool((wide[:, cols:] == 7).all())
+
+
+@pytest.mark.parametrize("rows,cols", [(256, 384), (384, 256)])
+@pytest.mark.parametrize("spectrum", ["equal", "wide", "spikes", "one"])
+def test_spectra(spectrum, rows, cols):
+    rng = np.random.default_rng(rows)
+    u, s, v = np.linalg.svd(rng.normal(size=(rows, cols)), full_matrices=False)
+    k = len(s)
+    s = {"equal": np.ones(k), "wide": np.logspace(0, -4, k), "spikes": np.r_[np.full(4, 30.0), np.ones(k - 4)],
+         "one": np.r_[1.0, np.zeros(k - 1)]}[spectrum]
+    G = torch.as_tensor(u @ np.diag(s) @ v, dtype=torch.float32, device=DEV)
+    y = som.som_orthogonalise(G)
+    assert _far(y, oracle.orthogonalise(G.double().cpu().numpy(), 5, QUINTIC)) <= WITHIN
+    got = np.linalg.svd(y.double().cpu().numpy(), compute_uv=False)
+    if spectrum in ("equal", "spikes"):
+        assert 0.6 < got.min() and got.max() < 1.25
+
+
+def test_many_cubic_steps_reach_an_orthogonal_matrix():
+    rng = np.random.default_rng(0)
+    G = torch.as_tensor(rng.normal(size=(64, 500)), dtype=torch.float32, device=DEV)
+    y = som.som_orthogonalise(G, 20, CUBIC).double()
+    gram = y @ y.t().contiguous()
+    # y's elements are 2^-8 off at the most, its rows 2^-8 of their length of one; the steps' 2^-11 settle at s = 1
+    assert float((gram - torch.eye(64, device=DEV, dtype=torch.float64)).abs().max()) < 3 * 2.0 ** -8
+
+
+@pytest.mark.parametrize("scale", [1e-38, 1e-30, 1.0, 1e30, 1e38])
+def test_sizes_whose_squares_leave_fp32(scale):
+    rng = np.random.default_rng(1)
+    G = torch.as_tensor(rng.uniform(-1, 1, size=(70, 90)), dtype=torch.float32, device=DEV)
+    y = som.som_orthogonalise(G * scale)
+    assert _far(y, oracle.orthogonalise((G * scale).double().cpu().numpy(), 5, QUINTIC)) <= WITHIN
+
+
+def test_zeros_and_values_that_are_not_finite():
+    for shape in ((1, 1), (70, 200), (300, 40)):
+        G = torch.zeros(shape, device=DEV)
+        assert not som.som_orthogonalise(G).any()
+        for bad in (float("nan"), float("inf"), float("-inf")):
+            G = torch.ones(shape, device=DEV)
+            G[-1, -1] = bad
+            assert bool(som.som_orthogonalise(G).isnan().all())
+
+
+def test_large_and_in_place():
+    g = torch.Generator(device=DEV)
+    g.manual_seed(0)
+    for rows, cols in ((1200, 2500), (2100, 2100)):
+        G = torch.randn((rows, cols), generator=g, device=DEV).bfloat16()
+        X = G.double() / torch.linalg.vector_norm(G.double())
+        for _ in range(5):
+            A = torch.mm(X, X.t().contiguous())
+            X = QUINTIC[0] * X + torch.mm(QUINTIC[1] * A + QUINTIC[2] * torch.mm(A, A), X)
+        y = som.som_orthogonalise(G)
+        assert float((y.double() - X).norm() / X.norm()) < WITHIN
+        back = som.som_orthogonalise(G.t().contiguous())
+        assert float((back.double().t() - X).norm() / X.norm()) < WITHIN
+        again = G.clone()
+        assert som.som_orthogonalise(again, y=again) is again and torch.equal(again, y)
+
+
+def test_streams_and_graphs():
+    rng = np.random.default_rng(2)
+    G = torch.as_tensor(rng.normal(size=(200, 333)), dtype=torch.float32, device=DEV)
+    want = som.som_orthogonalise(G)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    y = som.som_orthogonalise(G, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(y, want) and torch.equal(som.som_orthogonalise(G), want)
+    X, y = G.clone(), torch.empty_like(want)
+    ws = torch.empty(som.som_orthogonalise_workspace_bytes(200, 333), dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        som.som_orthogonalise(X, y=y, ws=ws)
+    for k in range(3):
+        X.copy_(G.roll(k, 0) + 0.1 * k)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, som.som_orthogonalise(X))
+
+
+def test_refusals():
+    G = torch.zeros((8, 16), device=DEV)
+    c = som.som_orthogonalise
+    fails = [(som.SomError, lambda: c(G, 0)), (som.SomError, lambda: c(G, 65)), (som.SomError, lambda: c(G[:0])),
+             (som.SomError, lambda: c(G, 5, (float("nan"), 0.0, 0.0))), (som.SomError, lambda: c(G, 5, (65.0, 0.0, 0.0))),
+             (TypeError, lambda: c(G.double())), (TypeError, lambda: c(G, y=G)), (ValueError, lambda: c(G.t())),
+             (ValueError, lambda: c(G, y=torch.empty((8, 15), dtype=torch.bfloat16, device=DEV))),
+             (ValueError, lambda: c(G, 5, (1.0, 2.0))),
+             (som.SomError, lambda: c(G, ws=torch.empty(64, dtype=torch.uint8, device=DEV)))]
+    for error, call in fails:
+        with pytest.raises(error):
+            call()
