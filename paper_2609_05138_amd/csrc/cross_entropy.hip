@@ -12,7 +12,11 @@
 // Backward: the product again, a piece of the classes at a time: its epilogue makes g of the
 // piece, in x's type because the matrix cores take 16 bits (as som_product_backward's dP), and
 // its column sums unrounded; two products add the piece to dx (in fp32 until the last piece)
-// and give its part of dW.  g is scaled by a power of two that dloss's largest value sets, so that
+// and give its part of dW.  A row of g sums to zero, so what all classes' weights have in common (a
+// codebook's are positive, with a mean far from zero) cancels in dx, but not what g's rounding does to it: that
+// is the row's sum of roundings times the common part, which is added back (with the mean of up to
+// 256 classes in its place; without it dx of a codebook of [0, 1) is 2.1 times as far from 64 bits as
+// its own rounding, with it 1.4 times, as where nothing is in common).  g is scaled by a power of two that dloss's largest value sets, so that
 // fp16 holds what a mean over many rows gives (1 / M times a probability).
 //
 // Bound: the matrix cores.
@@ -167,9 +171,53 @@ __global__ void __launch_bounds__(256) k_grad_clean(const T* x, int64_t ldx, int
   }
 }
 
+// lost[i] = the row's parts, 16 rows and 16 slices of the strips a workgroup.
+__global__ void __launch_bounds__(256) k_grad_lost(const float* __restrict__ part, int64_t strips, int64_t rows,
+                                                   float* __restrict__ lost) {
+  __shared__ float sums[16][17];
+  const int r = threadIdx.x & 15, slice = threadIdx.x >> 4;
+  const int64_t i = group_index() * 16 + r;
+  float s = 0.0f;
+  if (i < rows) {
+    constexpr int kDeep = 8;
+    for (int64_t p0 = slice; p0 < strips; p0 += 16 * kDeep) {
+      float one[kDeep];
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d) one[d] = p0 + 16 * d < strips ? part[(p0 + 16 * d) * rows + i] : 0.0f;
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d) s += one[d];
+    }
+  }
+  sums[slice][r] = s;
+  __syncthreads();
+  if (slice || i >= rows) return;
+#pragma unroll
+  for (int w = 1; w < 16; ++w) s += sums[w][r];
+  lost[i] = s;
+}
+
+// common[k] = the mean of up to 256 classes' weights, spread over all classes; one feature a wave.
+template <typename T>
+__global__ void __launch_bounds__(256) k_grad_common(const T* W, int64_t ldw, bool units, int64_t classes, int64_t cols,
+                                                     float* common) {
+  const int lane = threadIdx.x & 63;
+  const int64_t k = group_index() * 4 + (threadIdx.x >> 6);
+  if (k >= cols) return;
+  const int64_t some = classes < 256 ? classes : 256;
+  float s = 0.0f;
+  for (int64_t c = lane; c < some; c += 64) {
+    const int64_t n = c * classes / some;
+    s += static_cast<float>(units ? W[n * ldw + k] : W[k * ldw + n]);
+  }
+#pragma unroll
+  for (int off = 32; off; off >>= 1) s += __shfl_xor(s, off, 64);
+  s /= static_cast<float>(some);
+  // (weights that are not finite make NaNs of what they reach, and no more than that)
+  if (lane == 0) common[k] = fabsf(s) < INFINITY ? s : 0.0f;
+}
+
 // g and its column sums from a split product's parts: 512 columns a workgroup, every (4
 // gridDim.y)th row, as k_act_grad.
-template <typename T>
 __global__ void __launch_bounds__(256) k_grad_scores(const GradArgs a) {
   __shared__ float sums[4][512];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -178,18 +226,22 @@ __global__ void __launch_bounds__(256) k_grad_scores(const GradArgs a) {
   const float factor = *a.factor;
   float bias[8] = {}, db[8] = {};
   if (a.bias) load8(a.bias + col, n, bias);
-  if (n > 0)
-    for (int64_t row = static_cast<int64_t>(blockIdx.y) * 4 + wave; row < a.I; row += int64_t(gridDim.y) * 4) {
+  for (int64_t row = static_cast<int64_t>(blockIdx.y) * 4 + wave; row < a.I; row += int64_t(gridDim.y) * 4) {
+    float lost = 0.0f;
+    if (n > 0) {
       float v[8];
       join8(a, row, col, v);
       grad8(a, grad_row(a, row, col, true), bias, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        db[e] += v[e];
-        v[e] *= factor;
-      }
-      store8(static_cast<T*>(a.out) + row * a.ldo + col, 8, v);
+      for (int e = 0; e < 8; ++e) db[e] += v[e];
+      lost = store_g(a, row, col, n, factor, v);
     }
+    if (a.lost_part) {
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) lost += __shfl_xor(lost, off, 64);
+      if (lane == 0) a.lost_part[blockIdx.x * a.I + row] = lost;
+    }
+  }
   if (!a.column_part) return;
 #pragma unroll
   for (int e = 0; e < 8; ++e) sums[wave][lane * 8 + e] = db[e];
@@ -273,6 +325,12 @@ GradWs grad_ws(int64_t M, int64_t N, int64_t K, int elem) {
     }
   w.column = o;
   o += align_up(sizeof(float) * groups * w.ld_column, 256);
+  w.common = o;
+  o += align_up(sizeof(float) * w.ldx, 256);
+  w.lost = o;
+  o += align_up(sizeof(float) * M, 256);
+  w.lost_part = o;                     // a wave's columns: 32 at the least
+  o += align_up(sizeof(float) * M * ((w.piece + 255) / 256 * 8), 256);
   w.partial = o;
   w.total = o + align_up(sizeof(float) * need, 256);
   return w;
@@ -354,7 +412,14 @@ static hipError_t prepare_rows(const GradCall& c, const GradWs& w, void* ws, hip
   hipLaunchKernelGGL(k_grad_head, dim3(1), dim3(1024), 0, stream, c.labels, c.lse, c.dloss, c.M, c.N,
                      c.dtype == kF16 ? 14 : 0, head);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !c.dW) return e;
+  if (e != hipSuccess) return e;
+  if (c.dx) {
+    hipLaunchKernelGGL(k_grad_common<T>, groups_grid((c.K + 3) / 4), dim3(256), 0, stream, static_cast<const T*>(c.W), c.ldw,
+                       c.units, c.N, c.K, at<float>(ws, w.common));
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (!c.dW) return hipSuccess;
   const T* const x = static_cast<const T*>(c.x);
   hipLaunchKernelGGL(k_grad_scan<T>, groups_grid((c.M + 3) / 4), dim3(256), 0, stream, x, c.ldx, c.M, c.K, c.labels,
                      c.lse, c.dloss, c.N, head);
@@ -400,24 +465,29 @@ hipError_t launch_loss_back(const GradCall& c, void* ws, hipStream_t stream) {
     a.classes = c.N;
     a.column_part = c.dbias ? at<float>(ws, w.column) : nullptr;
     a.ld_column = w.ld_column;
+    a.lost_part = c.dx ? at<float>(ws, w.lost_part) : nullptr;
     a.dma = rows_on_16(a);
     const ProductPlan p = plan_extra(a.I, a.J, a.K, a.elem, true, a.q_kc, a.dma);
     set_launch(a, p, partial);
     e = launch_mode(kGrad, p.shape, a, stream);
     if (e != hipSuccess) return e;
+    const int64_t strips = p.splits > 1 ? (n + kLostStrip - 1) / kLostStrip : int64_t(a.tiles_j) * kInfo[p.shape].waves_j;
     int64_t groups = a.tiles_i;
     if (p.splits > 1) {
       groups = scores_groups(c.M);
       const dim3 grid(static_cast<uint32_t>((n + 511) / 512), static_cast<uint32_t>(groups));
-      if (c.dtype == kF16)
-        hipLaunchKernelGGL(k_grad_scores<f16>, grid, dim3(256), 0, stream, a);
-      else
-        hipLaunchKernelGGL(k_grad_scores<bf16>, grid, dim3(256), 0, stream, a);
+      hipLaunchKernelGGL(k_grad_scores, grid, dim3(256), 0, stream, a);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
     if (c.dbias) {
       e = launch_column_sums(a.column_part, groups, w.ld_column, n, c.dbias + n0, stream);
+      if (e != hipSuccess) return e;
+    }
+    if (c.dx) {
+      hipLaunchKernelGGL(k_grad_lost, groups_grid((c.M + 15) / 16), dim3(256), 0, stream, a.lost_part, strips, c.M,
+                         at<float>(ws, w.lost));
+      e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
     ExtraArgs d{};
@@ -443,6 +513,8 @@ hipError_t launch_loss_back(const GradCall& c, void* ws, hipStream_t stream) {
       d.out = last ? c.dx : sum;
       d.ldo = last ? c.lddx : w.ldx;
       d.out_type = last ? c.dtype : kF32;
+      d.row = at<float>(ws, w.lost);
+      d.column = at<float>(ws, w.common);
       e = launch_extra(d, partial, stream);
       if (e != hipSuccess) return e;
     }
@@ -456,6 +528,7 @@ hipError_t launch_loss_back(const GradCall& c, void* ws, hipStream_t stream) {
       d.I = c.units ? n : c.K;
       d.J = c.units ? c.K : n;
       d.K = c.M;
+      d.row = nullptr;
       d.residual = nullptr;
       d.out = static_cast<char*>(c.dW) + dskip;
       d.ldo = c.lddw;

@@ -67,8 +67,10 @@ enum Shape { kShape256 = 0, kShape256x128, kShape128, kShape64, kShape32, kShape
 struct ShapeInfo {
   int bi, bj;                // rows and columns of C
   int wgs;                   // workgroups that a CU holds
+  int waves_j;               // waves side by side
 };
-constexpr ShapeInfo kInfo[kShapes] = {{256, 256, 1}, {256, 128, 1}, {128, 128, 1}, {64, 128, 2}, {32, 128, 2}, {16, 128, 2}};
+constexpr ShapeInfo kInfo[kShapes] = {{256, 256, 1, 4}, {256, 128, 1, 2}, {128, 128, 1, 4},
+                                      {64, 128, 2, 4},  {32, 128, 2, 4},  {16, 128, 2, 4}};
 struct ProductPlan {
   int shape;
   int splits;

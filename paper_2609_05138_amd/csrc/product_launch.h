@@ -7,7 +7,7 @@ namespace som {
 
 template <int SHAPE, int E, bool PKC, bool QKC, int MODE, int WI, int WJ, int TI, int TJ, int NS>
 hipError_t launch_one(const typename ModeArgs<MODE>::type& a, hipStream_t stream) {
-  static_assert(kInfo[SHAPE].bi == WI * TI * 16 && kInfo[SHAPE].bj == WJ * TJ * 16, "the grid is laid out for these tiles");
+  static_assert(kInfo[SHAPE].bi == WI * TI * 16 && kInfo[SHAPE].bj == WJ * TJ * 16 && kInfo[SHAPE].waves_j == WJ, "the grid is laid out for these tiles");
   constexpr size_t lds = static_cast<size_t>(NS) * (WI * TI + WJ * TJ) * 16 * kStepBytes;
   if constexpr (lds > 64 * 1024) {
     const hipError_t e = allow_lds(k_product<E, PKC, QKC, WI, WJ, TI, TJ, NS, MODE>, lds);

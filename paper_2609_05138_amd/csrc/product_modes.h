@@ -6,10 +6,11 @@
 
 namespace som {
 
-// out = alpha factor sum + beta residual (of a type of its own), and the same times half_scale
-// in the operands' type.
+// out = alpha factor (sum + row_i column_j) + beta residual (of a type of its own), and the same
+// times half_scale in the operands' type.
 struct ExtraArgs : ProductArgs {
   const float* factor;       // or nullptr
+  const float *row, *column; // or nullptr
   float beta;
   int res_type;
   void* half;                // [I][ldh] or nullptr
@@ -31,14 +32,17 @@ struct LossArgs : ProductArgs {
 };
 
 // g = dloss (exp(v - lse) - [label]) times *factor in the operands' type to out (whose rows are
-// padded to eight columns), and its unscaled sums over the tile's rows.
+// padded to eight columns), its unscaled sums over the tile's rows, and of each row what the rounding
+// of g times *factor took away in 16 TJ columns (those of a wave).
 struct GradArgs : ProductArgs {
   const int32_t* labels;
   const float *lse, *dloss, *factor;
   int64_t first, classes;    // the first of these columns' classes, and all there are
   float* column_part;        // [tiles_i][ld_column] or nullptr
   int64_t ld_column;
+  float* lost_part;          // [strips][I] or nullptr
 };
+constexpr int kLostStrip = 512;        // columns of a strip where k_grad_scores makes g
 
 template <>
 struct ModeArgs<kExtra> {
@@ -91,6 +95,14 @@ __device__ __forceinline__ RowTerms extra_terms(const ExtraArgs& a, float scale,
   return r;
 }
 
+// The rank-one term enters the sums.
+__device__ __forceinline__ void add_outer(const ExtraArgs& a, int64_t i, const float (&column)[8], float (&v)[8]) {
+  if (!a.row) return;
+  const float r = a.row[i];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = fmaf(r, column[e], v[e]);
+}
+
 template <bool kWhole>
 __device__ __forceinline__ void finish_extra(const ExtraArgs& a, int64_t i, int64_t j, int n, float (&v)[8],
                                              const RowTerms& r) {
@@ -131,6 +143,8 @@ __device__ __forceinline__ void extra_tile(const TileOf& tile, const ExtraArgs& 
     const int64_t i = tile.first + g * TileOf::kRows;
     return extra_terms(a, scale, i, tile.j, g < TileOf::kGroups && i < a.I ? tile.n : 0);
   };
+  float column[8] = {};
+  if (a.row) load8(a.column + tile.j, tile.n, column);
   RowTerms ahead[kAhead];
 #pragma unroll
   for (int g = 0; g < kAhead; ++g) ahead[g] = terms(g);
@@ -139,7 +153,9 @@ __device__ __forceinline__ void extra_tile(const TileOf& tile, const ExtraArgs& 
 #pragma unroll
     for (int k = 0; k + 1 < kAhead; ++k) ahead[k] = ahead[k + 1];
     ahead[kAhead - 1] = terms(g + kAhead);
-    if (i < a.I && tile.n > 0) finish8_extra(a, i, tile.j, tile.n, v, now);
+    if (i >= a.I || tile.n <= 0) return;
+    add_outer(a, i, column, v);
+    finish8_extra(a, i, tile.j, tile.n, v, now);
   });
 }
 
@@ -246,6 +262,25 @@ __device__ __forceinline__ void grad8(const GradArgs& a, const GradRow& r, const
   }
 }
 
+// Eight values of g times `factor`, rounded to T; returns what the rounding of n of them took away.
+template <typename T>
+__device__ __forceinline__ float store_g(T* p, int n, float factor, const float (&g)[8]) {
+  typename Eight<T>::vec r;
+  float lost = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float v = g[e] * factor;
+    r[e] = static_cast<T>(v);
+    lost += e < n ? v - static_cast<float>(r[e]) : 0.0f;
+  }
+  *reinterpret_cast<typename Eight<T>::at*>(p) = r;
+  return lost;
+}
+__device__ __forceinline__ float store_g(const GradArgs& a, int64_t i, int64_t j, int n, float factor, const float (&g)[8]) {
+  return a.elem == kF16 ? store_g(static_cast<f16*>(a.out) + i * a.ldo + j, n, factor, g)
+                        : store_g(static_cast<bf16*>(a.out) + i * a.ldo + j, n, factor, g);
+}
+
 template <class TileOf, int TI, int TJ>
 __device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a, const f4 (&acc)[TI][TJ],
                                           const TilePlace& place) {
@@ -271,17 +306,19 @@ __device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a,
 #pragma unroll
     for (int k = 0; k + 1 < kAhead; ++k) ahead[k] = ahead[k + 1];
     ahead[kAhead - 1] = terms(g + kAhead);
-    if (i >= a.I || tile.n <= 0) return;
-    grad8(a, now, bias, v);
+    const bool in = i < a.I && tile.n > 0;
+    float lost = 0.0f;
+    if (in) {
+      grad8(a, now, bias, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      sums[e] += v[e];
-      v[e] *= factor;
+      for (int e = 0; e < 8; ++e) sums[e] += v[e];
+      lost = store_g(a, i, tile.j, tile.n, factor, v);
     }
-    if (a.elem == kF16)
-      store8(static_cast<f16*>(a.out) + i * a.ldo + tile.j, 8, v);
-    else
-      store8(static_cast<bf16*>(a.out) + i * a.ldo + tile.j, 8, v);
+    if (a.lost_part) {
+#pragma unroll
+      for (int off = 1; off < kLanes; off <<= 1) lost += __shfl_xor(lost, off, 64);
+      if (i < a.I && tile.col == 0) a.lost_part[(place.tj * WJ + tile.wave % WJ) * a.I + i] = lost;
+    }
   });
   if (!a.column_part) return;
   // over the lanes that share the columns, then over the waves below each other, in order

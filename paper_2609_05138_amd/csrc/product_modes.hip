@@ -13,6 +13,11 @@ __global__ void __launch_bounds__(256) k_join_extra(const ExtraArgs a) {
   const RowTerms r = extra_terms(a, extra_scale(a), i, j, n);
   float v[8];
   join8(a, i, j, v);
+  if (a.row) {
+    float column[8];
+    load8(a.column + j, n, column);
+    add_outer(a, i, column, v);
+  }
   finish8_extra(a, i, j, n, v, r);
 }
 
