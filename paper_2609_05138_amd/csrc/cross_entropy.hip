@@ -110,21 +110,31 @@ struct GradHead {
   float factor, inverse;     // of g as it is stored: a power of two
   int32_t swap;              // 1: a row that counts for nothing holds a NaN or an infinity
 };
+constexpr int kScanGroups = 512;       // and as many flags
+constexpr int64_t kMostCommon = 256;
 
 // A row counts for nothing.
-__device__ __forceinline__ bool no_row(const int32_t* labels, const float* lse, const float* dloss, int64_t classes,
-                                       int64_t i) {
-  const int32_t label = labels[i];
-  return label < 0 || label >= classes || lse[i] == -INFINITY || dloss[i] == 0.0f;
+__device__ __forceinline__ bool no_row(const GradCall& c, int64_t i) {
+  const int32_t label = c.labels[i];
+  const float lse = c.lse[i], dloss = c.dloss[i];        // (three loads on their way at once)
+  return label < 0 || label >= c.N || lse == -INFINITY || dloss == 0.0f;
 }
 
-// The head, by one workgroup (an order for the whole of it, and M is small beside M K).
-__global__ void __launch_bounds__(1024) k_grad_head(const int32_t* labels, const float* lse, const float* dloss,
-                                                    int64_t rows, int64_t classes, int bits, GradHead* head) {
-  __shared__ uint32_t tops[16];
+// Workgroup 0: the head.  dloss's largest value is had by one workgroup, so it needs no second
+// launch (8,192 rows: 6 us).
+__device__ void grad_head(const GradCall& c, int bits, GradHead* head, uint32_t* tops) {
   uint32_t top = 0;
-  for (int64_t i = threadIdx.x; i < rows; i += 1024)
-    if (!no_row(labels, lse, dloss, classes, i)) top = max(top, __float_as_uint(dloss[i]) & 0x7fffffffu);
+  for (int64_t i0 = threadIdx.x; i0 < c.M; i0 += 4 * 1024) {
+    uint32_t one[4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const int64_t i = min(i0 + d * 1024, c.M - 1);
+      const uint32_t size = __float_as_uint(c.dloss[i]) & 0x7fffffffu;
+      one[d] = no_row(c, i) ? 0 : size;
+    }
+#pragma unroll
+    for (int d = 0; d < 4; ++d) top = max(top, one[d]);
+  }
   top = group_max<1024>(top, tops);
   if (threadIdx.x) return;
   const float most = __uint_as_float(top);
@@ -132,92 +142,130 @@ __global__ void __launch_bounds__(1024) k_grad_head(const int32_t* labels, const
   if (top && most < INFINITY) e = bits - min(max(ilogbf(most), -100), 100);
   head->factor = ldexpf(1.0f, e);
   head->inverse = ldexpf(1.0f, -e);
-  head->swap = 0;
 }
 
-// A wave per row: looks through the rows of x that count for nothing.
+// common[k] = the mean of up to 256 classes' weights, spread over all classes; a feature a wave.
 template <typename T>
-__global__ void __launch_bounds__(256) k_grad_scan(const T* x, int64_t ldx, int64_t rows, int64_t cols,
-                                                   const int32_t* labels, const float* lse, const float* dloss,
-                                                   int64_t classes, GradHead* head) {
-  const int64_t i = group_index() * 4 + (threadIdx.x >> 6);
-  if (i >= rows || !no_row(labels, lse, dloss, classes, i)) return;
-  bool bad = false;
-  for (int64_t c = (threadIdx.x & 63) * 8; c < cols; c += 512) {
-    const int n = cols - c >= 8 ? 8 : static_cast<int>(cols - c);
-    float v[8];
-    load8(x + i * ldx + c, n, v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) bad |= !(fabsf(v[e]) < INFINITY);
-  }
-  if (bad) head->swap = 1;             // (the same value, whoever writes it)
-}
-
-// x with zeros in such rows, if there are any.
-template <typename T>
-__global__ void __launch_bounds__(256) k_grad_clean(const T* x, int64_t ldx, int64_t rows, int64_t cols,
-                                                    const int32_t* labels, const float* lse, const float* dloss,
-                                                    int64_t classes, const GradHead* head, T* out, int64_t ldo) {
-  if (head->swap == 0) return;
-  const int lane = threadIdx.x & 63;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); i < rows; i += int64_t(gridDim.x) * 4) {
-    const bool none = no_row(labels, lse, dloss, classes, i);
-    for (int64_t c = lane * 8; c < cols; c += 512) {
-      const int n = cols - c >= 8 ? 8 : static_cast<int>(cols - c);
-      float v[8] = {};
-      if (!none) load8(x + i * ldx + c, n, v);
-      store8(out + i * ldo + c, 8, v);
-    }
-  }
-}
-
-// lost[i] = the row's parts, 16 rows and 16 slices of the strips a workgroup.
-__global__ void __launch_bounds__(256) k_grad_lost(const float* __restrict__ part, int64_t strips, int64_t rows,
-                                                   float* __restrict__ lost) {
-  __shared__ float sums[16][17];
-  const int r = threadIdx.x & 15, slice = threadIdx.x >> 4;
-  const int64_t i = group_index() * 16 + r;
+__device__ void grad_common(const GradCall& c, int64_t group, float* common) {
+  const T* const W = static_cast<const T*>(c.W);
+  const int64_t k = group * 16 + (threadIdx.x >> 6);
+  if (k >= c.K) return;
+  const int64_t some = c.N < kMostCommon ? c.N : kMostCommon;
   float s = 0.0f;
-  if (i < rows) {
-    constexpr int kDeep = 8;
-    for (int64_t p0 = slice; p0 < strips; p0 += 16 * kDeep) {
-      float one[kDeep];
 #pragma unroll
-      for (int d = 0; d < kDeep; ++d) one[d] = p0 + 16 * d < strips ? part[(p0 + 16 * d) * rows + i] : 0.0f;
-#pragma unroll
-      for (int d = 0; d < kDeep; ++d) s += one[d];
-    }
-  }
-  sums[slice][r] = s;
-  __syncthreads();
-  if (slice || i >= rows) return;
-#pragma unroll
-  for (int w = 1; w < 16; ++w) s += sums[w][r];
-  lost[i] = s;
-}
-
-// common[k] = the mean of up to 256 classes' weights, spread over all classes; one feature a wave.
-template <typename T>
-__global__ void __launch_bounds__(256) k_grad_common(const T* W, int64_t ldw, bool units, int64_t classes, int64_t cols,
-                                                     float* common) {
-  const int lane = threadIdx.x & 63;
-  const int64_t k = group_index() * 4 + (threadIdx.x >> 6);
-  if (k >= cols) return;
-  const int64_t some = classes < 256 ? classes : 256;
-  float s = 0.0f;
-  for (int64_t c = lane; c < some; c += 64) {
-    const int64_t n = c * classes / some;
-    s += static_cast<float>(units ? W[n * ldw + k] : W[k * ldw + n]);
+  for (int d = 0; d < kMostCommon / 64; ++d) {
+    const int64_t at = d * 64 + (threadIdx.x & 63), n = at * c.N / some;
+    if (at < some) s += static_cast<float>(c.units ? W[n * c.ldw + k] : W[k * c.ldw + n]);
   }
 #pragma unroll
   for (int off = 32; off; off >>= 1) s += __shfl_xor(s, off, 64);
   s /= static_cast<float>(some);
   // (weights that are not finite make NaNs of what they reach, and no more than that)
-  if (lane == 0) common[k] = fabsf(s) < INFINITY ? s : 0.0f;
+  if ((threadIdx.x & 63) == 0) common[k] = fabsf(s) < INFINITY ? s : 0.0f;
 }
 
-// g and its column sums from a split product's parts: 512 columns a workgroup, every (4
-// gridDim.y)th row, as k_act_grad.
+// Looks through the rows of x that count for nothing, a wave a row; a flag a workgroup.
+template <typename T>
+__device__ void grad_scan(const GradCall& c, int64_t group, int64_t groups, int32_t* flags) {
+  bool bad = false;
+  for (int64_t i = group * 16 + (threadIdx.x >> 6); i < c.M; i += groups * 16) {
+    if (!no_row(c, i)) continue;
+    for (int64_t k = (threadIdx.x & 63) * 8; k < c.K; k += 512) {
+      const int n = c.K - k >= 8 ? 8 : static_cast<int>(c.K - k);
+      float v[8];
+      load8(static_cast<const T*>(c.x) + i * c.ldx + k, n, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bad |= !(fabsf(v[e]) < INFINITY);
+    }
+  }
+  const int any = __syncthreads_or(bad);
+  if (threadIdx.x == 0) flags[group] = any;
+}
+
+// Everything that goes before the scores, by workgroups: the head, `commons` for the common
+// weights, the rest for the rows.
+template <typename T>
+__global__ void __launch_bounds__(1024) k_grad_prepare(const GradCall c, int bits, GradHead* head, int64_t commons,
+                                                       float* common, int32_t* flags) {
+  __shared__ uint32_t tops[16];
+  const int64_t g = group_index();
+  const int64_t scans = int64_t(gridDim.x) * gridDim.y - 1 - commons;
+  if (g == 0)
+    grad_head(c, bits, head, tops);
+  else if (g <= commons)
+    grad_common<T>(c, g - 1, common);
+  else if (g - 1 - commons < scans)
+    grad_scan<T>(c, g - 1 - commons, scans, flags);
+}
+
+// x with zeros in the rows that count for nothing, if one of them is not finite.
+template <typename T>
+__device__ void grad_clean(const GradCall& c, int64_t group, int64_t groups, const int32_t* flags, int nflags,
+                           GradHead* head, T* out, int64_t ldo) {
+  const int any = __syncthreads_or(threadIdx.x < nflags && flags[threadIdx.x]);
+  if (group == 0 && threadIdx.x == 0) head->swap = any;
+  if (!any) return;
+  for (int64_t i = group * 16 + (threadIdx.x >> 6); i < c.M; i += groups * 16) {
+    const bool none = no_row(c, i);
+    for (int64_t k = (threadIdx.x & 63) * 8; k < c.K; k += 512) {
+      const int n = c.K - k >= 8 ? 8 : static_cast<int>(c.K - k);
+      float v[8] = {};
+      if (!none) load8(static_cast<const T*>(c.x) + i * c.ldx + k, n, v);
+      store8(out + i * ldo + k, 8, v);
+    }
+  }
+}
+
+// Columns' sums (out[j] = sum over g of part[g * ld + j], 64 columns a workgroup, in order within
+// fixed groups) or rows' (of part[g * rows + i]), which are the same.
+__device__ void sum_parts(const float* __restrict__ part, int64_t parts, int64_t ld, int64_t n, int64_t group,
+                          float* __restrict__ out, float (&sums)[16][64]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c = group * 64 + lane;
+  float s = 0.0f;
+  if (c < n)
+    for (int64_t g0 = wave; g0 < parts; g0 += 16 * 8) {
+      float v[8];                       // eight on their way
+#pragma unroll
+      for (int d = 0; d < 8; ++d) v[d] = g0 + 16 * d < parts ? part[(g0 + 16 * d) * ld + c] : 0.0f;
+#pragma unroll
+      for (int d = 0; d < 8; ++d) s += v[d];
+    }
+  sums[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && c < n) {
+    for (int w = 1; w < 16; ++w) s += sums[w][lane];
+    out[c] = s;
+  }
+}
+
+// Everything between a piece's scores and its products, by workgroups: `columns` of them for
+// dbias, `losts` for the rows' roundings, the rest for x.
+struct GradBetween {
+  const float *column_part, *lost_part;
+  float *dbias, *lost;
+  int64_t columns, column_parts, ld_column, n, losts, lost_parts;
+  const int32_t* flags;
+  GradHead* head;
+  void* clean;
+  int64_t ld_clean;
+  int nflags;
+};
+template <typename T>
+__global__ void __launch_bounds__(1024) k_grad_between(const GradCall c, const GradBetween b) {
+  __shared__ float sums[16][64];
+  const int64_t g = group_index(), rest = g - b.columns - b.losts;
+  const int64_t cleans = int64_t(gridDim.x) * gridDim.y - b.columns - b.losts;
+  if (g < b.columns)
+    sum_parts(b.column_part, b.column_parts, b.ld_column, b.n, g, b.dbias, sums);
+  else if (rest < 0)
+    sum_parts(b.lost_part, b.lost_parts, c.M, c.M, g - b.columns, b.lost, sums);
+  else
+    grad_clean<T>(c, rest, cleans, b.flags, b.nflags, b.head, static_cast<T*>(b.clean), b.ld_clean);
+}
+
+// g, its column sums and what its rounding takes from each row, from a split product's parts: 512
+// columns a workgroup, every (4 gridDim.y)th row, as k_act_grad.
 __global__ void __launch_bounds__(256) k_grad_scores(const GradArgs a) {
   __shared__ float sums[4][512];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -231,10 +279,20 @@ __global__ void __launch_bounds__(256) k_grad_scores(const GradArgs a) {
     if (n > 0) {
       float v[8];
       join8(a, row, col, v);
-      grad8(a, grad_row(a, row, col, true), bias, v);
+      grad8(a, grad_row(a, row, col, true), factor, bias, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) db[e] += v[e];
-      lost = store_g(a, row, col, n, factor, v);
+      for (int h = 0; h < 2; ++h) {
+        float four[4], rounded = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          four[e] = 4 * h + e < n ? v[4 * h + e] : 0.0f;
+          db[4 * h + e] += four[e];
+          lost += four[e];
+        }
+        const u2 word = round4(a.elem, four, &rounded);
+        lost -= rounded;
+        *reinterpret_cast<u2*>(static_cast<uint16_t*>(a.out) + row * a.ldo + col + 4 * h) = word;
+      }
     }
     if (a.lost_part) {
 #pragma unroll
@@ -249,13 +307,18 @@ __global__ void __launch_bounds__(256) k_grad_scores(const GradArgs a) {
   for (int c = threadIdx.x; c < 512; c += 256) {
     const int64_t at = static_cast<int64_t>(blockIdx.x) * 512 + c;
     if (at < a.J)
-      a.column_part[static_cast<int64_t>(blockIdx.y) * a.ld_column + at] = sums[0][c] + sums[1][c] + sums[2][c] + sums[3][c];
+      a.column_part[static_cast<int64_t>(blockIdx.y) * a.ld_column + at] =
+          (sums[0][c] + sums[1][c] + sums[2][c] + sums[3][c]) / factor;
   }
 }
 
 int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
 size_t most(size_t a, size_t b) { return a > b ? a : b; }
 
+int64_t scan_groups(int64_t rows) {
+  const int64_t g = (rows + 15) / 16;
+  return g < kScanGroups ? g : kScanGroups;
+}
 int64_t scores_groups(int64_t rows) {
   const int64_t g = (rows + 3) / 4;
   return g < 64 ? g : 64;
@@ -329,6 +392,8 @@ GradWs grad_ws(int64_t M, int64_t N, int64_t K, int elem) {
   o += align_up(sizeof(float) * w.ldx, 256);
   w.lost = o;
   o += align_up(sizeof(float) * M, 256);
+  w.flags = o;
+  o += sizeof(int32_t) * kScanGroups;
   w.lost_part = o;                     // a wave's columns: 32 at the least
   o += align_up(sizeof(float) * M * ((w.piece + 255) / 256 * 8), 256);
   w.partial = o;
@@ -407,33 +472,47 @@ hipError_t launch_loss(const LossCall& c, void* ws, hipStream_t stream) {
 }
 
 template <typename T>
-static hipError_t prepare_rows(const GradCall& c, const GradWs& w, void* ws, hipStream_t stream) {
-  GradHead* const head = at<GradHead>(ws, w.head);
-  hipLaunchKernelGGL(k_grad_head, dim3(1), dim3(1024), 0, stream, c.labels, c.lse, c.dloss, c.M, c.N,
-                     c.dtype == kF16 ? 14 : 0, head);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (c.dx) {
-    hipLaunchKernelGGL(k_grad_common<T>, groups_grid((c.K + 3) / 4), dim3(256), 0, stream, static_cast<const T*>(c.W), c.ldw,
-                       c.units, c.N, c.K, at<float>(ws, w.common));
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
+static hipError_t prepare(const GradCall& c, const GradWs& w, void* ws, hipStream_t stream) {
+  const int64_t commons = c.dx ? (c.K + 15) / 16 : 0, scans = c.dW ? scan_groups(c.M) : 0;
+  hipLaunchKernelGGL(k_grad_prepare<T>, groups_grid(1 + commons + scans), dim3(1024), 0, stream, c,
+                     c.dtype == kF16 ? 14 : 0, at<GradHead>(ws, w.head), commons, at<float>(ws, w.common),
+                     at<int32_t>(ws, w.flags));
+  return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t between(const GradCall& c, const GradWs& w, const GradArgs& a, int64_t column_parts, int64_t strips,
+                          bool first, void* ws, hipStream_t stream) {
+  GradBetween b{};
+  if (c.dbias) {
+    b.columns = (a.J + 63) / 64;
+    b.column_part = a.column_part;
+    b.column_parts = column_parts;
+    b.ld_column = a.ld_column;
+    b.n = a.J;
+    b.dbias = c.dbias + a.first;
   }
-  if (!c.dW) return hipSuccess;
-  const T* const x = static_cast<const T*>(c.x);
-  hipLaunchKernelGGL(k_grad_scan<T>, groups_grid((c.M + 3) / 4), dim3(256), 0, stream, x, c.ldx, c.M, c.K, c.labels,
-                     c.lse, c.dloss, c.N, head);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int64_t groups = (c.M + 3) / 4;
-  hipLaunchKernelGGL(k_grad_clean<T>, dim3(static_cast<uint32_t>(groups < 2048 ? groups : 2048)), dim3(256), 0, stream, x,
-                     c.ldx, c.M, c.K, c.labels, c.lse, c.dloss, c.N, head, at<T>(ws, w.clean), w.ldx);
+  if (c.dx) {
+    b.losts = (c.M + 63) / 64;
+    b.lost_part = a.lost_part;
+    b.lost_parts = strips;
+    b.lost = at<float>(ws, w.lost);
+  }
+  const int64_t scans = c.dW && first ? scan_groups(c.M) : 0;
+  b.flags = at<int32_t>(ws, w.flags);
+  b.nflags = static_cast<int>(scans);
+  b.head = at<GradHead>(ws, w.head);
+  b.clean = at<void>(ws, w.clean);
+  b.ld_clean = w.ldx;
+  const int64_t groups = b.columns + b.losts + scans;
+  if (groups == 0) return hipSuccess;
+  hipLaunchKernelGGL(k_grad_between<T>, groups_grid(groups), dim3(1024), 0, stream, c, b);
   return hipGetLastError();
 }
 
 hipError_t launch_loss_back(const GradCall& c, void* ws, hipStream_t stream) {
   const GradWs w = grad_ws(c.M, c.N, c.K, c.dtype);
-  hipError_t e = c.dtype == kF16 ? prepare_rows<f16>(c, w, ws, stream) : prepare_rows<bf16>(c, w, ws, stream);
+  hipError_t e = c.dtype == kF16 ? prepare<f16>(c, w, ws, stream) : prepare<bf16>(c, w, ws, stream);
   if (e != hipSuccess) return e;
   GradHead* const head = at<GradHead>(ws, w.head);
   float* const partial = at<float>(ws, w.partial);
@@ -480,16 +559,9 @@ hipError_t launch_loss_back(const GradCall& c, void* ws, hipStream_t stream) {
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
-    if (c.dbias) {
-      e = launch_column_sums(a.column_part, groups, w.ld_column, n, c.dbias + n0, stream);
-      if (e != hipSuccess) return e;
-    }
-    if (c.dx) {
-      hipLaunchKernelGGL(k_grad_lost, groups_grid((c.M + 15) / 16), dim3(256), 0, stream, a.lost_part, strips, c.M,
-                         at<float>(ws, w.lost));
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
-    }
+    e = c.dtype == kF16 ? between<f16>(c, w, a, groups, strips, n0 == 0, ws, stream)
+                        : between<bf16>(c, w, a, groups, strips, n0 == 0, ws, stream);
+    if (e != hipSuccess) return e;
     ExtraArgs d{};
     d.elem = c.dtype;
     d.alpha = c.alpha;

@@ -236,110 +236,172 @@ __device__ __forceinline__ void loss_tile(const TileOf& tile, const LossArgs& a,
 // ---------------------------------------------------------------------------
 
 struct GradRow {
-  int64_t label;             // among the eight columns' classes, counted from their first
+  int label;                 // counted from the caller's first column
   float lse, dloss;          // dloss: 0 where the row has no label, or no score to choose from
 };
 
 __device__ __forceinline__ GradRow grad_row(const GradArgs& a, int64_t i, int64_t j, bool in) {
   GradRow r = {-1, 0.0f, 0.0f};
   if (!in) return r;
-  const int64_t label = a.labels[i];
+  const int label = a.labels[i];
   const float lse = a.lse[i];
   if (label < 0 || label >= a.classes || lse == -INFINITY) return r;
-  r.label = label - a.first - j;
+  r.label = label - static_cast<int>(a.first + j);           // (classes are at most 2^30)
   r.lse = lse;
   r.dloss = a.dloss[i];
   return r;
 }
 
-// g of eight columns from their sums, in place; a row without a label gives zeros whatever its sums.
-__device__ __forceinline__ void grad8(const GradArgs& a, const GradRow& r, const float (&bias)[8], float (&v)[8]) {
+// g times `factor` of eight columns from their sums, in place; a row without a label gives zeros
+// whatever its sums.
+__device__ __forceinline__ void grad8(const GradArgs& a, const GradRow& r, float factor, const float (&bias)[8],
+                                      float (&v)[8]) {
+  const float d = r.dloss * factor;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float z = bias[e] == -INFINITY ? -INFINITY : fmaf(v[e], a.alpha, bias[e]);
-    const float p = __builtin_amdgcn_exp2f(kLog2e * (z - r.lse));
-    v[e] = r.dloss == 0.0f ? 0.0f : r.dloss * (r.label == e ? p - 1.0f : p);
+    const float p = __builtin_amdgcn_exp2f(fmaf(v[e], a.alpha * kLog2e, kLog2e * bias[e] - kLog2e * r.lse));
+    v[e] = r.dloss == 0.0f ? 0.0f : r.label == e ? fmaf(d, p, -d) : d * p;
   }
 }
 
-// Eight values of g times `factor`, rounded to T; returns what the rounding of n of them took away.
-template <typename T>
-__device__ __forceinline__ float store_g(T* p, int n, float factor, const float (&g)[8]) {
-  typename Eight<T>::vec r;
-  float lost = 0.0f;
+// Four values rounded to the operands' type, as they are stored, and sum plus the rounded ones
+// (by the dot product with ones: two values an instruction).
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u2 round4(int elem, const float (&v)[4], float* sum) {
+  typedef bf16 b2 __attribute__((ext_vector_type(2)));
+  u2 word;
+  if (elem == kF16) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float v = g[e] * factor;
-    r[e] = static_cast<T>(v);
-    lost += e < n ? v - static_cast<float>(r[e]) : 0.0f;
+    for (int h = 0; h < 2; ++h) {
+      const h2 r = {static_cast<f16>(v[2 * h]), static_cast<f16>(v[2 * h + 1])};
+      *sum = __builtin_amdgcn_fdot2(r, h2{static_cast<f16>(1.0f), static_cast<f16>(1.0f)}, *sum, false);
+      word[h] = __builtin_bit_cast(uint32_t, r);
+    }
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const b2 r = {static_cast<bf16>(v[2 * h]), static_cast<bf16>(v[2 * h + 1])};
+      *sum = __builtin_amdgcn_fdot2_f32_bf16(r, b2{static_cast<bf16>(1.0f), static_cast<bf16>(1.0f)}, *sum, false);
+      word[h] = __builtin_bit_cast(uint32_t, r);
+    }
   }
-  *reinterpret_cast<typename Eight<T>::at*>(p) = r;
-  return lost;
-}
-__device__ __forceinline__ float store_g(const GradArgs& a, int64_t i, int64_t j, int n, float factor, const float (&g)[8]) {
-  return a.elem == kF16 ? store_g(static_cast<f16*>(a.out) + i * a.ldo + j, n, factor, g)
-                        : store_g(static_cast<bf16*>(a.out) + i * a.ldo + j, n, factor, g);
+  return word;
 }
 
+// Straight from the matrix instructions' registers, as loss_tile: a lane has four consecutive classes
+// of a row in each of TJ places.  exp(v - lse) is a power of two of alpha log2(e) sum + (bias - lse) log2(e);
+// the label's class is looked for once a row and wave.
 template <class TileOf, int TI, int TJ>
 __device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a, const f4 (&acc)[TI][TJ],
                                           const TilePlace& place) {
   if (a.splits > 1) return tile.part(a, acc, place.split);
-  constexpr int kAhead = TileOf::kAhead, kLanes = TileOf::kLanes, WI = TileOf::kWI, WJ = TileOf::kWJ;
-  constexpr int BJ = WJ * TJ * 16;
-  float bias[8], sums[8] = {};
+  constexpr int WI = TileOf::kWI, WJ = TileOf::kWJ, BJ = WJ * TJ * 16;
+  const int wi = tile.wave / WJ, wj = tile.wave % WJ, g = tile.lane >> 4;
+  const int64_t wave_j = tile.j0 + wj * TJ * 16, j = wave_j + g * 4;        // + y * 16 + e
+  const float factor = *a.factor, alpha = a.alpha * kLog2e;
+  float bias[TJ][4], sums[TJ][4];
+  const int left = static_cast<int>(min<int64_t>(a.J - wave_j, TJ * 16));
 #pragma unroll
-  for (int e = 0; e < 8; ++e) bias[e] = 0.0f;
-  if (a.bias) load8(a.bias + tile.j, tile.n, bias);
-  const float factor = *a.factor;
+  for (int y = 0; y < TJ; ++y)
 #pragma unroll
-  for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(bias[e]));
-  auto terms = [&](int g) __attribute__((always_inline)) {
-    const int64_t i = tile.first + g * TileOf::kRows;
-    return grad_row(a, i, tile.j, g < TileOf::kGroups && i < a.I && tile.n > 0);
-  };
-  GradRow ahead[kAhead];
+    for (int e = 0; e < 4; ++e) {
+      bias[y][e] = y * 16 + g * 4 + e >= left ? -INFINITY : a.bias ? kLog2e * a.bias[j + y * 16 + e] : 0.0f;
+      sums[y][e] = 0.0f;
+    }
+  // The rows' terms by way of LDS: one wait for all of them, and no registers.
+  typedef float f3 __attribute__((ext_vector_type(3)));
+  typedef __attribute__((address_space(3))) f3 lds_f3;
+  typedef __attribute__((address_space(3))) float lds_float;
+  lds_float* const all = reinterpret_cast<lds_float*>(tile.lds);      // [WI][BJ], column sums
+  lds_f3* const terms = reinterpret_cast<lds_f3*>(tile.lds + WI * BJ * 4);       // [BI], 16 bytes each
+  if (threadIdx.x < WI * TI * 16) {
+    const int64_t i = tile.i0 + threadIdx.x;
+    const GradRow r = grad_row(a, i, tile.j0, i < a.I);
+    terms[threadIdx.x] = f3{__int_as_float(r.label), kLog2e * r.lse, r.dloss * factor};
+  }
+  __syncthreads();
+  const int rows = static_cast<int>(min<int64_t>(a.I - tile.i0, WI * TI * 16));
+  int row = wi * TI * 16 + (tile.lane & 15);
+  uint16_t* out = static_cast<uint16_t*>(a.out) + (tile.i0 + row) * a.ldo + wave_j;
+  float* lost_part = a.lost_part + (place.tj * WJ + wj) * a.I + tile.i0;
 #pragma unroll
-  for (int g = 0; g < kAhead; ++g) ahead[g] = terms(g);
-  tile.rows(acc, [&](int g, int64_t i, float (&v)[8]) __attribute__((always_inline)) {
-    const GradRow now = ahead[0];
+  for (int x = 0; x < TI; ++x, row += 16, out += 16 * a.ldo) {
+    // (row by row: all rows' terms at once take the registers that the sums are in)
+    __builtin_amdgcn_sched_barrier(0);
+    const f3 r = terms[row];
+    const float lse = r[1], d = r[2];
+    const int label = __float_as_int(r[0]) - wj * TJ * 16;
+    const bool none = d == 0.0f, here = label >= 0 && label < TJ * 16 && (label >> 2 & 3) == g;
+    float v[TJ][4], lost = 0.0f;
 #pragma unroll
-    for (int k = 0; k + 1 < kAhead; ++k) ahead[k] = ahead[k + 1];
-    ahead[kAhead - 1] = terms(g + kAhead);
-    const bool in = i < a.I && tile.n > 0;
-    float lost = 0.0f;
-    if (in) {
-      grad8(a, now, bias, v);
+    for (int y = 0; y < TJ; ++y)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sums[e] += v[e];
-      lost = store_g(a, i, tile.j, tile.n, factor, v);
+      for (int e = 0; e < 4; ++e)
+        v[y][e] = d * __builtin_amdgcn_exp2f(fmaf(acc[x][y][e], alpha, bias[y][e] - lse));
+    if (__any(here)) {
+#pragma unroll
+      for (int y = 0; y < TJ; ++y)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (here && label == y * 16 + g * 4 + e) v[y][e] -= d;
+    }
+    if (__any(none)) {                   // zeros whatever the sums hold
+#pragma unroll
+      for (int y = 0; y < TJ; ++y)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[y][e] = none ? 0.0f : v[y][e];
+    }
+    float rounded = 0.0f;
+    u2 word[TJ];
+#pragma unroll
+    for (int y = 0; y < TJ; ++y) {
+      word[y] = round4(a.elem, v[y], &rounded);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        lost += v[y][e];
+        sums[y][e] += v[y][e];
+        // (here: left to the compiler, the sums are made where they are used, and v is kept for that)
+        asm volatile("" : "+v"(sums[y][e]));
+      }
+    }
+    lost -= rounded;
+    // Of two places 16 columns apart the lanes of odd g give up the first and those of even g the
+    // second, so that a lane has eight consecutive columns and a row's lanes 64 bytes.
+#pragma unroll
+    for (int y = 0; y < TJ; y += 2) {
+      u4 both;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u2 swapped = __builtin_amdgcn_permlane16_swap(word[y][h], word[y + 1][h], false, false);
+        both[h] = swapped[0];
+        both[2 + h] = swapped[1];
+      }
+      const int at = (y + (g & 1)) * 16 + (g >> 1) * 8;
+      if (row < rows && at < left) *reinterpret_cast<u4*>(out + at) = both;
     }
     if (a.lost_part) {
-#pragma unroll
-      for (int off = 1; off < kLanes; off <<= 1) lost += __shfl_xor(lost, off, 64);
-      if (i < a.I && tile.col == 0) a.lost_part[(place.tj * WJ + tile.wave % WJ) * a.I + i] = lost;
+      lost += __shfl_xor(lost, 16, 64);
+      lost += __shfl_xor(lost, 32, 64);
+      if (g == 0 && row < rows) lost_part[row] = lost;
     }
-  });
+  }
   if (!a.column_part) return;
   // over the lanes that share the columns, then over the waves below each other, in order
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
+  for (int y = 0; y < TJ; ++y)
 #pragma unroll
-    for (int off = kLanes; off < 64; off <<= 1) sums[e] += __shfl_xor(sums[e], off, 64);
-  __syncthreads();
-  typedef __attribute__((address_space(3))) float lds_float;
-  lds_float* const all = reinterpret_cast<lds_float*>(tile.lds);      // [WI][BJ]
-  if (tile.lane < kLanes) {
+    for (int e = 0; e < 4; ++e) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) all[tile.wave / WJ * BJ + tile.wave % WJ * TJ * 16 + tile.lane * 8 + e] = sums[e];
-  }
+      for (int off = 1; off < 16; off <<= 1) sums[y][e] += __shfl_xor(sums[y][e], off, 64);
+      if ((tile.lane & 15) == 0) all[wi * BJ + wj * TJ * 16 + y * 16 + g * 4 + e] = sums[y][e];
+    }
   __syncthreads();
-  const int64_t j = tile.j0 + threadIdx.x;
-  if (threadIdx.x < BJ && j < a.J) {
+  const int64_t col = tile.j0 + threadIdx.x;
+  if (threadIdx.x < BJ && col < a.J) {
     float s = all[threadIdx.x];
 #pragma unroll
     for (int w = 1; w < WI; ++w) s += all[w * BJ + threadIdx.x];
-    a.column_part[place.ti * a.ld_column + j] = s;
+    a.column_part[place.ti * a.ld_column + col] = s / factor;          // (a power of two)
   }
 }
 
