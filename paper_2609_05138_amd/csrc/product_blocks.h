@@ -164,10 +164,14 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product_blocks(const BlockArgs 
   };
   auto multiply = [&](int x, int y) __attribute__((always_inline)) {
     const int n = x * TJ + y, at = n % kRing;
-    // (the tile kLate before this one; the first ones' are the last of the step before)
-    if (kCarry || n >= kLate) enter((n + kTiles - kLate) % kTiles);
+    // One matrix instruction, then, while it runs, the sums of the tile kLate before (the first
+    // ones' are the last of the step before).  In this order: left to the compiler, three matrix
+    // instructions follow each other and the sums wait for the last (1.81 us a step of 256 x 256).
     ring[at] = block_sum<EXACT>(fq[y], fp[x & 1]);
     late_scale[at] = UNITS ? by_row[x & 1] : by_row[x & 1] * by_unit;
+    __builtin_amdgcn_sched_barrier(0);
+    if (kCarry || n >= kLate) enter((n + kTiles - kLate) % kTiles);
+    __builtin_amdgcn_sched_barrier(0);
   };
   auto drain = [&]() __attribute__((always_inline)) {
 #pragma unroll

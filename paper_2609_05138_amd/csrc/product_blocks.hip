@@ -115,8 +115,7 @@ hipError_t launch_shape(int shape, const BlockArgs& a, hipStream_t stream) {
       if constexpr (!EXACT) return launch_one<kShape256, EXACT, UNITS, 2, 4, 8, 4, 2>(a, stream);
       return hipErrorInvalidValue;
     case kShape256x128:
-      if constexpr (!EXACT) return launch_one<kShape256x128, EXACT, UNITS, 4, 2, 4, 4, 3>(a, stream);
-      return hipErrorInvalidValue;
+      return launch_one<kShape256x128, EXACT, UNITS, 4, 2, 4, 4, 3>(a, stream);
     case kShape128:
       return launch_one<kShape128, EXACT, UNITS, 2, 4, 4, 2, 4>(a, stream);
     case kShape64:
@@ -131,7 +130,7 @@ hipError_t launch_shape(int shape, const BlockArgs& a, hipStream_t stream) {
 }  // namespace
 
 ProductPlan plan_blocks(int64_t I, int64_t J, int64_t K, bool dma, bool exact) {
-  if (exact) return plan_product(I, J, K, kE4M3, true, true, dma, true, kShape128);
+  if (exact) return plan_product(I, J, K, kE4M3, true, true, dma, true, kShape256x128);
   // a step of the 8-bit instructions takes what one of 16 bits and half the k does
   ProductPlan p = plan_product(I, J, (K + 1) / 2, kBF16, true, true, dma);
   p.k_split *= 2;
