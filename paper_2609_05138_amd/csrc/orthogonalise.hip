@@ -16,6 +16,10 @@
 // X lies in rows and columns rounded up to 64 (a step of the product), with zeros, which stay
 // zeros: no product but the last, whose result is y, has a partial step or column.
 //
+// Small matrices take products of their own: tiles of 32 x 32, whose eight waves share the k axis and read their fragments from the L2 without LDS, so that a
+// product is little more than a launch and two memory latencies.  They read rows of k only, so
+// X's fp16 copy is kept transposed too.
+//
 // Bound: the matrix cores for sides of 2,048 and more; else 3 launches a step.
 #include "orthogonalise.h"
 
@@ -27,6 +31,10 @@ namespace som {
 namespace {
 
 constexpr int kParts = 512;            // sums of squares, one a workgroup
+// Up to this size the small products are taken (us a call, theirs and the large ones': 64 x 64 46
+// and 57, 512 x 512 82 and 92, 1,024 x 512 104 and 116; 1,024 x 1,024 272 and 151, 256 x 4,096 147
+// and 118, since their fragments come from the L2 64 bytes a row).
+constexpr int64_t kSmall = 1 << 19, kSmallSide = 1024;
 
 // Sum over the workgroup's 256 threads, in a fixed order.
 __device__ __forceinline__ double sum256(double v, double* part) {
@@ -56,17 +64,18 @@ __global__ void __launch_bounds__(256) k_ortho_squares(const T* G, int64_t ldg, 
   if (threadIdx.x == 0) parts[blockIdx.x] = s;
 }
 
-// X and its fp16 copy, [all_rows][ldx], zeros beyond G.
+// X and its fp16 copy, all_rows x all_cols, zeros beyond G.
 template <typename T>
 __global__ void __launch_bounds__(256) k_ortho_start(const T* G, int64_t ldg, int64_t rows, int64_t cols,
                                                      const double* parts, int nparts, float* X, f16* half,
-                                                     int64_t all_rows, int64_t ldx, float scale) {
+                                                     int64_t all_rows, int64_t all_cols, int64_t ldx,
+                                                     float scale) {
   __shared__ double part[4];
   double s = 0.0;
   for (int p = threadIdx.x; p < nparts; p += 256) s += parts[p];
   s = sum256(s, part);
   const double inverse = s == 0.0 ? 0.0 : 1.0 / sqrt(s);
-  const int64_t groups = ldx / 8, all = groups * all_rows;
+  const int64_t groups = all_cols / 8, all = groups * all_rows;
   for (int64_t g = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; g < all; g += int64_t(gridDim.x) * 256) {
     const int64_t row = g / groups, col = (g - row * groups) * 8;
     float v[8];
@@ -78,6 +87,186 @@ __global__ void __launch_bounds__(256) k_ortho_start(const T* G, int64_t ldg, in
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= scale;
     store8(half + row * ldx + col, 8, v);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Small products
+// ---------------------------------------------------------------------------
+
+constexpr int kSmallWaves = 8;
+
+// C[i][j] = alpha sum_k P[i][k] Q[j][k] + beta residual; I, J and K are multiples of 64.
+struct SmallArgs {
+  const f16 *P, *Q;
+  int64_t ldp, ldq;
+  int32_t I, J, K;
+  float alpha, beta;
+  const void* residual;      // fp32 (or fp16 with res_half), or nullptr
+  bool res_half;
+  int64_t ldr;
+  void* out;                 // of out_type, rows x cols of it; or nullptr
+  int out_type;
+  int64_t ldo, rows, cols;
+  f16 *half, *half_t;        // [I][ldh] and its transpose [J][ldt], times half_scale; or nullptr
+  int64_t ldh, ldt;
+  float half_scale;
+};
+
+// 32 x 32 a workgroup; wave w takes the steps w, w + 8, ... of 64 of k.
+__global__ void __launch_bounds__(kSmallWaves * 64) k_ortho_small(const SmallArgs a) {
+  constexpr int TT = 2, kSide = TT * 16, kRow = kSide + 4;     // floats; 4 more: other banks
+  __shared__ __align__(16) float sums[kSmallWaves * kSide * kRow];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
+  const int tiles_j = a.J / kSide;
+  const int ti = blockIdx.x / tiles_j, tj = blockIdx.x - ti * tiles_j;
+  const f16* const p = a.P + static_cast<int64_t>(ti * kSide + r) * a.ldp + g * 8;
+  const f16* const q = a.Q + static_cast<int64_t>(tj * kSide + r) * a.ldq + g * 8;
+  const int steps = a.K / 64, active = min(steps, kSmallWaves);
+  f4 acc[TT][TT];
+#pragma unroll
+  for (int x = 0; x < TT; ++x)
+#pragma unroll
+    for (int y = 0; y < TT; ++y) acc[x][y] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+  struct Step {
+    h8 p[TT][2], q[TT][2];
+  };
+  auto load = [&](Step& s, int step) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) s.p[t][h] = *reinterpret_cast<const h8*>(p + t * 16 * a.ldp + step * 64 + h * 32);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) s.q[t][h] = *reinterpret_cast<const h8*>(q + t * 16 * a.ldq + step * 64 + h * 32);
+    }
+  };
+  auto multiply = [&](const Step& s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int x = 0; x < TT; ++x)
+#pragma unroll
+        for (int y = 0; y < TT; ++y)
+          acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(s.q[y][h], s.p[x][h], acc[x][y], 0, 0, 0);
+  };
+  typedef f16 h4 __attribute__((ext_vector_type(4)));
+  // four columns of C, of half the threads; the residual, asked for before anything is waited for
+  const bool mine = threadIdx.x < kSide * kSide / 4;
+  const int row = threadIdx.x / (kSide / 4), col = threadIdx.x % (kSide / 4) * 4;
+  const int64_t i = ti * kSide + row, j = tj * kSide + col;
+  f4 res = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (mine && a.residual && !a.res_half)
+    res = *reinterpret_cast<const f4*>(static_cast<const float*>(a.residual) + i * a.ldr + j);
+  if (mine && a.residual && a.res_half) {
+    const h4 h = *reinterpret_cast<const h4*>(static_cast<const f16*>(a.residual) + i * a.ldr + j);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) res[e] = static_cast<float>(h[e]);
+  }
+  if (wave < steps) {
+    constexpr int kDeep = 2;           // steps on their way
+    Step some[kDeep];
+    for (int s0 = wave; s0 < steps; s0 += kSmallWaves * kDeep) {
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d)
+        if (s0 + d * kSmallWaves < steps) load(some[d], s0 + d * kSmallWaves);
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d)
+        if (s0 + d * kSmallWaves < steps) multiply(some[d]);
+    }
+#pragma unroll
+    for (int x = 0; x < TT; ++x)
+#pragma unroll
+      for (int y = 0; y < TT; ++y)
+        *reinterpret_cast<f4*>(&sums[(wave * kSide + x * 16 + r) * kRow + y * 16 + g * 4]) = acc[x][y];
+  }
+  __syncthreads();
+  f4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (mine) {
+    for (int w = 0; w < active; ++w) v += *reinterpret_cast<const f4*>(&sums[(w * kSide + row) * kRow + col]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fmaf(a.beta, res[e], a.alpha * v[e]);
+    if (a.out && i < a.rows) {
+      if (a.out_type == kF32) {          // X, whose rows are padded
+        *reinterpret_cast<f4*>(static_cast<float*>(a.out) + i * a.ldo + j) = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (j + e < a.cols) static_cast<bf16*>(a.out)[i * a.ldo + j + e] = static_cast<bf16>(v[e]);
+      }
+    }
+    if (a.half) {
+      h4 h;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[e] = static_cast<f16>(v[e] * a.half_scale);
+      *reinterpret_cast<h4*>(a.half + i * a.ldh + j) = h;
+    }
+  }
+  if (!a.half_t) return;
+  // the transpose, by way of the first wave's place
+  __syncthreads();
+  if (mine) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[(col + e) * kRow + row] = v[e] * a.half_scale;
+  }
+  __syncthreads();
+  if (mine) {
+    const f4 s = *reinterpret_cast<const f4*>(&sums[row * kRow + col]);
+    const h4 h = {static_cast<f16>(s[0]), static_cast<f16>(s[1]), static_cast<f16>(s[2]), static_cast<f16>(s[3])};
+    *reinterpret_cast<h4*>(a.half_t + static_cast<int64_t>(tj * kSide + row) * a.ldt + ti * kSide + col) = h;
+  }
+}
+
+hipError_t launch_small(const SmallArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(k_ortho_small, dim3(static_cast<uint32_t>((a.I / 32) * (a.J / 32))), dim3(kSmallWaves * 64), 0, stream,
+                     a);
+  return hipGetLastError();
+}
+
+// X, its fp16 copy and that copy's transpose, 64 x 64 a workgroup.
+template <typename T>
+__global__ void __launch_bounds__(256) k_ortho_start_small(const T* G, int64_t ldg, int64_t rows, int64_t cols,
+                                                           const double* parts, int nparts, float* X, f16* half,
+                                                           int64_t ldx, f16* half_t, int64_t ldt, int64_t all_cols, float scale) {
+  __shared__ double part[4];
+  __shared__ float tile[64][65];
+  const int64_t across = all_cols / 64, ti = blockIdx.x / across, tj = blockIdx.x - ti * across;
+  float all[2][8];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const int at = n * 256 + threadIdx.x, r = at >> 3, c = (at & 7) * 8;
+    const int64_t row = ti * 64 + r, col = tj * 64 + c;
+    const int some = row >= rows || col >= cols ? 0 : cols - col >= 8 ? 8 : static_cast<int>(cols - col);
+    load8(G + row * ldg + col, some, all[n]);                  // (zeros beyond)
+  }
+  double s = 0.0;
+  for (int p = threadIdx.x; p < nparts; p += 256) s += parts[p];
+  s = sum256(s, part);
+  const double inverse = s == 0.0 ? 0.0 : 1.0 / sqrt(s);
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const int at = n * 256 + threadIdx.x, r = at >> 3, c = (at & 7) * 8;
+    const int64_t row = ti * 64 + r, col = tj * 64 + c;
+    float v[8];
+    // (beyond G zeros, also where the norm is not a number)
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      v[e] = row < rows && col + e < cols ? static_cast<float>(all[n][e] * inverse) : 0.0f;
+    store8(X + row * ldx + col, 8, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] *= scale;
+      tile[c + e][r] = v[e];
+    }
+    store8(half + row * ldx + col, 8, v);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const int at = n * 256 + threadIdx.x, r = at >> 3, c = (at & 7) * 8;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = tile[r][c + e];
+    store8(half_t + (tj * 64 + r) * ldt + ti * 64 + c, 8, v);
   }
 }
 
@@ -109,6 +298,7 @@ Step step_of(int64_t rows, int64_t cols, bool tall) {
   s.gram.K = n;
   s.gram.p_kc = s.gram.q_kc = !tall;
   s.poly.p_kc = s.poly.q_kc = true;            // A and B are symmetric
+  s.gram.symmetric = s.poly.symmetric = true;
   s.update.I = rows;
   s.update.J = cols;
   s.update.K = m;
@@ -118,7 +308,7 @@ Step step_of(int64_t rows, int64_t cols, bool tall) {
 }
 
 size_t partial_floats(const ExtraArgs& a) {
-  return plan_extra(a.I, a.J, a.K, a.elem, a.p_kc, a.q_kc, true).partial_floats;
+  return plan_extra(a.I, a.J, a.K, a.elem, a.p_kc, a.q_kc, true, a.symmetric).partial_floats;
 }
 
 }  // namespace
@@ -127,8 +317,11 @@ OrthoWs ortho_ws(int64_t rows, int64_t cols) {
   OrthoWs w{};
   const bool tall = rows > cols;
   w.rows = round64(rows);
-  w.ldx = round64(cols);
-  w.ldm = tall ? w.ldx : w.rows;
+  w.cols = round64(cols);
+  w.short_side = tall ? w.cols : w.rows;
+  w.ldx = w.cols;
+  w.ldt = w.rows;
+  w.ldm = w.short_side;
   size_t o = sizeof(double) * kParts;
   w.x = o;
   o += align_up(sizeof(float) * w.rows * w.ldx, 256);
@@ -136,12 +329,19 @@ OrthoWs ortho_ws(int64_t rows, int64_t cols) {
     h = o;
     o += align_up(2 * w.rows * w.ldx, 256);
   }
+  w.small = w.rows * w.cols <= kSmall && w.rows <= kSmallSide && w.cols <= kSmallSide;
+  if (w.small)
+    for (size_t& h : w.half_t) {
+      h = o;
+      o += align_up(2 * w.cols * w.ldt, 256);
+    }
   for (size_t* g : {&w.gram, &w.poly}) {
     *g = o;
-    o += align_up(2 * w.ldm * w.ldm, 256);
+    o += align_up(2 * w.short_side * w.ldm, 256);
   }
-  w.partial = o;
-  const Step s = step_of(w.rows, w.ldx, tall);
+  w.partial = w.total = o;
+  if (w.small) return w;
+  const Step s = step_of(w.rows, w.cols, tall);
   size_t need = 0;
   for (const ExtraArgs* p : {&s.gram, &s.poly, &s.update}) {
     const size_t f = partial_floats(*p);
@@ -158,15 +358,90 @@ OrthoWs ortho_ws(int64_t rows, int64_t cols) {
 template <typename T>
 static hipError_t start(const OrthoCall& c, const OrthoWs& w, float scale, void* ws, hipStream_t stream) {
   const int groups = norm_groups(c.rows, c.cols);
-  hipLaunchKernelGGL(k_ortho_squares<T>, dim3(groups), dim3(256), 0, stream, static_cast<const T*>(c.G), c.ldg, c.rows,
-                     c.cols, at<double>(ws, w.parts));
+  const T* const G = static_cast<const T*>(c.G);
+  double* const parts = at<double>(ws, w.parts);
+  float* const X = at<float>(ws, w.x);
+  f16* const half = at<f16>(ws, w.half[0]);
+  hipLaunchKernelGGL(k_ortho_squares<T>, dim3(groups), dim3(256), 0, stream, G, c.ldg, c.rows, c.cols, parts);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t all = (w.ldx / 8 * w.rows + 255) / 256;
-  hipLaunchKernelGGL(k_ortho_start<T>, dim3(static_cast<uint32_t>(all < 2048 ? all : 2048)), dim3(256), 0, stream,
-                     static_cast<const T*>(c.G), c.ldg, c.rows, c.cols, at<double>(ws, w.parts), groups,
-                     at<float>(ws, w.x), at<f16>(ws, w.half[0]), w.rows, w.ldx, scale);
+  if (w.small) {
+    hipLaunchKernelGGL(k_ortho_start_small<T>, dim3(static_cast<uint32_t>(w.rows / 64 * (w.cols / 64))), dim3(256), 0, stream,
+                       G, c.ldg, c.rows, c.cols, parts, groups, X, half, w.ldx, at<f16>(ws, w.half_t[0]), w.ldt, w.cols, scale);
+  } else {
+    const int64_t all = (w.cols / 8 * w.rows + 255) / 256;
+    hipLaunchKernelGGL(k_ortho_start<T>, dim3(static_cast<uint32_t>(all < 2048 ? all : 2048)), dim3(256), 0, stream, G, c.ldg,
+                       c.rows, c.cols, parts, groups, X, half, w.rows, w.cols, w.ldx, scale);
+  }
   return hipGetLastError();
+}
+
+static hipError_t small_steps(const OrthoCall& c, const OrthoWs& w, float scale, void* ws, hipStream_t stream) {
+  const bool tall = c.rows > c.cols;
+  const float inverse = 1.0f / scale;
+  f16 *const A = at<f16>(ws, w.gram), *const B = at<f16>(ws, w.poly);
+  const int32_t m = static_cast<int32_t>(w.short_side), rows = static_cast<int32_t>(w.rows), cols = static_cast<int32_t>(w.cols);
+  for (int t = 0; t < c.steps; ++t) {
+    const f16 *const now = at<f16>(ws, w.half[t & 1]), *const now_t = at<f16>(ws, w.half_t[t & 1]);
+    SmallArgs s{};
+    s.P = s.Q = tall ? now_t : now;
+    s.ldp = s.ldq = tall ? w.ldt : w.ldx;
+    s.I = s.J = m;
+    s.K = tall ? rows : cols;
+    s.alpha = inverse * inverse;
+    s.half = A;
+    s.ldh = w.ldm;
+    s.half_scale = 1.0f;
+    hipError_t e = launch_small(s, stream);
+    if (e != hipSuccess) return e;
+    const f16* poly = A;
+    if (c.c != 0.0f) {
+      s.P = s.Q = A;
+      s.ldp = s.ldq = s.ldr = w.ldm;
+      s.K = m;
+      s.alpha = c.c;
+      s.beta = c.b;
+      s.residual = A;
+      s.res_half = true;
+      s.half = B;
+      e = launch_small(s, stream);
+      if (e != hipSuccess) return e;
+      poly = B;
+    }
+    SmallArgs u{};
+    u.P = tall ? now : poly;
+    u.ldp = tall ? w.ldx : w.ldm;
+    u.Q = tall ? poly : now_t;
+    u.ldq = tall ? w.ldm : w.ldt;
+    u.I = rows;
+    u.J = cols;
+    u.K = m;
+    u.alpha = inverse * (c.c != 0.0f ? 1.0f : c.b);
+    u.beta = c.a;
+    u.residual = at<float>(ws, w.x);
+    u.ldr = w.ldx;
+    if (t + 1 < c.steps) {
+      u.out = at<float>(ws, w.x);
+      u.out_type = kF32;
+      u.ldo = w.ldx;
+      u.rows = rows;
+      u.cols = cols;
+      u.half = at<f16>(ws, w.half[~t & 1]);
+      u.ldh = w.ldx;
+      u.half_t = at<f16>(ws, w.half_t[~t & 1]);
+      u.ldt = w.ldt;
+      u.half_scale = scale;
+    } else {
+      u.out = c.y;
+      u.out_type = kBF16;
+      u.ldo = c.ldy;
+      u.rows = c.rows;
+      u.cols = c.cols;
+    }
+    e = launch_small(u, stream);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_orthogonalise(const OrthoCall& c, void* ws, hipStream_t stream) {
@@ -179,13 +454,14 @@ hipError_t launch_orthogonalise(const OrthoCall& c, void* ws, hipStream_t stream
                  : c.dtype == kF16 ? start<f16>(c, w, scale, ws, stream)
                                    : start<bf16>(c, w, scale, ws, stream);
   if (e != hipSuccess) return e;
+  if (w.small) return small_steps(c, w, scale, ws, stream);
   const bool tall = c.rows > c.cols;
   float* const partial = at<float>(ws, w.partial);
   f16 *const A = at<f16>(ws, w.gram), *const B = at<f16>(ws, w.poly);
   float* const X = at<float>(ws, w.x);
   for (int t = 0; t < c.steps; ++t) {
     f16 *const now = at<f16>(ws, w.half[t & 1]), *const next = at<f16>(ws, w.half[~t & 1]);
-    Step s = step_of(w.rows, w.ldx, tall);
+    Step s = step_of(w.rows, w.cols, tall);
     s.gram.P = s.gram.Q = now;
     s.gram.ldp = s.gram.ldq = w.ldx;
     s.gram.alpha = inverse * inverse;

@@ -76,11 +76,12 @@ struct ProductPlan {
   int splits;
   int64_t k_split;
   size_t partial_floats;
+  bool symmetric;            // only the tiles on and above the diagonal
 };
 // `dma`: the rows of both operands start on 16 bytes; `few`: the kernels of few rows will do;
-// `first`: the largest shape that will
+// `first`: the largest shape that will; `symmetric`: C is, and half of its tiles will do
 ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma, bool few = true,
-                         int first = kShape256);
+                         int first = kShape256, bool symmetric = false);
 // Rows of both operands start on 16 bytes, at strides that a tile's 32-bit offsets span.
 bool rows_on_16(const ProductArgs& a);
 void set_launch(ProductArgs& a, const ProductPlan& p, float* partial);
@@ -657,6 +658,23 @@ __device__ __forceinline__ TilePlace tile_place(const ProductArgs& a) {
   return t;
 }
 
+// The same of the tiles on and above the diagonal: row r's and row T - 1 - r's together are T + 1.
+__device__ __forceinline__ TilePlace upper_place(const ProductArgs& a) {
+  const uint32_t T = a.tiles_i, tiles = T * (T + 1) / 2;
+  const uint32_t lin = blockIdx.x % kXcds * a.per_xcd + blockIdx.x / kXcds;
+  TilePlace t;
+  t.live = lin < tiles;
+  if (!t.live) return t;
+  t.split = 0;
+  const uint32_t pair = __builtin_amdgcn_readfirstlane(lin / (T + 1)), in = lin - pair * (T + 1);
+  const bool first = in < T - pair;
+  t.ti = first ? pair : T - 1 - pair;
+  t.tj = first ? pair + in : in - 1;             // T - 1 - pair + in - (T - pair)
+  t.k0 = 0;
+  t.k1 = static_cast<int32_t>(a.K);
+  return t;
+}
+
 // The epilogue by rows: up to 64 rows of the wave's columns at a time go through its own
 // part of LDS, so that a lane has eight consecutive columns and the wave's reads and
 // writes of C are whole lines.  Quads of columns are swizzled by row: the 16 lanes that
@@ -714,6 +732,40 @@ struct Tile {
       __builtin_amdgcn_wave_barrier();
     }
   }
+  // The tile's transpose: `take`(row of C's transpose, its first column, eight sums).  Through the same
+  // place, 16 rows' parts turned by their column's quad: the lanes that write meet no bank twice.
+  template <class Take>
+  __device__ __forceinline__ void columns(const f4 (&acc)[TI][TJ], Take take) const {
+    constexpr int kWide = kBatch * 16, kTurn = kWide / 16 - 1;       // rows of C in a batch
+    typedef __attribute__((address_space(3))) float lds_float;
+    lds_float* const place = reinterpret_cast<lds_float*>(mine);
+    const int64_t row0 = i0 + wave / WJ * TI * 16, col0 = j0 + wave % WJ * kCols;
+#pragma unroll 1
+    for (int b = 0; b < TI / kBatch; ++b) {
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int x = 0; x < kBatch; ++x)
+#pragma unroll
+        for (int y = 0; y < TJ; ++y) {
+          f4 v = acc[x][y];
+          if constexpr (TI > kBatch) v = b ? acc[kBatch + x][y] : v;
+          const int quad = y * 4 + (lane >> 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) place[(quad * 4 + e) * kWide + ((x ^ (quad & kTurn)) * 16 + (lane & 15))] = v[e];
+        }
+      __builtin_amdgcn_wave_barrier();
+      constexpr int kPer = kWide / 8, kAt = 64 / kPer;               // lanes of a row, rows of an access
+#pragma unroll 1
+      for (int r = 0; r < kCols; r += kAt) {
+        const int row = r + lane / kPer, at = lane % kPer * 8;
+        const int turned = (((at >> 4) ^ ((row >> 2) & kTurn)) << 4) | (at & 15);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = place[row * kWide + turned + e];
+        take(col0 + row, row0 + b * kWide + at, v);
+      }
+    }
+  }
   // sums of a split k axis
   __device__ __forceinline__ void part(const ProductArgs& a, const f4 (&acc)[TI][TJ], uint32_t split) const {
     const int32_t ld_part = static_cast<int32_t>((a.J + 7) / 8 * 8);
@@ -762,13 +814,20 @@ struct No {
 
 // What becomes of a tile's sums: the epilogue of som_product, or one of product_modes.h,
 // which take more arguments.
-constexpr int kPlain = 0, kExtra = 1, kLoss = 2, kGrad = 3;
+constexpr int kPlain = 0, kExtra = 1, kLoss = 2, kGrad = 3, kMirror = 4;
 template <int MODE>
 struct ModeArgs;
 template <>
 struct ModeArgs<kPlain> {
   typedef ProductArgs type;
 };
+template <int MODE>
+__device__ __forceinline__ TilePlace mode_place(const typename ModeArgs<MODE>::type& a) {
+  if constexpr (MODE == kMirror)
+    return upper_place(a);
+  else
+    return tile_place(a);
+}
 template <int MODE, class TileOf, int TI, int TJ>
 __device__ __forceinline__ void finish_mode(const TileOf& tile, const typename ModeArgs<MODE>::type& a,
                                             const f4 (&acc)[TI][TJ], const TilePlace& place);
@@ -784,7 +843,7 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product(const typename ModeArgs
   constexpr int kStep = kStepBytes / ES;
   extern __shared__ __align__(1024) char lds[];
 
-  const TilePlace place = tile_place(a);
+  const TilePlace place = mode_place<MODE>(a);
   if (!place.live) return;
   const int64_t i0 = static_cast<int64_t>(place.ti) * BI, j0 = static_cast<int64_t>(place.tj) * BJ;
   const int32_t k0 = place.k0, k1 = place.k1;

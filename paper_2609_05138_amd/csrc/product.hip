@@ -108,11 +108,11 @@ double product_time(int shape, int64_t n, int64_t steps, bool e4m3, bool dma) {
 // against 17.6; two rows are no faster; 4,096 x 4,096: 11.4 against 8.9, since a
 // narrow strip's lines are read by several CUs).
 ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma,
-                         bool few, int first) {
-  if (few && p_kc && J <= kFewMaxColumns && (q_kc ? I <= 4 : I == 1 && J >= 8192)) return {kFew, 1, K, 0};
+                         bool few, int first, bool symmetric) {
+  if (few && p_kc && J <= kFewMaxColumns && (q_kc ? I <= 4 : I == 1 && J >= 8192)) return {kFew, 1, K, 0, false};
   const int64_t step = elem == kE4M3 ? 128 : 64;
   const int64_t steps = (K + step - 1) / step;
-  ProductPlan best{first, 1, steps * step, 0};
+  ProductPlan best{first, 1, steps * step, 0, false};
   double least = 1e300;
   const int last = p_kc ? kShape16 : kShape64;
   for (int shape = first; shape <= last; ++shape) {
@@ -130,10 +130,19 @@ ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, b
       if (splits > 1) t += kJoinTime + 8.0 * static_cast<double>(splits) * I * J / kJoinBytes;
       if (t < least) {
         least = t;
-        best = {shape, static_cast<int>(splits), per * step, 0};
+        best = {shape, static_cast<int>(splits), per * step, 0, false};
       }
     }
   }
+  if (symmetric)
+    for (const int shape : {kShape256, kShape128}) {
+      const int64_t side = (I + kInfo[shape].bi - 1) / kInfo[shape].bi;
+      const double t = product_time(shape, side * (side + 1) / 2, steps, elem == kE4M3, dma);
+      if (t < least) {
+        least = t;
+        best = {shape, 1, steps * step, 0, true};
+      }
+    }
   if (best.splits > 1) best.partial_floats = static_cast<size_t>(best.splits) * I * ((J + 7) / 8 * 8);
   return best;
 }
@@ -153,7 +162,8 @@ void set_launch(ProductArgs& a, const ProductPlan& p, float* partial) {
   a.partial = partial;
   a.tiles_i = static_cast<uint32_t>((a.I + s.bi - 1) / s.bi);
   a.tiles_j = static_cast<uint32_t>((a.J + s.bj - 1) / s.bj);
-  const int64_t wgs = static_cast<int64_t>(a.tiles_i) * a.tiles_j * a.splits;
+  const int64_t wgs = p.symmetric ? static_cast<int64_t>(a.tiles_i) * (a.tiles_i + 1) / 2
+                                  : static_cast<int64_t>(a.tiles_i) * a.tiles_j * a.splits;
   a.per_xcd = static_cast<uint32_t>((wgs + kXcds - 1) / kXcds);
 }
 

@@ -1,5 +1,5 @@
 // The matrix product's kernel with epilogues of its own: sums and factors that stay on the
-// device (kExtra), and the two passes of cross entropy (kLoss, kGrad).
+// device (kExtra), of symmetric products (kMirror), and the two passes of cross entropy (kLoss, kGrad).
 #pragma once
 
 #include "product.h"
@@ -16,6 +16,9 @@ struct ExtraArgs : ProductArgs {
   void* half;                // [I][ldh] or nullptr
   int64_t ldh;
   float half_scale;
+  // C is symmetric (I = J; `residual` too; no row, column, half and swap): kMirror, which calculates the
+  // tiles on and above the diagonal and writes their transposes too, will do where it is faster
+  bool symmetric;
   // where *swap is not 0, P (or Q) is read from `swapped` instead
   const int32_t* swap;       // or nullptr
   const void* swapped;
@@ -49,6 +52,10 @@ struct ModeArgs<kExtra> {
   typedef ExtraArgs type;
 };
 template <>
+struct ModeArgs<kMirror> {
+  typedef ExtraArgs type;
+};
+template <>
 struct ModeArgs<kLoss> {
   typedef LossArgs type;
 };
@@ -59,14 +66,16 @@ struct ModeArgs<kGrad> {
 
 // The plan of a kExtra product (no kernels of few rows), and the product with the join of a split
 // k axis.
-inline ProductPlan plan_extra(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma) {
-  return plan_product(I, J, K, elem, p_kc, q_kc, dma, false);
+inline ProductPlan plan_extra(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma,
+                              bool symmetric = false) {
+  return plan_product(I, J, K, elem, p_kc, q_kc, dma, false, kShape256, symmetric);
 }
 hipError_t launch_extra(ExtraArgs a, float* partial, hipStream_t stream);
 // The kernel alone; `a`, the mode's arguments, has its launch's fields.
 hipError_t launch_mode(int mode, int shape, const ProductArgs& a, hipStream_t stream);
 hipError_t launch_modes_f16(int mode, int shape, const ProductArgs& a, hipStream_t stream);
 hipError_t launch_modes_bf16(int mode, int shape, const ProductArgs& a, hipStream_t stream);
+hipError_t launch_mirror_f16(int shape, const ExtraArgs& a, hipStream_t stream);
 
 // ---------------------------------------------------------------------------
 // kExtra
@@ -156,6 +165,20 @@ __device__ __forceinline__ void extra_tile(const TileOf& tile, const ExtraArgs& 
     if (i >= a.I || tile.n <= 0) return;
     add_outer(a, i, column, v);
     finish8_extra(a, i, tile.j, tile.n, v, now);
+  });
+}
+
+// The same of a symmetric C, by itself so that its registers are not kExtra's.
+template <class TileOf, int TI, int TJ>
+__device__ __forceinline__ void mirror_tile(const TileOf& tile, const ExtraArgs& a, const f4 (&acc)[TI][TJ],
+                                            const TilePlace& place) {
+  tile.rows(acc, [&](int, int64_t i, float (&v)[8]) __attribute__((always_inline)) {
+    if (i < a.I && tile.n > 0) finish8_extra(a, i, tile.j, tile.n, v, extra_terms(a, a.alpha, i, tile.j, tile.n));
+  });
+  if (place.ti == place.tj) return;
+  tile.columns(acc, [&](int64_t i, int64_t j, float (&v)[8]) __attribute__((always_inline)) {
+    const int n = static_cast<int>(min<int64_t>(8, a.J - j));
+    if (i < a.I && n > 0) finish8_extra(a, i, j, n, v, extra_terms(a, a.alpha, i, j, n));
   });
 }
 
@@ -410,6 +433,8 @@ __device__ __forceinline__ void finish_mode(const TileOf& tile, const typename M
                                             const f4 (&acc)[TI][TJ], const TilePlace& place) {
   if constexpr (MODE == kExtra)
     extra_tile(tile, a, acc, place);
+  else if constexpr (MODE == kMirror)
+    mirror_tile(tile, a, acc, place);
   else if constexpr (MODE == kLoss)
     loss_tile(tile, a, acc, place);
   else

@@ -15,6 +15,14 @@ hipError_t launch_layout(int shape, const typename ModeArgs<MODE>::type& a, hipS
   return hipErrorInvalidValue;
 }
 
+// Square tiles, both operands laid out alike.
+template <int E, bool KC, int MODE>
+hipError_t launch_square(int shape, const typename ModeArgs<MODE>::type& a, hipStream_t stream) {
+  if (shape == kShape256) return launch_one<kShape256, E, KC, KC, MODE, 2, 4, 8, 4, 2>(a, stream);
+  if (shape == kShape128) return launch_one<kShape128, E, KC, KC, MODE, 2, 4, 4, 2, 4>(a, stream);
+  return hipErrorInvalidValue;
+}
+
 // `a` is the mode's arguments.
 template <int E>
 hipError_t launch_mode_elem(int mode, int shape, const ProductArgs& a, hipStream_t stream) {
