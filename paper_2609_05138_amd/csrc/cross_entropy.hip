@@ -7,7 +7,8 @@
 // Forward: a tile of the product leaves for each of its rows the largest score m and s = sum
 // exp(v - m) (8 bytes for 256 or 128 scores), and the label's score; k_loss_join puts a row's
 // pairs together.  Where the k axis is split, or the kernels of few rows are faster, the scores go
-// through the workspace, as fp32, to k_loss_scores, which makes the pairs of 2,048 columns.
+// through the workspace, as fp32, to k_loss_scores, which makes the pairs of 8,192 columns, or of up to
+// 32,768 the loss itself.
 //
 // Backward: the product again, a piece of the classes at a time: its epilogue makes g of the
 // piece, in x's type because the matrix cores take 16 bits (as som_product_backward's dP), and
@@ -27,54 +28,79 @@
 namespace som {
 namespace {
 
-constexpr int kScoreColumns = 2048;            // of a workgroup of k_loss_scores
+constexpr int kScoreThreads = 1024, kScoreColumns = kScoreThreads * 8;   // of a pass of k_loss_scores
+constexpr int64_t kOneWorkgroup = 4 * kScoreColumns;     // a row of so many goes without k_loss_join
 constexpr int64_t kRowsAtOnce = 65536;         // forward: rows of one launch, for the pairs' room
 constexpr int64_t kPieceBytes = int64_t(1) << 28;
 constexpr int64_t kLeastPiece = 2048;
 
 typedef float f2 __attribute__((ext_vector_type(2)));
 
-// One row and 2,048 columns a workgroup, from fp32 sums.
-__global__ void __launch_bounds__(256) k_loss_scores(const LossArgs a, uint32_t chunks) {
-  __shared__ f2 sums[4];
+// A row's loss and lse from its largest score and the sum of exponentials below it.
+struct LossOut {
+  const int32_t* labels;
+  const float* label_score;
+  float *loss, *lse;
+  int64_t classes;
+};
+__device__ __forceinline__ void finish_loss(const LossOut& o, int64_t i, float m, float s, float own) {
+  const float all = m + logf(s);       // no score but -infinity: -infinity
+  o.lse[i] = all;
+  const int32_t label = o.labels[i];
+  // (a label that cannot be had costs infinitely much, also where nothing can)
+  o.loss[i] = label < 0 || label >= o.classes ? 0.0f : all == -INFINITY ? INFINITY : all - own;
+}
+
+// One row and `passes` x 8,192 columns a workgroup, from fp32 sums; with one such chunk to a row
+// its loss too.
+__global__ void __launch_bounds__(kScoreThreads) k_loss_scores(const LossArgs a, const LossOut o, uint32_t chunks,
+                                                               int passes) {
+  __shared__ f2 sums[kScoreThreads / 64];
+  __shared__ float own;
   const int64_t g = group_index(), i = g / chunks, chunk = g - i * chunks;
   if (i >= a.I) return;
-  const int64_t j = chunk * kScoreColumns + threadIdx.x * 8;
-  const int n = a.J - j >= 8 ? 8 : a.J > j ? static_cast<int>(a.J - j) : 0;
-  float v[8], bias[8] = {}, m = -INFINITY, s = 0.0f;
-  if (n > 0) {
+  const int64_t first = chunk * passes * kScoreColumns + threadIdx.x * 8;
+  const int64_t label = a.labels[i];
+  float m = -INFINITY, s = 0.0f;
+  for (int p = 0; p < passes; ++p) {
+    const int64_t j = first + p * kScoreColumns;
+    const int n = a.J - j >= 8 ? 8 : a.J > j ? static_cast<int>(a.J - j) : 0;
+    if (n <= 0) break;
+    float v[8], bias[8] = {}, top = -INFINITY, sum = 0.0f;
     join8(a, i, j, v);
     if (a.bias) load8(a.bias + j, n, bias);
-    const int64_t label = a.labels[i] - j;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       v[e] = e >= n || bias[e] == -INFINITY ? -INFINITY : fmaf(v[e], a.alpha, bias[e]);
-      m = fmaxf(m, v[e]);
-      if (e < n && label == e) a.label_score[i] = v[e];
+      top = fmaxf(top, v[e]);
+      if (e < n && label - j == e) {
+        if (chunks > 1)
+          a.label_score[i] = v[e];
+        else
+          own = v[e];
+      }
     }
+    const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += __builtin_amdgcn_exp2f(kLog2e * (v[e] - base));
+    join_max_sum(m, s, top, sum);
   }
 #pragma unroll
-  for (int off = 32; off; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-  const float base = m == -INFINITY ? 0.0f : m;
-  if (n > 0) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s += __builtin_amdgcn_exp2f(kLog2e * (v[e] - base));
-  }
-#pragma unroll
-  for (int off = 32; off; off >>= 1) s += __shfl_xor(s, off, 64);
+  for (int off = 32; off; off >>= 1) join_max_sum(m, s, __shfl_xor(m, off, 64), __shfl_xor(s, off, 64));
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = f2{m, s};
   __syncthreads();
   if (threadIdx.x) return;
 #pragma unroll
-  for (int w = 1; w < 4; ++w) join_max_sum(m, s, sums[w][0], sums[w][1]);
-  reinterpret_cast<f2*>(a.part)[chunk * a.I + i] = f2{m, s};
+  for (int w = 1; w < kScoreThreads / 64; ++w) join_max_sum(m, s, sums[w][0], sums[w][1]);
+  if (chunks > 1)
+    reinterpret_cast<f2*>(a.part)[chunk * a.I + i] = f2{m, s};
+  else
+    finish_loss(o, i, m, s, own);
 }
 
 // 16 rows a workgroup, 16 threads a row, each every 16th pair.
 __global__ void __launch_bounds__(256) k_loss_join(const f2* __restrict__ part, int64_t parts, int64_t rows,
-                                                   const int32_t* __restrict__ labels, int64_t classes,
-                                                   const float* __restrict__ label_score, float* __restrict__ loss,
-                                                   float* __restrict__ lse) {
+                                                   const LossOut o) {
   __shared__ f2 sums[16][17];
   const int r = threadIdx.x & 15, slice = threadIdx.x >> 4;
   const int64_t i = group_index() * 16 + r;
@@ -94,11 +120,7 @@ __global__ void __launch_bounds__(256) k_loss_join(const f2* __restrict__ part, 
   if (slice || i >= rows) return;
 #pragma unroll
   for (int w = 1; w < 16; ++w) join_max_sum(m, s, sums[w][r][0], sums[w][r][1]);
-  const float all = m + logf(s);       // no score but -infinity: -infinity
-  lse[i] = all;
-  const int32_t label = labels[i];
-  // (a label that cannot be had costs infinitely much, also where nothing can)
-  loss[i] = label < 0 || label >= classes ? 0.0f : all == -INFINITY ? INFINITY : all - label_score[i];
+  finish_loss(o, i, m, s, o.label_score[i]);
 }
 
 // ---------------------------------------------------------------------------
@@ -437,7 +459,7 @@ hipError_t launch_loss(const LossCall& c, void* ws, hipStream_t stream) {
     a.dma = rows_on_16(a);
     const ProductPlan p = plan_product(a.I, a.J, a.K, a.elem, true, a.q_kc, a.dma);
     float* const scores = at<float>(ws, w.scores);
-    int64_t parts;
+    const LossOut o = {a.labels, a.label_score, c.loss + m0, c.lse + m0, c.N};
     hipError_t e;
     if (p.shape == kFew) {             // plain sums, which k_loss_scores takes like one split
       ProductArgs f = a;
@@ -450,21 +472,24 @@ hipError_t launch_loss(const LossCall& c, void* ws, hipStream_t stream) {
       e = launch_product_few(f, stream);
       a.partial = scores;
       a.splits = 1;
-      parts = (c.N + kScoreColumns - 1) / kScoreColumns;
     } else {
       set_launch(a, p, scores);
       e = launch_mode(kLoss, p.shape, a, stream);
-      parts = p.splits > 1 ? (c.N + kScoreColumns - 1) / kScoreColumns : a.tiles_j;
     }
     if (e != hipSuccess) return e;
+    int64_t parts = a.tiles_j;
     if (p.shape == kFew || p.splits > 1) {
-      hipLaunchKernelGGL(k_loss_scores, groups_grid(parts * rows), dim3(256), 0, stream, a, static_cast<uint32_t>(parts));
+      const bool one = c.N <= kOneWorkgroup;
+      const int passes = one ? static_cast<int>((c.N + kScoreColumns - 1) / kScoreColumns) : 1;
+      parts = one ? 1 : (c.N + kScoreColumns - 1) / kScoreColumns;
+      hipLaunchKernelGGL(k_loss_scores, groups_grid(parts * rows), dim3(kScoreThreads), 0, stream, a, o,
+                         static_cast<uint32_t>(parts), passes);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
+      if (one) continue;
     }
     hipLaunchKernelGGL(k_loss_join, groups_grid((rows + 15) / 16), dim3(256), 0, stream,
-                       reinterpret_cast<const f2*>(a.part), parts, rows, a.labels, c.N, a.label_score, c.loss + m0,
-                       c.lse + m0);
+                       reinterpret_cast<const f2*>(a.part), parts, rows, o);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -76,15 +76,22 @@ struct ProductPlan {
   int splits;
   int64_t k_split;
   size_t partial_floats;
-  bool symmetric;            // only the tiles on and above the diagonal
 };
-// `dma`: the rows of both operands start on 16 bytes; `few`: the kernels of few rows will do;
-// `first`: the largest shape that will; `symmetric`: C is, and half of its tiles will do
-ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma, bool few = true,
-                         int first = kShape256, bool symmetric = false);
+// `dma`: the rows of both operands start on 16 bytes
+ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma);
+// The same where not every kernel will do.
+struct PlanRules {
+  bool few = true;           // the kernels of few rows
+  int first = kShape256;     // the largest shape
+  bool symmetric = false;    // C is, and the tiles on and above its diagonal will do
+};
+struct RuledPlan : ProductPlan {
+  bool upper;                // only those tiles
+};
+RuledPlan plan_product_by(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma, const PlanRules& rules);
 // Rows of both operands start on 16 bytes, at strides that a tile's 32-bit offsets span.
 bool rows_on_16(const ProductArgs& a);
-void set_launch(ProductArgs& a, const ProductPlan& p, float* partial);
+void set_launch(ProductArgs& a, const ProductPlan& p, float* partial, bool upper = false);
 // Fills the launch's fields of `a` and enqueues it (and the join of a split k axis);
 // `partial`: plan_product's floats.
 hipError_t launch_product(ProductArgs a, float* partial, hipStream_t stream);

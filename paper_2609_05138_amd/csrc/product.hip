@@ -107,15 +107,18 @@ double product_time(int shape, int64_t n, int64_t steps, bool e4m3, bool dma) {
 // launches).  With k strided one row does from 8,192 columns on (2,048 x 16,384: 13.4
 // against 17.6; two rows are no faster; 4,096 x 4,096: 11.4 against 8.9, since a
 // narrow strip's lines are read by several CUs).
-ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma,
-                         bool few, int first, bool symmetric) {
-  if (few && p_kc && J <= kFewMaxColumns && (q_kc ? I <= 4 : I == 1 && J >= 8192)) return {kFew, 1, K, 0, false};
+ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma) {
+  return plan_product_by(I, J, K, elem, p_kc, q_kc, dma, {});
+}
+
+RuledPlan plan_product_by(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma, const PlanRules& rules) {
+  if (rules.few && p_kc && J <= kFewMaxColumns && (q_kc ? I <= 4 : I == 1 && J >= 8192)) return {{kFew, 1, K, 0}, false};
   const int64_t step = elem == kE4M3 ? 128 : 64;
   const int64_t steps = (K + step - 1) / step;
-  ProductPlan best{first, 1, steps * step, 0, false};
+  RuledPlan best{{rules.first, 1, steps * step, 0}, false};
   double least = 1e300;
   const int last = p_kc ? kShape16 : kShape64;
-  for (int shape = first; shape <= last; ++shape) {
+  for (int shape = rules.first; shape <= last; ++shape) {
     const ShapeInfo& s = kInfo[shape];
     // not worth the host's time: tiles of four times the rows, or very many of them unless
     // they are one row (40 x 512 x 1,048,576: 64 x 128 254 us, 128 x 128 338; 16 x 1,024 x
@@ -130,17 +133,17 @@ ProductPlan plan_product(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, b
       if (splits > 1) t += kJoinTime + 8.0 * static_cast<double>(splits) * I * J / kJoinBytes;
       if (t < least) {
         least = t;
-        best = {shape, static_cast<int>(splits), per * step, 0, false};
+        best = {{shape, static_cast<int>(splits), per * step, 0}, false};
       }
     }
   }
-  if (symmetric)
+  if (rules.symmetric)
     for (const int shape : {kShape256, kShape128}) {
       const int64_t side = (I + kInfo[shape].bi - 1) / kInfo[shape].bi;
       const double t = product_time(shape, side * (side + 1) / 2, steps, elem == kE4M3, dma);
       if (t < least) {
         least = t;
-        best = {shape, 1, steps * step, 0, true};
+        best = {{shape, 1, steps * step, 0}, true};
       }
     }
   if (best.splits > 1) best.partial_floats = static_cast<size_t>(best.splits) * I * ((J + 7) / 8 * 8);
@@ -155,15 +158,15 @@ bool rows_on_16(const ProductArgs& a) {
   return whole(a.P, a.ldp) && whole(a.Q, a.ldq);
 }
 
-void set_launch(ProductArgs& a, const ProductPlan& p, float* partial) {
+void set_launch(ProductArgs& a, const ProductPlan& p, float* partial, bool upper) {
   const ShapeInfo& s = kInfo[p.shape];
   a.splits = p.splits;
   a.k_split = p.k_split;
   a.partial = partial;
   a.tiles_i = static_cast<uint32_t>((a.I + s.bi - 1) / s.bi);
   a.tiles_j = static_cast<uint32_t>((a.J + s.bj - 1) / s.bj);
-  const int64_t wgs = p.symmetric ? static_cast<int64_t>(a.tiles_i) * (a.tiles_i + 1) / 2
-                                  : static_cast<int64_t>(a.tiles_i) * a.tiles_j * a.splits;
+  const int64_t wgs = upper ? static_cast<int64_t>(a.tiles_i) * (a.tiles_i + 1) / 2
+                            : static_cast<int64_t>(a.tiles_i) * a.tiles_j * a.splits;
   a.per_xcd = static_cast<uint32_t>((wgs + kXcds - 1) / kXcds);
 }
 

@@ -130,7 +130,7 @@ hipError_t launch_shape(int shape, const BlockArgs& a, hipStream_t stream) {
 }  // namespace
 
 ProductPlan plan_blocks(int64_t I, int64_t J, int64_t K, bool dma, bool exact) {
-  if (exact) return plan_product(I, J, K, kE4M3, true, true, dma, true, kShape256x128);
+  if (exact) return plan_product_by(I, J, K, kE4M3, true, true, dma, {true, kShape256x128, false});
   // a step of the 8-bit instructions takes what one of 16 bits and half the k does
   ProductPlan p = plan_product(I, J, (K + 1) / 2, kBF16, true, true, dma);
   p.k_split *= 2;

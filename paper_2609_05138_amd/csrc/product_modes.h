@@ -66,9 +66,9 @@ struct ModeArgs<kGrad> {
 
 // The plan of a kExtra product (no kernels of few rows), and the product with the join of a split
 // k axis.
-inline ProductPlan plan_extra(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma,
-                              bool symmetric = false) {
-  return plan_product(I, J, K, elem, p_kc, q_kc, dma, false, kShape256, symmetric);
+inline RuledPlan plan_extra(int64_t I, int64_t J, int64_t K, int elem, bool p_kc, bool q_kc, bool dma,
+                            bool symmetric = false) {
+  return plan_product_by(I, J, K, elem, p_kc, q_kc, dma, {false, kShape256, symmetric});
 }
 hipError_t launch_extra(ExtraArgs a, float* partial, hipStream_t stream);
 // The kernel alone; `a`, the mode's arguments, has its launch's fields.

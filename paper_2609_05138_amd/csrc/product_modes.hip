@@ -29,9 +29,9 @@ hipError_t launch_mode(int mode, int shape, const ProductArgs& a, hipStream_t st
 
 hipError_t launch_extra(ExtraArgs a, float* partial, hipStream_t stream) {
   a.dma = rows_on_16(a);
-  const ProductPlan p = plan_extra(a.I, a.J, a.K, a.elem, a.p_kc, a.q_kc, a.dma, a.symmetric);
-  set_launch(a, p, partial);
-  if (p.symmetric) return launch_mirror_f16(p.shape, a, stream);
+  const RuledPlan p = plan_extra(a.I, a.J, a.K, a.elem, a.p_kc, a.q_kc, a.dma, a.symmetric);
+  set_launch(a, p, partial, p.upper);
+  if (p.upper) return launch_mirror_f16(p.shape, a, stream);
   const hipError_t e = launch_mode(kExtra, p.shape, a, stream);
   if (e != hipSuccess || p.splits == 1) return e;
   const int64_t groups = (a.J + 7) / 8 * a.I;

@@ -1039,11 +1039,18 @@ def som_quantise(x: torch.Tensor, block_rows: int = 1, transpose: bool = False, 
     qp, ldq = _rows(q, "q", torch.float8_e4m3fn, (qr, qc), device)
     shape = (qr if block_rows == 1 else _blocks(qr), _blocks(qc))
     if scale is None:
-        scale = _new((shape[1], shape[0]), torch.float32, x.device, stream).t()
+        scale = _new_factors(shape, x.device, stream)
     sp, sr, sb = _factors(scale, "scale", shape, device)
     _check(lib.som_quantise(xp, ldx, dt, rows, cols, block_rows, 1 if transpose else 0, qp, ldq, sp, sr, sb,
                             _raw_stream(device, stream)))
     return q, scale
+
+
+def _new_factors(shape, device, stream):
+    """Factors of which those of one block of columns are next to each other."""
+    if stream is None:
+        return torch.empty_strided(shape, (1, shape[0]), dtype=torch.float32, device=device)
+    return _new((shape[1], shape[0]), torch.float32, device, stream).t()
 
 
 def _factors(t: torch.Tensor, name: str, shape, device: int):
@@ -1149,11 +1156,33 @@ def _block_scale(t: torch.Tensor, name: str, rows: int, k: int, device: int) -> 
     """The factors of a rows x k operand: one for each row and block of k, or for 128 rows."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    if t.dim() != 2 or t.shape[0] not in (rows, _blocks(rows)):
-        raise ValueError(f"{name} must be {rows} or {_blocks(rows)} x {_blocks(k)} (got "
-                         f"{' x '.join(str(n) for n in t.shape)})")
-    p, row, block = _factors(t, name, (t.shape[0], _blocks(k)), device)
-    return som_block_scale(p, row, block, 1 if t.shape[0] == rows else 128, 0)
+    size = t.shape
+    if len(size) != 2 or size[0] != rows and size[0] != _blocks(rows):
+        raise ValueError(f"{name} must be {rows} or {_blocks(rows)} x {_blocks(k)} (got {' x '.join(str(n) for n in size)})")
+    return som_block_scale(*_factors(t, name, (size[0], _blocks(k)), device), 1 if size[0] == rows else 128, 0)
+
+
+def _unit_codes(W: torch.Tensor, name: str, k: int, device: int):
+    """A K x N matrix of codes as the transposed view of an N x K one: (pointer, row stride, N)."""
+    if not isinstance(W, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if W.dtype != torch.float8_e4m3fn:
+        raise TypeError(f"{name} must be {torch.float8_e4m3fn} (got {W.dtype})")
+    if W.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device} like the first tensor (got {W.device})")
+    size = W.shape
+    if len(size) != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    if size[0] != k:
+        raise ValueError(f"x has {k} columns and {name} {size[0]} rows")
+    one, ld = W.stride()
+    if one != 1 and k > 1:
+        raise ValueError(f"{name} must be the transposed view of an N x K matrix (unit-major)")
+    if ld < k:
+        if size[1] > 1:
+            raise ValueError(f"{name}: rows must not overlap")
+        ld = k
+    return W.data_ptr(), ld, size[1]
 
 
 def som_product_blocks(x: torch.Tensor, x_scale: torch.Tensor, W: torch.Tensor, w_scale: torch.Tensor,
@@ -1174,14 +1203,7 @@ def som_product_blocks(x: torch.Tensor, x_scale: torch.Tensor, W: torch.Tensor, 
         with torch.cuda.device(device):
             return som_product_blocks(x, x_scale, W, w_scale, bias, act, residual, alpha, y, dtype, pre, ws, stream)
     M, K = x.shape
-    Wp, ldw, units = _weights(W, "W", x.dtype, device)
-    if not units and K > 1:
-        raise ValueError("W must be the transposed view of an N x K matrix (unit-major)")
-    if W.shape[0] != K:
-        raise ValueError(f"x has {K} columns and W {W.shape[0]} rows")
-    N = W.shape[1]
-    if not units:                                  # one element of each unit
-        ldw = max(W.stride(1), 1)
+    Wp, ldw, N = _unit_codes(W, "W", K, device)
     if act not in ACTIVATIONS:
         raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}")
     xs, wsc = _block_scale(x_scale, "x_scale", M, K, device), _block_scale(w_scale, "w_scale", N, K, device)
