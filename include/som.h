@@ -606,7 +606,7 @@ som_status som_cross_entropy(const void* x, int64_t ldx, const void* W, int64_t 
  *     dx = alpha g W^T,  dW = alpha x^T g,  dbias_n = sum_m g[m][n].
  *
  * dx and dW (laid out as W is) are of x's type, dbias is fp32; each may be NULL.  The scores
- * are calculated again, for a piece of the classes at a time (about 256 MB of g); g is rounded to
+ * are calculated again, for a piece of the classes at a time (128 MB of g, or 8,192 classes); g is rounded to
  * x's type for the two products, scaled by a power of two so that fp16 holds a mean's small
  * values, and dbias sums it unrounded.  A document without a label, with dloss 0 or with no class left
  * gives zeros to everything, whatever its x holds, NaN too.  lse has no gradient of its own.

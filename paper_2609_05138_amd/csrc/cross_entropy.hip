@@ -31,8 +31,11 @@ namespace {
 constexpr int kScoreThreads = 1024, kScoreColumns = kScoreThreads * 8;   // of a pass of k_loss_scores
 constexpr int64_t kOneWorkgroup = 4 * kScoreColumns;     // a row of so many goes without k_loss_join
 constexpr int64_t kRowsAtOnce = 65536;         // forward: rows of one launch, for the pairs' room
-constexpr int64_t kPieceBytes = int64_t(1) << 28;
-constexpr int64_t kLeastPiece = 2048;
+// Backward: a piece's g has 2^27 bytes, half of what the memory-side cache holds, but no fewer than 8,192
+// classes, since dx's sums are read and written for each (8,192 x 2,048 x 65,536: pieces of 2^27
+// bytes 5,261 us, 2^28 5,400, 2^30 5,347; 16,384 x 1,024 x 65,536: 6,705, 6,134 and 6,051).
+constexpr int64_t kPieceBytes = int64_t(1) << 27;
+constexpr int64_t kLeastPiece = 8192;
 
 typedef float f2 __attribute__((ext_vector_type(2)));
 

@@ -18,7 +18,9 @@
 //
 // Small matrices take products of their own: tiles of 32 x 32, whose eight waves share the k axis and read their fragments from the L2 without LDS, so that a
 // product is little more than a launch and two memory latencies.  They read rows of k only, so
-// X's fp16 copy is kept transposed too.
+// X's fp16 copy is kept transposed too.  Of sides up to kLowSide, which average less of it out, what
+// rounding leaves of B is kept and multiplied as well (153 x 221, 6 steps: 2.1e-3 from 64 bits before
+// y's rounding, with it 1.5e-3).
 //
 // Bound: the matrix cores for sides of 2,048 and more; else 3 launches a step.
 #include "orthogonalise.h"
@@ -35,6 +37,7 @@ constexpr int kParts = 512;            // sums of squares, one a workgroup
 // and 57, 512 x 512 82 and 92, 1,024 x 512 104 and 116; 1,024 x 1,024 272 and 151, 256 x 4,096 147
 // and 118, since their fragments come from the L2 64 bytes a row).
 constexpr int64_t kSmall = 1 << 19, kSmallSide = 1024;
+constexpr int64_t kLowSide = 256;      // what rounding leaves of B is kept up to this (512 x 512: 82 us, with it 94)
 
 // Sum over the workgroup's 256 threads, in a fixed order.
 __device__ __forceinline__ double sum256(double v, double* part) {
@@ -101,6 +104,7 @@ struct SmallArgs {
   const f16 *P, *Q;
   int64_t ldp, ldq;
   int32_t I, J, K;
+  int32_t wrap_p, wrap_q;    // steps of 64 after which the operand starts again
   float alpha, beta;
   const void* residual;      // fp32 (or fp16 with res_half), or nullptr
   bool res_half;
@@ -109,6 +113,7 @@ struct SmallArgs {
   int out_type;
   int64_t ldo, rows, cols;
   f16 *half, *half_t;        // [I][ldh] and its transpose [J][ldt], times half_scale; or nullptr
+  int32_t low;               // columns further on: what half's rounding leaves (0: nowhere)
   int64_t ldh, ldt;
   float half_scale;
 };
@@ -132,12 +137,13 @@ __global__ void __launch_bounds__(kSmallWaves * 64) k_ortho_small(const SmallArg
     h8 p[TT][2], q[TT][2];
   };
   auto load = [&](Step& s, int step) __attribute__((always_inline)) {
+    const int at_p = (step < a.wrap_p ? step : step - a.wrap_p) * 64, at_q = (step < a.wrap_q ? step : step - a.wrap_q) * 64;
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) s.p[t][h] = *reinterpret_cast<const h8*>(p + t * 16 * a.ldp + step * 64 + h * 32);
+      for (int h = 0; h < 2; ++h) s.p[t][h] = *reinterpret_cast<const h8*>(p + t * 16 * a.ldp + at_p + h * 32);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) s.q[t][h] = *reinterpret_cast<const h8*>(q + t * 16 * a.ldq + step * 64 + h * 32);
+      for (int h = 0; h < 2; ++h) s.q[t][h] = *reinterpret_cast<const h8*>(q + t * 16 * a.ldq + at_q + h * 32);
     }
   };
   auto multiply = [&](const Step& s) __attribute__((always_inline)) {
@@ -199,6 +205,12 @@ __global__ void __launch_bounds__(kSmallWaves * 64) k_ortho_small(const SmallArg
 #pragma unroll
       for (int e = 0; e < 4; ++e) h[e] = static_cast<f16>(v[e] * a.half_scale);
       *reinterpret_cast<h4*>(a.half + i * a.ldh + j) = h;
+      if (a.low) {
+        h4 low;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) low[e] = static_cast<f16>(v[e] * a.half_scale - static_cast<float>(h[e]));
+        *reinterpret_cast<h4*>(a.half + i * a.ldh + j + a.low) = low;
+      }
     }
   }
   if (!a.half_t) return;
@@ -321,7 +333,6 @@ OrthoWs ortho_ws(int64_t rows, int64_t cols) {
   w.short_side = tall ? w.cols : w.rows;
   w.ldx = w.cols;
   w.ldt = w.rows;
-  w.ldm = w.short_side;
   size_t o = sizeof(double) * kParts;
   w.x = o;
   o += align_up(sizeof(float) * w.rows * w.ldx, 256);
@@ -329,7 +340,10 @@ OrthoWs ortho_ws(int64_t rows, int64_t cols) {
     h = o;
     o += align_up(2 * w.rows * w.ldx, 256);
   }
+  // (a rule for both sides, so that a matrix and its transpose are made alike)
   w.small = w.rows * w.cols <= kSmall && w.rows <= kSmallSide && w.cols <= kSmallSide;
+  w.low = w.small && w.short_side <= kLowSide;
+  w.ldm = w.low ? 2 * w.short_side : w.short_side;
   if (w.small)
     for (size_t& h : w.half_t) {
       h = o;
@@ -388,8 +402,10 @@ static hipError_t small_steps(const OrthoCall& c, const OrthoWs& w, float scale,
     s.ldp = s.ldq = tall ? w.ldt : w.ldx;
     s.I = s.J = m;
     s.K = tall ? rows : cols;
+    s.wrap_p = s.wrap_q = s.K / 64;
     s.alpha = inverse * inverse;
     s.half = A;
+    s.low = w.low ? m : 0;
     s.ldh = w.ldm;
     s.half_scale = 1.0f;
     hipError_t e = launch_small(s, stream);
@@ -399,6 +415,7 @@ static hipError_t small_steps(const OrthoCall& c, const OrthoWs& w, float scale,
       s.P = s.Q = A;
       s.ldp = s.ldq = s.ldr = w.ldm;
       s.K = m;
+      s.wrap_p = s.wrap_q = m / 64;
       s.alpha = c.c;
       s.beta = c.b;
       s.residual = A;
@@ -415,7 +432,9 @@ static hipError_t small_steps(const OrthoCall& c, const OrthoWs& w, float scale,
     u.ldq = tall ? w.ldm : w.ldt;
     u.I = rows;
     u.J = cols;
-    u.K = m;
+    u.K = w.low ? 2 * m : m;           // the rounded polynomial, then what its rounding left
+    u.wrap_p = tall ? m / 64 : u.K / 64;
+    u.wrap_q = tall ? u.K / 64 : m / 64;
     u.alpha = inverse * (c.c != 0.0f ? 1.0f : c.b);
     u.beta = c.a;
     u.residual = at<float>(ws, w.x);

@@ -282,7 +282,7 @@ __device__ __forceinline__ void grad8(const GradArgs& a, const GradRow& r, float
   const float d = r.dloss * factor;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float p = __builtin_amdgcn_exp2f(fmaf(v[e], a.alpha * kLog2e, kLog2e * bias[e] - kLog2e * r.lse));
+    const float p = __builtin_amdgcn_exp2f(kLog2e * fmaf(v[e], a.alpha, bias[e] - r.lse));
     v[e] = r.dloss == 0.0f ? 0.0f : r.label == e ? fmaf(d, p, -d) : d * p;
   }
 }
@@ -312,8 +312,8 @@ __device__ __forceinline__ u2 round4(int elem, const float (&v)[4], float* sum) 
 }
 
 // Straight from the matrix instructions' registers, as loss_tile: a lane has four consecutive classes
-// of a row in each of TJ places.  exp(v - lse) is a power of two of alpha log2(e) sum + (bias - lse) log2(e);
-// the label's class is looked for once a row and wave.
+// of a row in each of TJ places.  v - lse is alpha sum + (bias - lse), rounded at its own size, since
+// it is an exponent; the label's class is looked for once a row and wave.
 template <class TileOf, int TI, int TJ>
 __device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a, const f4 (&acc)[TI][TJ],
                                           const TilePlace& place) {
@@ -321,14 +321,14 @@ __device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a,
   constexpr int WI = TileOf::kWI, WJ = TileOf::kWJ, BJ = WJ * TJ * 16;
   const int wi = tile.wave / WJ, wj = tile.wave % WJ, g = tile.lane >> 4;
   const int64_t wave_j = tile.j0 + wj * TJ * 16, j = wave_j + g * 4;        // + y * 16 + e
-  const float factor = *a.factor, alpha = a.alpha * kLog2e;
+  const float factor = *a.factor;
   float bias[TJ][4], sums[TJ][4];
   const int left = static_cast<int>(min<int64_t>(a.J - wave_j, TJ * 16));
 #pragma unroll
   for (int y = 0; y < TJ; ++y)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      bias[y][e] = y * 16 + g * 4 + e >= left ? -INFINITY : a.bias ? kLog2e * a.bias[j + y * 16 + e] : 0.0f;
+      bias[y][e] = y * 16 + g * 4 + e >= left ? -INFINITY : a.bias ? a.bias[j + y * 16 + e] : 0.0f;
       sums[y][e] = 0.0f;
     }
   // The rows' terms by way of LDS: one wait for all of them, and no registers.
@@ -340,7 +340,7 @@ __device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a,
   if (threadIdx.x < WI * TI * 16) {
     const int64_t i = tile.i0 + threadIdx.x;
     const GradRow r = grad_row(a, i, tile.j0, i < a.I);
-    terms[threadIdx.x] = f3{__int_as_float(r.label), kLog2e * r.lse, r.dloss * factor};
+    terms[threadIdx.x] = f3{__int_as_float(r.label), r.lse, r.dloss * factor};
   }
   __syncthreads();
   const int rows = static_cast<int>(min<int64_t>(a.I - tile.i0, WI * TI * 16));
@@ -360,7 +360,7 @@ __device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a,
     for (int y = 0; y < TJ; ++y)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        v[y][e] = d * __builtin_amdgcn_exp2f(fmaf(acc[x][y][e], alpha, bias[y][e] - lse));
+        v[y][e] = d * __builtin_amdgcn_exp2f(kLog2e * fmaf(acc[x][y][e], a.alpha, bias[y][e] - lse));
     if (__any(here)) {
 #pragma unroll
       for (int y = 0; y < TJ; ++y)
