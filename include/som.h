@@ -609,7 +609,8 @@ som_status som_cross_entropy(const void* x, int64_t ldx, const void* W, int64_t 
  * are calculated again, for a piece of the classes at a time (128 MB of g, or 8,192 classes); g is rounded to
  * x's type for the two products, scaled by a power of two so that fp16 holds a mean's small
  * values, and dbias sums it unrounded.  A document without a label, with dloss 0 or with no class left
- * gives zeros to everything, whatever its x holds, NaN too.  lse has no gradient of its own.
+ * gives zeros to everything, whatever its x holds, NaN too (the weights of classes that are left
+ * out have to be finite).  lse has no gradient of its own.  No output overlaps an input.
  * With M == 0 dW and dbias are set to zero.  M up to 2^30.  ws:
  * som_cross_entropy_backward_workspace_bytes, 256-byte aligned. */
 size_t som_cross_entropy_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype);

@@ -208,13 +208,12 @@ __device__ void grad_scan(const GradCall& c, int64_t group, int64_t groups, int3
 }
 
 // Everything that goes before the scores, by workgroups: the head, `commons` for the common
-// weights, the rest for the rows.
+// weights, `scans` for the rows (the grid may hold more).
 template <typename T>
 __global__ void __launch_bounds__(1024) k_grad_prepare(const GradCall c, int bits, GradHead* head, int64_t commons,
-                                                       float* common, int32_t* flags) {
+                                                       float* common, int64_t scans, int32_t* flags) {
   __shared__ uint32_t tops[16];
   const int64_t g = group_index();
-  const int64_t scans = int64_t(gridDim.x) * gridDim.y - 1 - commons;
   if (g == 0)
     grad_head(c, bits, head, tops);
   else if (g <= commons)
@@ -265,7 +264,7 @@ __device__ void sum_parts(const float* __restrict__ part, int64_t parts, int64_t
 }
 
 // Everything between a piece's scores and its products, by workgroups: `columns` of them for
-// dbias, `losts` for the rows' roundings, the rest for x.
+// dbias, `losts` for the rows' roundings, `cleans` for x (as many as there are flags).
 struct GradBetween {
   const float *column_part, *lost_part;
   float *dbias, *lost;
@@ -274,19 +273,18 @@ struct GradBetween {
   GradHead* head;
   void* clean;
   int64_t ld_clean;
-  int nflags;
+  int cleans;
 };
 template <typename T>
 __global__ void __launch_bounds__(1024) k_grad_between(const GradCall c, const GradBetween b) {
   __shared__ float sums[16][64];
   const int64_t g = group_index(), rest = g - b.columns - b.losts;
-  const int64_t cleans = int64_t(gridDim.x) * gridDim.y - b.columns - b.losts;
   if (g < b.columns)
     sum_parts(b.column_part, b.column_parts, b.ld_column, b.n, g, b.dbias, sums);
   else if (rest < 0)
     sum_parts(b.lost_part, b.lost_parts, c.M, c.M, g - b.columns, b.lost, sums);
-  else
-    grad_clean<T>(c, rest, cleans, b.flags, b.nflags, b.head, static_cast<T*>(b.clean), b.ld_clean);
+  else if (rest < b.cleans)
+    grad_clean<T>(c, rest, b.cleans, b.flags, b.cleans, b.head, static_cast<T*>(b.clean), b.ld_clean);
 }
 
 // g, its column sums and what its rounding takes from each row, from a split product's parts: 512
@@ -504,7 +502,7 @@ static hipError_t prepare(const GradCall& c, const GradWs& w, void* ws, hipStrea
   const int64_t commons = c.dx ? (c.K + 15) / 16 : 0, scans = c.dW ? scan_groups(c.M) : 0;
   hipLaunchKernelGGL(k_grad_prepare<T>, groups_grid(1 + commons + scans), dim3(1024), 0, stream, c,
                      c.dtype == kF16 ? 14 : 0, at<GradHead>(ws, w.head), commons, at<float>(ws, w.common),
-                     at<int32_t>(ws, w.flags));
+                     scans, at<int32_t>(ws, w.flags));
   return hipGetLastError();
 }
 
@@ -528,7 +526,7 @@ static hipError_t between(const GradCall& c, const GradWs& w, const GradArgs& a,
   }
   const int64_t scans = c.dW && first ? scan_groups(c.M) : 0;
   b.flags = at<int32_t>(ws, w.flags);
-  b.nflags = static_cast<int>(scans);
+  b.cleans = static_cast<int>(scans);
   b.head = at<GradHead>(ws, w.head);
   b.clean = at<void>(ws, w.clean);
   b.ld_clean = w.ldx;

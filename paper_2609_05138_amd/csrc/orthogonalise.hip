@@ -319,8 +319,14 @@ Step step_of(int64_t rows, int64_t cols, bool tall) {
   return s;
 }
 
+// (rows longer than a tile's offsets span go through registers, by a plan of their own)
 size_t partial_floats(const ExtraArgs& a) {
-  return plan_extra(a.I, a.J, a.K, a.elem, a.p_kc, a.q_kc, true, a.symmetric).partial_floats;
+  size_t most = 0;
+  for (const bool dma : {true, false}) {
+    const size_t f = plan_extra(a.I, a.J, a.K, a.elem, a.p_kc, a.q_kc, dma, a.symmetric).partial_floats;
+    if (f > most) most = f;
+  }
+  return most;
 }
 
 }  // namespace
