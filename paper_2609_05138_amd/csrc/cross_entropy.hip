@@ -14,13 +14,18 @@
 // piece, in x's type because the matrix cores take 16 bits (as som_product_backward's dP), and
 // its column sums unrounded; two products add the piece to dx (in fp32 until the last piece)
 // and give its part of dW.  A row of g sums to zero, so what all classes' weights have in common (a
-// codebook's are positive, with a mean far from zero) cancels in dx, but not what g's rounding does to it: that
-// is the row's sum of roundings times the common part, which is added back (with the mean of up to
-// 256 classes in its place; without it dx of a codebook of [0, 1) is 2.1 times as far from 64 bits as
-// its own rounding, with it 1.4 times, as where nothing is in common).  g is scaled by a power of two that dloss's largest value sets, so that
-// fp16 holds what a mean over many rows gives (1 / M times a probability).
+// codebook's are positive, with a mean far from zero) cancels in dx, but not what g's rounding does
+// to it: that is the row's sum of roundings times the common part, which is added back (with the
+// mean of up to 256 classes in its place; without it dx of a codebook of [0, 1) is 2.1 times as far
+// from 64 bits as its own rounding, with it 1.4 times, as where nothing is in common).  g is scaled
+// by a power of two that dloss's largest value sets, so that fp16 holds what a mean over many rows
+// gives (1 / M times a probability).
 //
-// Bound: the matrix cores.
+// Bound: the matrix cores at the clock that power leaves them (8,192 x 4,096 x 65,536 in bf16 3,172
+// to 3,240 us, 1,360 to 1,390 TFLOP/s; gradients of 8,192 x 2,048 x 65,536 5,220 us, 1,260, of
+// which the scores' third, whose epilogue makes and writes g, 40%); one row: the weights' bytes
+// (65,536 x 2,048 40 us, 6.7 TB/s, and 10 us for the two launches after it); small gradients: five
+// launches.
 #include "cross_entropy.h"
 
 #include "product_modes.h"
@@ -31,9 +36,9 @@ namespace {
 constexpr int kScoreThreads = 1024, kScoreColumns = kScoreThreads * 8;   // of a pass of k_loss_scores
 constexpr int64_t kOneWorkgroup = 4 * kScoreColumns;     // a row of so many goes without k_loss_join
 constexpr int64_t kRowsAtOnce = 65536;         // forward: rows of one launch, for the pairs' room
-// Backward: a piece's g has 2^27 bytes, half of what the memory-side cache holds, but no fewer than 8,192
-// classes, since dx's sums are read and written for each (8,192 x 2,048 x 65,536: pieces of 2^27
-// bytes 5,261 us, 2^28 5,400, 2^30 5,347; 16,384 x 1,024 x 65,536: 6,705, 6,134 and 6,051).
+// Backward: a piece's g has 2^27 bytes, half of what the memory-side cache holds, but no fewer than
+// 8,192 classes, since dx's sums are read and written for each (8,192 x 2,048 x 65,536: pieces of
+// 2^27 bytes 5,261 us, 2^28 5,400, 2^30 5,347; 16,384 x 1,024 x 65,536: 6,705, 6,134 and 6,051).
 constexpr int64_t kPieceBytes = int64_t(1) << 27;
 constexpr int64_t kLeastPiece = 8192;
 

@@ -16,13 +16,16 @@
 // X lies in rows and columns rounded up to 64 (a step of the product), with zeros, which stay
 // zeros: no product but the last, whose result is y, has a partial step or column.
 //
-// Small matrices take products of their own: tiles of 32 x 32, whose eight waves share the k axis and read their fragments from the L2 without LDS, so that a
-// product is little more than a launch and two memory latencies.  They read rows of k only, so
-// X's fp16 copy is kept transposed too.  Of sides up to kLowSide, which average less of it out, what
-// rounding leaves of B is kept and multiplied as well (153 x 221, 6 steps: 2.1e-3 from 64 bits before
-// y's rounding, with it 1.5e-3).
+// Small matrices take products of their own: tiles of 32 x 32, whose eight waves share the k axis
+// and read their fragments from the L2 without LDS, so that a product is little more than a launch
+// and two memory latencies.  They read rows of k only, so X's fp16 copy is kept transposed too.  Of
+// sides up to kLowSide, which average less of it out, what rounding leaves of B is kept and
+// multiplied as well (153 x 221, 6 steps: 2.1e-3 from 64 bits before y's rounding, with it 1.5e-3).
 //
-// Bound: the matrix cores for sides of 2,048 and more; else 3 launches a step.
+// Bound: the matrix cores for sides of 2,048 and more (4,096 x 4,096, 5 steps: 1,613 us; the symmetric
+// products 88 to 97 us each on the 136 tiles that they need, the update 116 to 126, of which 25 are
+// X's reading and writing in fp32); else 3 launches a step (1,024 x 512: 104 us, 15 products of 4
+// to 8).
 #include "orthogonalise.h"
 
 #include <cmath>

@@ -8,15 +8,18 @@
 // Into 16 bits the 8-bit matrix instruction of 128 k is used.  It lines its products up before it
 // adds them and drops bits that fp32 keeps: 1.4e-5 of the sum's root mean square on normal
 // data (1.7e-5 of the sum of magnitudes at the most), started from zero for each block, against 2.0e-4
-// (fp16) and 1.7e-3 (bf16) of the output's rounding.  Into fp32 the codes are widened (exactly) to fp16 and
-// products and sums are fp32's, at half the rate.
+// (fp16) and 1.7e-3 (bf16) of the output's rounding.  Into fp32 the codes are widened (exactly) to
+// fp16 and products and sums are fp32's, at half the rate.
 //
 // The factors come into LDS with the operands: of the tile's rows, then of its columns, a dword a
 // lane.  A lane multiplies its sums of a row by one factor (Q's blocks of 128 units:
 // the wave's columns share theirs), or by the row's and by its columns' (blocks of one unit).
 //
-// Bound, large: the matrix cores and the clock that power leaves them; small, few rows: as the
-// product's.
+// Bound, large: the matrix cores at the clock that power leaves them, of whose cycles a step fills
+// 60%, and the sums' entering, which takes a ninth of the time (8,192^3 into bf16 450 to 484 us
+// over the cards measured on, 2,270 to 2,440 TFLOP/s; without the factors 442 where with them 484,
+// on zeros 391; with factors of columns 527 to 588; into fp32 903 to 942, 1,170 to 1,220); small,
+// few rows: as the product's (one row of 4,096 x 4,096 5.7 us of device time).
 #pragma once
 
 #include "product.h"
@@ -184,8 +187,9 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product_blocks(const BlockArgs 
     // Whole steps.  A step's rows of tiles are multiplied one by one while the next row's
     // fragments are read; at the last but one every wave has asked for all of the step: one
     // barrier, by which step t + 1 has arrived, then the last two rows, while step t + NS is
-    // sent for into t's place and t + 1's first fragments are read, each in the place of one
-    // that has just been used.
+    // sent for into t's place, a load or so a product (all of them before the first: 468 us for
+    // 8,192^3 instead of 450), and t + 1's first fragments are read, each in the place of one that
+    // has just been used.
     const int32_t full = (k1 - k0) / kStep;
     constexpr int kMost = OpP::kEach + OpQ::kEach + 1;
     static_assert(OpQ::whole, "every wave moves the same share of Q");
@@ -229,14 +233,16 @@ __global__ void __launch_bounds__(WI* WJ * 64) k_product_blocks(const BlockArgs 
         for (int x = 0; x < TI; ++x) {
           __builtin_amdgcn_sched_barrier(0);
           if (x + 1 < TI) read_p(freed, x + 1);
-          if (x == kTurn) {
-            arrived(t + 1, NS - 2);
-            if constexpr (decltype(fetches)::value)
-#pragma unroll
-              for (int n = 0; n < kMost; ++n) fetch_one(n, t + NS, freed);
-          }
+          if (x == kTurn) arrived(t + 1, NS - 2);
 #pragma unroll
           for (int y = 0; y < TJ; ++y) {
+            if constexpr (decltype(fetches)::value) {
+              constexpr int kOver = (TI - kTurn) * TJ;
+              const int m = (x - kTurn) * TJ + y;
+              if (x >= kTurn)
+#pragma unroll
+                for (int n = m * kMost / kOver; n < (m + 1) * kMost / kOver; ++n) fetch_one(n, t + NS, freed);
+            }
             multiply(x, y);
             // (after the last step: bytes that no product uses)
             if (x == TI - 1) read_q(next, y);

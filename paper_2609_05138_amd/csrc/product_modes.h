@@ -16,8 +16,9 @@ struct ExtraArgs : ProductArgs {
   void* half;                // [I][ldh] or nullptr
   int64_t ldh;
   float half_scale;
-  // C is symmetric (I = J; `residual` too; no row, column, half and swap): kMirror, which calculates the
-  // tiles on and above the diagonal and writes their transposes too, will do where it is faster
+  // C is symmetric (I = J; `residual` too; no row, column, half and swap): kMirror, which
+  // calculates the tiles on and above the diagonal and writes their transposes too, will do where
+  // it is faster
   bool symmetric;
   // where *swap is not 0, P (or Q) is read from `swapped` instead
   const int32_t* swap;       // or nullptr

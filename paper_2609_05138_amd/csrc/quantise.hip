@@ -3,8 +3,9 @@
 //
 //   s = max |x| / 448 over the block,  q = x / s
 //
-// Bound: HBM (a maximum, a product and a conversion per element).  An element is read once
-// and stays in registers while its block's maximum is made.
+// Bound: HBM (a maximum, a product and a conversion per element; 16,384 x 8,192 in bf16 76 us, 5.3
+// TB/s, a copy's rate; transposed 89 us, 4.5).  An element is read once and stays in registers
+// while its block's maximum is made.
 //
 //   rows    a wave takes 512 columns (four blocks) of four rows, 16 lanes a block; the
 //           workgroup's 16 rows are next to each other, so that the factors of a block of
@@ -34,7 +35,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) k_quantise_rows(const QuantiseArgs a, uint32_t col_groups) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // bands of kTileBand row groups: an XCD takes a row group's columns one after the other, and finds
-  // the lines that rows off 16 bytes share in its L2
+  // the lines that rows off 16 bytes share in its L2 (16,384 x 8,191 155 to 90 us)
   const int64_t g = group_index(), band = g / (int64_t(col_groups) * kTileBand), in = g - band * col_groups * kTileBand;
   const int64_t cg = in / kTileBand, rg = band * kTileBand + in % kTileBand;
   const int64_t row0 = rg * kRowsGroup + wave * kRowsWave, col = cg * 512 + lane * 8;
