@@ -586,14 +586,14 @@ som_status som_dropout(const void* x, int64_t ldx, const void* residual, int64_t
  *     lse[m] = log sum_n exp v[m][n],  loss[m] = lse[m] - v[m][labels[m]].
  *
  * x and W are as som_product's, fp16 or bf16; with alpha = 2 t and bias = -t |w_n|^2 the scores
- * are -t times the squared distances to a codebook's units, but for |x|^2, which cancels.  A label outside [0, N)
- * is none: that document's loss is 0 (its lse is made all the same).  A class whose bias is minus
- * infinity is left out; a document with no class left has lse minus infinity, and a label
- * that is left out costs plus infinity.  A NaN or plus infinity among a document's scores makes its lse NaN.
- * loss and lse are [M], fp32.
- * M in [0, 2^31), N and K in [1, 2^30], with som_product's limit on their tiles.  ws:
- * som_cross_entropy_workspace_bytes, 256-byte aligned (8 bytes for 128 scores of up to 65,536
- * documents, and the scores themselves where a product is small or has up to four rows). */
+ * are -t times the squared distances to a codebook's units, but for |x|^2, which cancels.  A
+ * label outside [0, N) is none: that document's loss is 0 (its lse is made all the same).  A
+ * class whose bias is minus infinity is left out; a document with no class left has lse minus
+ * infinity, and a label that is left out costs plus infinity.  A NaN or plus infinity among a
+ * document's scores makes its lse NaN. loss and lse are [M], fp32. M in [0, 2^31), N and K in [1,
+ * 2^30], with som_product's limit on their tiles.  ws: som_cross_entropy_workspace_bytes,
+ * 256-byte aligned (8 bytes for 128 scores of up to 65,536 documents, and the scores themselves
+ * where a product is small or has up to four rows). */
 size_t som_cross_entropy_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype);
 som_status som_cross_entropy(const void* x, int64_t ldx, const void* W, int64_t ldw, int32_t w_units, int32_t dtype,
                              int64_t M, int64_t N, int64_t K, const int32_t* labels, const float* bias, float alpha,
@@ -606,12 +606,12 @@ som_status som_cross_entropy(const void* x, int64_t ldx, const void* W, int64_t 
  *     dx = alpha g W^T,  dW = alpha x^T g,  dbias_n = sum_m g[m][n].
  *
  * dx and dW (laid out as W is) are of x's type, dbias is fp32; each may be NULL.  The scores
- * are calculated again, for a piece of the classes at a time (128 MB of g, or 8,192 classes); g is rounded to
- * x's type for the two products, scaled by a power of two so that fp16 holds a mean's small
- * values, and dbias sums it unrounded.  A document without a label, with dloss 0 or with no class left
- * gives zeros to everything, whatever its x holds, NaN too (the weights of classes that are left
- * out have to be finite).  lse has no gradient of its own.  No output overlaps an input.
- * With M == 0 dW and dbias are set to zero.  M up to 2^30.  ws:
+ * are calculated again, for a piece of the classes at a time (128 MB of g, or 8,192 classes); g
+ * is rounded to x's type for the two products, scaled by a power of two so that fp16 holds a
+ * mean's small values, and dbias sums it unrounded.  A document without a label, with dloss 0 or
+ * with no class left gives zeros to everything, whatever its x holds, NaN too (the weights of
+ * classes that are left out have to be finite).  lse has no gradient of its own.  No output
+ * overlaps an input. With M == 0 dW and dbias are set to zero.  M up to 2^30.  ws:
  * som_cross_entropy_backward_workspace_bytes, 256-byte aligned. */
 size_t som_cross_entropy_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype);
 som_status som_cross_entropy_backward(const float* dloss, const void* x, int64_t ldx, const void* W, int64_t ldw,
@@ -630,9 +630,9 @@ som_status som_cross_entropy_backward(const float* dloss, const void* x, int64_t
  * that q is; its factors are scale[r / block_rows * scale_row + c / 128 * scale_block] at
  * row r and column c of q, with strides that keep them apart.  som_product_blocks reads them
  * fastest with scale_row 1: the factors of one block of columns next to each other.
- * x is fp32, fp16 or bf16; q and scale do not overlap x.  A NaN or an infinity in a block makes its factor NaN or
- * infinite, and none of the block's values can be had from it.
- * Rows and cols below 2^31; rows == 0 is a no-op. */
+ * x is fp32, fp16 or bf16; q and scale do not overlap x.  A NaN or an infinity in a block makes
+ * its factor NaN or infinite, and none of the block's values can be had from it. Rows and cols
+ * below 2^31; rows == 0 is a no-op. */
 som_status som_quantise(const void* x, int64_t ldx, int32_t dtype, int64_t rows, int64_t cols, int32_t block_rows,
                         int32_t transpose, void* q, int64_t ldq, float* scale, int64_t scale_row,
                         int64_t scale_block, hipStream_t stream);
@@ -644,15 +644,15 @@ som_status som_quantise(const void* x, int64_t ldx, int32_t dtype, int64_t rows,
  *
  * x [M][ldx]; W is unit-major, [N][ldw].  sx and sw are x_scale's and w_scale's factors (fp32):
  * at row r and column k, p[r / rows * row_stride + k / 128 * block_stride], rows being 1 or 128;
- * strides may be 0 and up.  som_quantise makes such operands: x in blocks of one row and weights in blocks of 128
- * are the common choice, which is the fastest.  The gradients are products of the same kind: dx's
- * of dP in blocks along N and the transposed weights (whose blocks of 128 x 128 are the same
- * ones), dW's of dP and x transposed, both in blocks along M.
- * e as for som_product, without x_scale and w_scale, which have to be NULL.  y, residual and pre
- * are fp16, bf16 or fp32.  Sums over a block are rounded to about 16 bits of their size for
- * y of 16 bits (the 8-bit matrix instructions; errors of 1.4e-5 of their root mean square), to fp32 for
- * fp32 y, at half the rate; sums of blocks are fp32.
- * Sizes and workspace (som_product_blocks_workspace_bytes) as for som_product. */
+ * strides may be 0 and up.  som_quantise makes such operands: x in blocks of one row and weights
+ * in blocks of 128 are the common choice, which is the fastest.  The gradients are products of
+ * the same kind: dx's of dP in blocks along N and the transposed weights (whose blocks of 128 x
+ * 128 are the same ones), dW's of dP and x transposed, both in blocks along M. e as for
+ * som_product, without x_scale and w_scale, which have to be NULL.  y, residual and pre are fp16,
+ * bf16 or fp32.  Sums over a block are rounded to about 16 bits of their size for y of 16 bits
+ * (the 8-bit matrix instructions; errors of 1.4e-5 of their root mean square), to fp32 for fp32
+ * y, at half the rate; sums of blocks are fp32. Sizes and workspace
+ * (som_product_blocks_workspace_bytes) as for som_product. */
 typedef struct som_block_scale {
   const float* p;
   int64_t row_stride, block_stride;
@@ -670,15 +670,16 @@ som_status som_product_blocks(const void* x, int64_t ldx, const som_block_scale*
  *
  *     X = G / |G|_F;  `steps` times:  A = X X^T,  X = a X + (b A + c A A) X;  y = X
  *
- * (tall matrices: of the transpose, which is the same).  (3.4445, -4.7750, 2.0315) and 5 steps bring
- * singular values from 1 / 100 of the norm on to between 0.7 and 1.2; (1.5, -0.5, 0) and more steps to 1.
- * G [rows][ldg] is fp32, fp16 or bf16; y [rows][ldy] is bf16 and may be G.  X is kept in fp32, the
- * products take it and A in fp16: y is within 2e-3 (2-norm, relative) of the formula's beside its own rounding.  A
- * matrix of zeros gives zeros; a NaN or an infinity makes all of y NaN.  Singular values of X have to stay
- * below 3.9 and |a|, |b| and |c| are at most 64: coefficients for which they do not give infinities and NaN.
- * rows and cols in [1, 2^24], the smaller one up to 2^15, with som_product's limit on tiles;
- * steps in [1, 64].  ws: som_orthogonalise_workspace_bytes, 256-byte aligned (8 bytes for an
- * element of G and 4 for one of A, and more for small products). */
+ * (tall matrices: of the transpose, which is the same).  (3.4445, -4.7750, 2.0315) and 5 steps
+ * bring singular values from 1 / 100 of the norm on to between 0.7 and 1.2; (1.5, -0.5, 0) and
+ * more steps to 1. G [rows][ldg] is fp32, fp16 or bf16; y [rows][ldy] is bf16 and may be G.  X is
+ * kept in fp32, the products take it and A in fp16: y is within 2e-3 (2-norm, relative) of the
+ * formula's beside its own rounding.  A matrix of zeros gives zeros; a NaN or an infinity makes
+ * all of y NaN.  Singular values of X have to stay below 3.9 and |a|, |b| and |c| are at most 64:
+ * coefficients for which they do not give infinities and NaN. rows and cols in [1, 2^24], the
+ * smaller one up to 2^15, with som_product's limit on tiles; steps in [1, 64].  ws:
+ * som_orthogonalise_workspace_bytes, 256-byte aligned (8 bytes for an element of G and 4 for one
+ * of A, and more for small products). */
 size_t som_orthogonalise_workspace_bytes(int64_t rows, int64_t cols);
 som_status som_orthogonalise(const void* G, int64_t ldg, int32_t dtype, int64_t rows, int64_t cols, int32_t steps,
                              float a, float b, float c, void* y, int64_t ldy, void* ws, size_t ws_bytes,
