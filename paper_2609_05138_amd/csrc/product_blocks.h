@@ -15,11 +15,12 @@
 // lane.  A lane multiplies its sums of a row by one factor (Q's blocks of 128 units:
 // the wave's columns share theirs), or by the row's and by its columns' (blocks of one unit).
 //
-// Bound, large: the matrix cores at the clock that power leaves them, of whose cycles a step fills
-// 60%, and the sums' entering, which takes a ninth of the time (8,192^3 into bf16 450 to 484 us
-// over the cards measured on, 2,270 to 2,440 TFLOP/s; without the factors 442 where with them 484,
-// on zeros 391; with factors of columns 527 to 588; into fp32 903 to 942, 1,170 to 1,220); small,
-// few rows: as the product's (one row of 4,096 x 4,096 5.7 us of device time).
+// Bound, large: the matrix cores at the clock that power leaves them (busy in 47% of the cycles, at
+// 2.0 GHz, of 8,192 x 4,096 x 16,384 with GELU and its argument kept), the sums' entering, and the
+// step's LDS reads (8,192^3 into bf16 450 to 484 us over the cards measured on, 2,270 to 2,440
+// TFLOP/s; a variant without the factors took 442 us where with them it was 500, on zeros 359 and
+// 391; with factors of columns 527 to 588; into fp32 903 to 942, 1,170 to 1,220); small, few rows:
+// as the product's (one row of 4,096 x 4,096 5.7 us of device time).
 #pragma once
 
 #include "product.h"
