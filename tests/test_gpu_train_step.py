@@ -175,3 +175,46 @@ def test_two_graphs_with_workspaces_of_their_own_replay_at_once():
         torch.cuda.synchronize()
         for _, got, want, _, _ in cases:
             assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_two_threads_on_streams_of_their_own_get_their_own_results():
+    import threading
+
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    bf = torch.bfloat16
+    sizes = [(200, 256, 700), (131, 384, 1000)]
+    cases = []
+    for M, K, N in sizes:
+        x = torch.randn((M, K), generator=g, device=DEV).to(bf)
+        W = (torch.randn((N, K), generator=g, device=DEV) / 16).to(bf)
+        label = torch.randint(0, N, (M,), generator=g, device=DEV).int()
+        dloss = torch.rand(M, generator=g, device=DEV)
+
+        def run(stream, x=x, W=W, label=label, dloss=dloss):
+            loss, lse = som.som_cross_entropy(x, W.t(), label, stream=stream)
+            dx, dW, db = som.som_cross_entropy_backward(dloss, x, W.t(), label, lse, stream=stream)
+            step = som.som_orthogonalise(dW.t(), stream=stream)
+            q, s = som.som_quantise(x, stream=stream)
+            w, ws = som.som_quantise(step, 128, stream=stream)
+            return loss, lse, dx, dW, db, step, som.som_product_blocks(q, s, w.t(), ws, stream=stream)
+
+        want = run(None)
+        torch.cuda.synchronize()
+        cases.append((run, want, torch.cuda.Stream()))
+    got = [None, None]
+
+    def work(i):
+        run, _, stream = cases[i]
+        got[i] = [run(stream) for _ in range(20)]
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for (_, want, _), results in zip(cases, got):
+        assert results is not None
+        for result in results:
+            assert all(torch.equal(a, b) for a, b in zip(result, want))
