@@ -626,6 +626,8 @@ som_status som_cross_entropy_backward(const float* dloss, const void* x, int64_t
  *
  *     s = max |x| / 448 over the block, at least 2^-126 (1 where every x is 0),  q = x / s.
  *
+ * s and the quotient are fp32's, and q is the quotient rounded to nearest even.
+ *
  * q is x, or with transpose set x's transpose ([cols][ldq]), and the blocks are of the matrix
  * that q is; its factors are scale[r / block_rows * scale_row + c / 128 * scale_block] at
  * row r and column c of q, with strides that keep them apart.  som_product_blocks reads them

@@ -96,6 +96,33 @@ def test_not_finite_values_spoil_their_block_alone(bad, block_rows, transpose):
     assert bool(same[each.isfinite()].all())
 
 
+def _division(x, scale, block_rows):
+    """The codes of x / s: fp32's quotient, rounded to E4M3, by the host."""
+    each = scale.cpu().repeat_interleave(128, 1)[:, :x.shape[1]].repeat_interleave(block_rows, 0)[:x.shape[0]]
+    return (x.float().cpu() / each).to(torch.float8_e4m3fn)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("block_rows,transpose", [(1, False), (1, True), (128, False), (128, True)])
+def test_codes_are_the_quotients(kind, block_rows, transpose):
+    # every block of 128 x 128 of a size of its own, over the type's range, with zeros of both signs
+    # (two such matrices, whose quotients are next to a tie between two codes for many values)
+    small, large = {"f32": (-148, 118), "f16": (-20, 10), "bf16": (-132, 118)}[kind]
+    for seed in (0, 1):
+        x = _x(1100, 1000, kind, 0, seed).float()
+        size = torch.as_tensor(np.random.default_rng(seed).integers(small, large, (9, 8)), device=DEV)
+        half = (size // 2).repeat_interleave(128, 0).repeat_interleave(128, 1)[:1100, :1000]
+        rest = (size - size // 2).repeat_interleave(128, 0).repeat_interleave(128, 1)[:1100, :1000]
+        x = (torch.ldexp(torch.ldexp(x, half), rest)).to(T[kind])
+        x[::7, ::5] = 0.0
+        x[::11, ::3] = -0.0
+        q, scale = som.som_quantise(x, block_rows, transpose)
+        want = _division(x.t() if transpose else x, scale, block_rows)
+        assert bool(scale.isfinite().all())
+        differ = q.cpu().view(torch.uint8) != want.view(torch.uint8)
+        assert not bool(differ.any()), (int(differ.sum()), differ.nonzero()[:4].tolist())
+
+
 def test_many_rows_and_columns():
     x = torch.randn((70000, 136), device=DEV).bfloat16()
     # in 64 bits: torch divides an fp32 tensor by a number as a product with its rounded inverse
