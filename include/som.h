@@ -673,13 +673,20 @@ som_status som_product_blocks(const void* x, int64_t ldx, const som_block_scale*
  *     X = G / |G|_F;  `steps` times:  A = X X^T,  X = a X + (b A + c A A) X;  y = X
  *
  * (tall matrices: of the transpose, which is the same).  (3.4445, -4.7750, 2.0315) and 5 steps
- * bring singular values from 1 / 100 of the norm on to between 0.7 and 1.2; (1.5, -0.5, 0) and
- * more steps to 1. G [rows][ldg] is fp32, fp16 or bf16; y [rows][ldy] is bf16 and may be G.  X is
- * kept in fp32, the products take it and A in fp16: y is within 2e-3 (2-norm, relative) of the
- * formula's beside its own rounding.  A matrix of zeros gives zeros; a NaN or an infinity makes
- * all of y NaN.  Singular values of X have to stay below 3.9 and |a|, |b| and |c| are at most 64:
- * coefficients for which they do not give infinities and NaN. rows and cols in [1, 2^24], the
- * smaller one up to 2^15, with som_product's limit on tiles; steps in [1, 64].  ws:
+ * bring singular values from 1 / 100 of the norm on to between 0.68 and 1.14; (1.5, -0.5, 0) and
+ * more steps to 1. G [rows][ldg] is fp32, fp16 or bf16; y [rows][ldy] is bf16 and may be G.  A
+ * matrix of zeros gives zeros; a NaN or an infinity makes all of y NaN.
+ *
+ * X is kept in fp32, the products take it and A in fp16.  What these roundings leave of y, beside its
+ * own (2-norm, relative, measured on matrices of normal values, sides of 8 to 20,000), is 1e-3 to 3e-3 after
+ * 5 or 6 steps of (3.4445, -4.7750, 2.0315) and grows with the steps: 3e-3 to 4e-3 after 10, up to
+ * 2e-2 after 64; (1.5, -0.5, 0) stays below 6e-4.  It grows with the slope of a s + b s^3 + c s^5
+ * about s = 1, too: (4.0848, -6.8946, 2.9270), whose slope there reaches -3, gives 5e-3 to 8e-3 after 5
+ * steps, up to 5e-2 after 8, and after 20 y is no longer the formula's.
+ *
+ * Singular values of X have to stay below 3.9 and |a|, |b| and |c| are at most 64: coefficients for
+ * which they do not give infinities and NaN. rows and cols in [1, 2^24], the smaller one up to
+ * 2^15, with som_product's limit on tiles; steps in [1, 64].  ws:
  * som_orthogonalise_workspace_bytes, 256-byte aligned (8 bytes for an element of G and 4 for one
  * of A, and more for small products). */
 size_t som_orthogonalise_workspace_bytes(int64_t rows, int64_t cols);

@@ -7,9 +7,10 @@
 //
 // What is rounded: X is kept in fp32, which the term a X takes as it is; the products take X, A and
 // B in fp16, whose 11 bits and not bf16's 8 are what the steps, which amplify small directions 3.4
-// times each, leave as errors: 1e-3 to 2e-3 of the result (2-norm; half of what bf16's rounding of y
-// adds), with bf16 between the steps 1e-2, with X in fp16 too 5e-3 where singular values spread
-// over 10^4.  X's fp16 copy is scaled by a power of two that makes its elements' size about 1,
+// times each, leave as errors: 1e-3 to 2e-3 of the result after 5 steps of (3.4445, -4.7750, 2.0315)
+// (2-norm; bf16's rounding of y adds 1.7e-3), 3e-3 to 4e-3 after 10, 2e-2 after 64, and more with
+// coefficients whose map is steeper about 1; with bf16 between the steps 1e-2, with X in fp16 too
+// 5e-3 where singular values spread over 10^4.  X's fp16 copy is scaled by a power of two that makes its elements' size about 1,
 // since they are 1 / sqrt(m n) of the norm and would lie among fp16's subnormal numbers.
 // The norm is summed in fp64, so no gradient is too small or large for its squares.
 //
@@ -20,7 +21,8 @@
 // and read their fragments from the L2 without LDS, so that a product is little more than a launch
 // and two memory latencies.  They read rows of k only, so X's fp16 copy is kept transposed too.  Of
 // sides up to kLowSide, which average less of it out, what rounding leaves of B is kept and
-// multiplied as well (153 x 221, 6 steps: 2.1e-3 from 64 bits before y's rounding, with it 1.5e-3).
+// multiplied as well (5 steps, before y's rounding: 32 x 1,000 3.1e-3 without and 1.8e-3 with it, 153 x 221
+// 1.8e-3 and 1.4e-3).
 //
 // Bound: the matrix cores for sides of 2,048 and more (4,096 x 4,096, 5 steps: 1,613 us; the symmetric
 // products 88 to 97 us each on the 136 tiles that they need, the update 116 to 126, of which 25 are

@@ -139,6 +139,51 @@ def test_streams_and_graphs():
         assert torch.equal(y, som.som_orthogonalise(X))
 
 
+STEEP = (4.0848, -6.8946, 2.9270)          # |slope| up to 3.2 about s = 1: roundings grow with every step
+
+
+def _own(want):
+    """The result's own rounding."""
+    return _far(torch.as_tensor(want).to(torch.bfloat16), want)
+
+
+def _roundings(G, steps, coefficients, low, seed=0):
+    """What the documented roundings leave of the result: X, A and B off by up to 2^-11 of each element (2^-25
+    where that is more: fp16's subnormal step), uniformly, in 64 bits.  A rounding to 11 bits is off
+    by 2^-11 at the most and by half of it where its leading digits are largest, so this is more
+    than it leaves (1.4 times, for elements of all sizes alike)."""
+    rng = np.random.default_rng(seed)
+    a, b, c = coefficients
+    G = G.T if G.shape[0] > G.shape[1] else G
+
+    def off(v, symmetric):
+        e = rng.uniform(-1.0, 1.0, v.shape) * np.maximum(2.0 ** -11 * np.abs(v), 2.0 ** -25 if symmetric else 0.0)
+        return v + (np.triu(e) + np.triu(e, 1).T if symmetric else e)
+
+    X = Y = G / np.linalg.norm(G)
+    for _ in range(steps):
+        h = off(X, False)
+        A = off(h @ h.T, True)
+        B = b * A + c * (A @ A)
+        X = a * X + (B if low else off(B, True)) @ h
+        S = Y @ Y.T
+        Y = a * Y + (b * S + c * (S @ S)) @ Y
+    return np.linalg.norm(X - Y) / np.linalg.norm(Y)
+
+
+# (short sides above and up to 256, of the small products and of the large ones)
+@pytest.mark.parametrize("rows,cols", [(300, 300), (153, 221), (600, 500), (1100, 600)])
+@pytest.mark.parametrize("coefficients,steps", [(QUINTIC, 1), (QUINTIC, 5), (QUINTIC, 10), (QUINTIC, 30), (QUINTIC, 64),
+                                                (STEEP, 3), (STEEP, 5), (STEEP, 8)])
+def test_errors_grow_with_steps_and_slopes_as_roundings_do(coefficients, steps, rows, cols):
+    # within a quarter more than the simulated roundings, which are of other draws, and y's own
+    G = torch.as_tensor(np.random.default_rng(steps).normal(size=(rows, cols)), dtype=torch.float32, device=DEV)
+    G64 = G.double().cpu().numpy()
+    want = oracle.orthogonalise(G64, steps, coefficients)
+    error = _roundings(G64, steps, coefficients, min(rows, cols) <= 256)
+    assert _far(som.som_orthogonalise(G, steps, coefficients), want) <= np.hypot(1.25 * error, 1.01 * _own(want))
+
+
 def test_refusals():
     G = torch.zeros((8, 16), device=DEV)
     c = som.som_orthogonalise
