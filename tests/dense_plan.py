@@ -48,3 +48,35 @@ def tile(lib, I, J, K, elem, p_contiguous, q_contiguous, on16):
     fn.restype = _Plan
     fn.argtypes = [ctypes.c_int64] * 3 + [ctypes.c_int] + [ctypes.c_bool] * 3
     return SHAPES[fn(I, J, K, elem, p_contiguous, q_contiguous, on16).shape]
+
+
+class _Rules(ctypes.Structure):
+    _fields_ = [("few", ctypes.c_bool), ("first", ctypes.c_int), ("symmetric", ctypes.c_bool)]
+
+
+class _RuledPlan(ctypes.Structure):
+    _fields_ = _Plan._fields_ + [("upper", ctypes.c_bool)]
+
+
+def extra(lib, I, J, K, elem, p_contiguous, q_contiguous, on16, symmetric=False):
+    """(tile's name, splits of k, whether only tiles on and above the diagonal) of a product with an epilogue of
+    its own."""
+    fn = lib._ZN3som15plan_product_byElllibbbRKNS_9PlanRulesE
+    fn.restype = _RuledPlan
+    fn.argtypes = [ctypes.c_int64] * 3 + [ctypes.c_int] + [ctypes.c_bool] * 3 + [ctypes.POINTER(_Rules)]
+    p = fn(I, J, K, elem, p_contiguous, q_contiguous, on16, ctypes.byref(_Rules(False, 0, symmetric)))
+    return SHAPES[p.shape], p.splits, p.upper
+
+
+# (documents, classes, features) of gradients: (splits of the scores' k axis, of dx's)
+CLASSES = {
+    (300, 1024, 512): (1, 1),
+    (200, 600, 6000): (12, 1),
+    (600, 3000, 256): (1, None),         # 6 or 8
+    (8200, 16500, 24): (1, None),        # three pieces of the classes
+}
+
+
+def gradient_splits(lib, M, N, K, units, on16):
+    n = min(N, 8192)
+    return extra(lib, M, n, K, BF16, True, units, on16)[1], extra(lib, M, K, n, BF16, True, not units, on16)[1]

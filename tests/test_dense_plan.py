@@ -4,7 +4,7 @@ import os
 
 import pytest
 
-from dense_plan import BF16, E4M3, F16, GRADIENTS, PRODUCTS, PRODUCTS_8, tile
+from dense_plan import (BF16, CLASSES, E4M3, F16, GRADIENTS, PRODUCTS, PRODUCTS_8, gradient_splits, tile)
 
 som = pytest.importorskip("paper_2609_05138_amd.som")
 
@@ -54,3 +54,11 @@ RAGGED = {
 def test_rows_off_16_bytes_take_the_best_tiles(lib):
     for (M, N, K), want in RAGGED.items():
         assert tile(lib, M, N, K, BF16, True, True, False) == want, (M, N, K)
+
+
+def test_gradients_with_and_without_split_axes(lib):
+    for (M, N, K), (scores, dx) in CLASSES.items():
+        for units in (False, True):
+            for on16 in (False, True):
+                got = gradient_splits(lib, M, N, K, units, on16)
+                assert got[0] == scores and (got[1] == dx if dx else got[1] > 1), (M, N, K, units, on16, got)

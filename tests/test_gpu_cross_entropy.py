@@ -15,6 +15,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
+from dense_plan import CLASSES  # noqa: E402
 from oracle import train as oracle  # noqa: E402
 
 if torch.cuda.is_available():
@@ -162,6 +163,48 @@ def test_pieces_of_the_classes_and_rows(M, N, K, layout):
         one = som.som_cross_entropy(x[i:i + 1], W, labels[i:i + 1], bias)
         assert abs(float(one[1]) - float(lse[i])) < 1e-5
     assert bool((dx.float()[labels < 0] == 0).all())
+
+
+# (unsplit; the scores' and dx's k axis split; more than one piece of the classes)
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("layout", ["feature", "unit"])
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("M,N,K", sorted(CLASSES))
+def test_what_rounding_takes_from_a_codebooks_gradient_comes_back(M, N, K, pad, layout, kind):
+    """dx of classes that have a mean mu in common.  Its own rounding leaves e of it.  g's roundings are of the
+    same size relative to g, and leave e |g| |W - mu| and their sum times mu, where dx itself is |g| |W -
+    mu| in size (the rows of g sum to zero): with uniform weights |mu|^2 = 3 |W - mu|^2, so e sqrt(1 + 1 +
+    3) = 2.2 e in all, e sqrt(2) = 1.4 e where the sum comes back, and e sqrt(1 + 1 + 4 * 3) = 3.7 e where
+    it is added with the wrong sign.  The limit lies between the first two, 1.7 e (of 24 features and
+    few documents the sizes are off by up to a tenth)."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(M)
+    Wu = torch.rand((N, K), generator=g, device=DEV)
+    Wm = Wu if layout == "unit" else Wu.t()
+    W = torch.full((Wm.shape[0], Wm.shape[1] + pad), float("nan"), device=DEV).to(T[kind])[:, :Wm.shape[1]]
+    W.copy_(Wm)
+    W = W.t() if layout == "unit" else W
+    t = 16.0 / K
+    W64 = W.double().contiguous()
+    labels = torch.randint(0, N, (M,), generator=g, device=DEV)
+    x = (W64.t()[labels].float() + 0.3 * torch.randn((M, K), generator=g, device=DEV)).to(T[kind])
+    labels[torch.rand(M, generator=g, device=DEV) < 0.1] = -1
+    labels = labels.int()
+    bias = (-t * (W64 * W64).sum(0)).float()
+    dloss = 0.5 + torch.rand(M, generator=g, device=DEV)
+    lse = som.som_cross_entropy(x, W, labels, bias, 2.0 * t)[1]
+    dx = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias, 2.0 * t, need_dW=False, need_dbias=False)[0]
+    _, _, want, _, _ = _double(x, W, labels, bias, 2.0 * t, dloss)
+    own = _far(want.to(T[kind]), want)
+    assert _far(dx, want) <= 1.7 * own
+    # and it would be more without: g rounded as documented, its sums not put back
+    has = (labels >= 0).double()
+    v = torch.exp(2.0 * t * torch.mm(x.double(), W64) + bias.double() - lse.double()[:, None])
+    v[torch.arange(M, device=DEV), labels.clamp(min=0).long()] -= 1.0
+    v *= (dloss.double() * has)[:, None]
+    size = 2.0 ** (14 if kind == "f16" else 0)              # dloss's largest is in [1, 2)
+    rounded = (v * size).to(T[kind]).double() / size
+    assert _far((2.0 * t * torch.mm(rounded, W64.t().contiguous())).to(T[kind]), want) > 1.9 * own
 
 
 def test_gradients_against_differences():
