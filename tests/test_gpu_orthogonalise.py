@@ -184,6 +184,37 @@ def test_errors_grow_with_steps_and_slopes_as_roundings_do(coefficients, steps, 
     assert _far(som.som_orthogonalise(G, steps, coefficients), want) <= np.hypot(1.25 * error, 1.01 * _own(want))
 
 
+def _in_16_bits(G, steps, coefficients, low):
+    """The steps with X, A and B rounded to fp16, and what that leaves of A and B multiplied too (low) or not."""
+    a, b, c = coefficients
+    tall = G.shape[0] > G.shape[1]
+    X = (G.T if tall else G) / np.linalg.norm(G)
+    size = 2.0 ** round(0.5 * np.log2(G.size))
+
+    def half(v):
+        return v.astype(np.float16).astype(np.float64)
+
+    for _ in range(steps):
+        h = half(X * size) / size
+        A = half(h @ h.T)
+        B = b * A + c * (A @ A)
+        X = a * X + (B if low else half(B)) @ h
+    return X.T if tall else X
+
+
+@pytest.mark.parametrize("rows,cols", [(32, 1000), (100, 900), (900, 100)])
+def test_what_rounding_leaves_of_the_polynomial_is_multiplied_too(rows, cols):
+    G = torch.as_tensor(np.random.default_rng(rows).normal(size=(rows, cols)), dtype=torch.float32, device=DEV)
+    G64 = G.double().cpu().numpy()
+    want = oracle.orthogonalise(G64, 5, QUINTIC)
+    size = np.linalg.norm(want)
+    kept, dropped = (np.linalg.norm(_in_16_bits(G64, 5, QUINTIC, low) - want) / size for low in (True, False))
+    # the same roundings but for those of fp32, which move a few of them; y's own is known to a hundredth
+    limit = 1.02 * np.hypot(1.15 * kept, _own(want))
+    assert np.hypot(dropped, _own(want)) > limit
+    assert _far(som.som_orthogonalise(G), want) <= limit
+
+
 def test_refusals():
     G = torch.zeros((8, 16), device=DEV)
     c = som.som_orthogonalise
