@@ -68,6 +68,20 @@ def extra(lib, I, J, K, elem, p_contiguous, q_contiguous, on16, symmetric=False)
     return SHAPES[p.shape], p.splits, p.upper
 
 
+# (rows, cols) of updates whose symmetric products take 256 x 256 tiles
+MIRRORED = {(4096, 4096), (4030, 4100), (4100, 4030)}
+
+
+def symmetric_tile(lib, rows, cols):
+    """(tile, only on and above the diagonal) of an update's A X X^T and of A A, where they are the same."""
+    rows, cols = (rows + 63) // 64 * 64, (cols + 63) // 64 * 64
+    tall, m = rows > cols, min(rows, cols)
+    gram = extra(lib, m, m, max(rows, cols), F16, not tall, not tall, True, True)
+    poly = extra(lib, m, m, m, F16, True, True, True, True)
+    assert gram == poly
+    return gram[0], gram[2]
+
+
 # (documents, classes, features) of gradients: (splits of the scores' k axis, of dx's)
 CLASSES = {
     (300, 1024, 512): (1, 1),

@@ -4,7 +4,8 @@ import os
 
 import pytest
 
-from dense_plan import (BF16, CLASSES, E4M3, F16, GRADIENTS, PRODUCTS, PRODUCTS_8, gradient_splits, tile)
+from dense_plan import (BF16, CLASSES, E4M3, F16, GRADIENTS, MIRRORED, PRODUCTS, PRODUCTS_8, gradient_splits,
+                        symmetric_tile, tile)
 
 som = pytest.importorskip("paper_2609_05138_amd.som")
 
@@ -54,6 +55,13 @@ RAGGED = {
 def test_rows_off_16_bytes_take_the_best_tiles(lib):
     for (M, N, K), want in RAGGED.items():
         assert tile(lib, M, N, K, BF16, True, True, False) == want, (M, N, K)
+
+
+def test_large_updates_take_the_largest_symmetric_tiles(lib):
+    for rows, cols in MIRRORED:
+        assert symmetric_tile(lib, rows, cols) == ("256x256", True), (rows, cols)
+    # a smaller one, whose products are tested too
+    assert symmetric_tile(lib, 2100, 2100) == ("128x128", True)
 
 
 def test_gradients_with_and_without_split_axes(lib):

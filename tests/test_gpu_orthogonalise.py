@@ -17,6 +17,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
+from dense_plan import MIRRORED, symmetric_tile  # noqa: E402
 from oracle import train as oracle  # noqa: E402
 
 if torch.cuda.is_available():
@@ -213,6 +214,31 @@ def test_what_rounding_leaves_of_the_polynomial_is_multiplied_too(rows, cols):
     limit = 1.02 * np.hypot(1.15 * kept, _own(want))
     assert np.hypot(dropped, _own(want)) > limit
     assert _far(som.som_orthogonalise(G), want) <= limit
+
+
+# (both layouts; the last row and column of tiles are partial)
+@pytest.mark.parametrize("rows,cols", sorted(MIRRORED))
+def test_symmetric_products_in_the_largest_tiles(rows, cols):
+    assert symmetric_tile(som.load(), rows, cols) == ("256x256", True)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(4)
+    G = torch.randn((rows, cols), generator=g, device=DEV)
+    X = G.double() / torch.linalg.vector_norm(G.double())
+    X = X.t().contiguous() if rows > cols else X
+    for _ in range(3):
+        A = torch.mm(X, X.t().contiguous())
+        X = QUINTIC[0] * X + torch.mm(QUINTIC[1] * A + QUINTIC[2] * torch.mm(A, A), X)
+    X = X.t() if rows > cols else X
+    y = som.som_orthogonalise(G, 3)
+    assert float((y.double() - X).norm() / X.norm()) <= WITHIN
+    # everywhere alike: no block of 32 x 32 has more than its share (a wrong one is off by its whole size,
+    # an element by 2^-8 of itself and the typical error five times over)
+    bad = (y.double() - X).abs() > 2.0 ** -8 * X.abs() + 5 * WITHIN * float(X.norm()) / (rows * cols) ** 0.5
+    assert int(bad.sum()) <= 1e-4 * rows * cols and not bool(_blocks_mean(bad.float()).gt(0.1).any())
+
+
+def _blocks_mean(v):
+    return torch.nn.functional.avg_pool2d(v[None, None], 32, ceil_mode=True, count_include_pad=False)[0, 0]
 
 
 def test_refusals():
