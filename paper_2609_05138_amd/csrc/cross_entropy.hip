@@ -16,7 +16,7 @@
 // and give its part of dW.  A row of g sums to zero, so what all classes' weights have in common (a
 // codebook's are positive, with a mean far from zero) cancels in dx, but not what g's rounding does
 // to it: that is the row's sum of roundings times the common part, which is added back (with the
-// mean of up to 256 classes in its place; without it dx of a codebook of [0, 1) is 2.1 times as far
+// mean of up to 64 classes in its place; without it dx of a codebook of [0, 1) is 2.1 times as far
 // from 64 bits as its own rounding, with it 1.4 times, as where nothing is in common).  g is scaled
 // by a power of two that dloss's largest value sets, so that fp16 holds what a mean over many rows
 // gives (1 / M times a probability).
@@ -141,7 +141,6 @@ struct GradHead {
   int32_t swap;              // 1: a row that counts for nothing holds a NaN or an infinity
 };
 constexpr int kScanGroups = 512;       // and as many flags
-constexpr int64_t kMostCommon = 256;
 
 // A row counts for nothing.
 __device__ __forceinline__ bool no_row(const GradCall& c, int64_t i) {
@@ -174,24 +173,37 @@ __device__ void grad_head(const GradCall& c, int bits, GradHead* head, uint32_t*
   head->inverse = ldexpf(1.0f, -e);
 }
 
-// common[k] = the mean of up to 256 classes' weights, spread over all classes; a feature a wave.
+// common[k] = the mean weight of up to 64 classes, spread over all that are not left out; a feature a wave,
+// a class a lane.  It is 0 where it is smaller than the weights' mean distance from it (what they have
+// by chance, or a few large ones make; not taking it back adds half to the error's square at the
+// most), and where it is further than 0 from the classes that as many documents are labelled with
+// (those whose bias leaves them no document may have any weights).
 template <typename T>
 __device__ void grad_common(const GradCall& c, int64_t group, float* common) {
   const T* const W = static_cast<const T*>(c.W);
   const int64_t k = group * 16 + (threadIdx.x >> 6);
   if (k >= c.K) return;
-  const int64_t some = c.N < kMostCommon ? c.N : kMostCommon;
-  float s = 0.0f;
+  const int lane = threadIdx.x & 63;
+  auto weight = [&](int64_t n) { return static_cast<float>(c.units ? W[n * c.ldw + k] : W[k * c.ldw + n]); };
+  auto spread = [&](int64_t all) { return all > 64 ? lane * all / 64 : lane < all ? lane : 0; };
+  const int64_t one = spread(c.N), i = spread(c.M);
+  const bool own = lane < c.M && !no_row(c, i), in = lane < c.N && !(c.bias && c.bias[one] == -INFINITY);
+  const float w = weight(one), v = weight(own ? c.labels[i] : 0);
+  float n = in ? 1.0f : 0.0f, s = in ? w : 0.0f;
 #pragma unroll
-  for (int d = 0; d < kMostCommon / 64; ++d) {
-    const int64_t at = d * 64 + (threadIdx.x & 63), n = at * c.N / some;
-    if (at < some) s += static_cast<float>(c.units ? W[n * c.ldw + k] : W[k * c.ldw + n]);
+  for (int off = 32; off; off >>= 1) {
+    n += __shfl_xor(n, off, 64);
+    s += __shfl_xor(s, off, 64);
   }
+  s /= n;
+  float more = in ? fabsf(s) - fabsf(w - s) : 0.0f, nearer = own ? fabsf(v) - fabsf(v - s) : 0.0f;
 #pragma unroll
-  for (int off = 32; off; off >>= 1) s += __shfl_xor(s, off, 64);
-  s /= static_cast<float>(some);
-  // (weights that are not finite make NaNs of what they reach, and no more than that)
-  if ((threadIdx.x & 63) == 0) common[k] = fabsf(s) < INFINITY ? s : 0.0f;
+  for (int off = 32; off; off >>= 1) {
+    more += __shfl_xor(more, off, 64);
+    nearer += __shfl_xor(nearer, off, 64);
+  }
+  // (of weights that are not finite both are NaN: they make NaNs of what they reach, and no more than that)
+  if (lane == 0) common[k] = more > 0.0f && nearer > 0.0f ? s : 0.0f;
 }
 
 // Looks through the rows of x that count for nothing, a wave a row; a flag a workgroup.

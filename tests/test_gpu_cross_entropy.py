@@ -207,6 +207,58 @@ def test_what_rounding_takes_from_a_codebooks_gradient_comes_back(M, N, K, pad, 
     assert _far((2.0 * t * torch.mm(rounded, W64.t().contiguous())).to(T[kind]), want) > 1.9 * own
 
 
+def _left_out(M, N, K, kind, layout, out, junk, mask, seed=0):
+    """dx, dW and dbias where the classes `out` have a bias of `mask` and weights of `junk`, and the same in 64
+    bits of the other classes alone (placed among zeros)."""
+    x, W, labels, bias, dloss = _inputs(M, N, K, kind, layout, seed=seed, ignored=0.1)
+    inside = torch.nonzero(~out)[:, 0].int()
+    labels = torch.where((labels >= 0) & (labels < N), inside[labels.clamp(0, N - 1).long() % len(inside)], labels)
+    bias[out] = mask
+    W[:, out] = junk
+    lse = som.som_cross_entropy(x, W, labels, bias)[1]
+    got = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias)
+    number = torch.full((N,), -1, dtype=torch.int32, device=DEV)
+    number[inside.long()] = torch.arange(len(inside), dtype=torch.int32, device=DEV)
+    has = (labels >= 0) & (labels < N)
+    mine = torch.where(has, number[labels.clamp(0, N - 1).long()], -1)
+    want = _double(x, W[:, ~out], mine, bias[~out], 1.0, dloss)
+    dW, dbias = torch.zeros((K, N), dtype=torch.float64, device=DEV), torch.zeros(N, dtype=torch.float64, device=DEV)
+    dW[:, ~out], dbias[~out] = want[3], want[4]
+    return got, (want[2], dW, dbias)
+
+
+# (one launch of the scores, and a split k axis)
+@pytest.mark.parametrize("M,N,K", [(300, 1000, 128), (60, 700, 4096)])
+@pytest.mark.parametrize("layout", ["feature", "unit"])
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("mask", [float("-inf"), -1e30])
+def test_weights_of_classes_that_are_left_out_do_not_reach_dx(mask, kind, layout, M, N, K):
+    # the output's rounding and g's, each of its own size (see above): e sqrt(2), and less than 1.7 e
+    out = torch.arange(N, device=DEV) % 3 == 0
+    (dx, dW, dbias), want = _left_out(M, N, K, kind, layout, out, 2.0 ** 15, mask)
+    for got, w in ((dx, want[0]), (dW, want[1])):
+        assert _far(got, w) <= 1.7 * _far(w.to(T[kind]), w) + 2.0 ** -16
+    assert _far(dbias, want[2]) <= 2.0 ** -16
+
+
+@pytest.mark.parametrize("layout", ["feature", "unit"])
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+def test_a_class_of_large_weights_moves_its_own_documents_alone(kind, layout):
+    M, N, K = 400, 200, 96
+    x, W, labels, bias, dloss = _inputs(M, N, K, kind, layout, ignored=0.1)
+    labels = torch.where(labels == 77, 78, labels)
+    labels[9] = 77
+    W[:, 77] = 3e4
+    bias[77] = -1e9                                  # no other document's
+    dloss = dloss * M                                # (dx among fp16's normal numbers)
+    lse = som.som_cross_entropy(x, W, labels, bias)[1]
+    dx = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias)[0]
+    want = _double(x, W, labels, bias, 1.0, dloss)[2]
+    rest = torch.arange(M, device=DEV) != 9
+    assert _far(dx[rest], want[rest]) <= 1.7 * _far(want[rest].to(T[kind]), want[rest])
+    assert _far(dx[9:10], want[9:10]) <= 2 * HALF[kind]
+
+
 def test_gradients_against_differences():
     M, N, K = 6, 40, 16
     x, W, labels, bias, dloss = _inputs(M, N, K, "f16", "feature", ignored=0.0)
