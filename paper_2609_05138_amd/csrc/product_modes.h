@@ -276,14 +276,14 @@ __device__ __forceinline__ GradRow grad_row(const GradArgs& a, int64_t i, int64_
   return r;
 }
 
-// g times `factor` of eight columns from their sums, in place; a row without a label gives zeros
-// whatever its sums.
+// g times `factor` of eight columns from their sums, in place; a row without a label, and but for its
+// label's d a class that is left out, give zeros whatever their sums.
 __device__ __forceinline__ void grad8(const GradArgs& a, const GradRow& r, float factor, const float (&bias)[8],
                                       float (&v)[8]) {
   const float d = r.dloss * factor;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float p = __builtin_amdgcn_exp2f(kLog2e * fmaf(v[e], a.alpha, bias[e] - r.lse));
+    const float p = bias[e] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(kLog2e * fmaf(v[e], a.alpha, bias[e] - r.lse));
     v[e] = r.dloss == 0.0f ? 0.0f : r.label == e ? fmaf(d, p, -d) : d * p;
   }
 }
@@ -324,14 +324,17 @@ __device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a,
   const int64_t wave_j = tile.j0 + wj * TJ * 16, j = wave_j + g * 4;        // + y * 16 + e
   const float factor = *a.factor;
   float bias[TJ][4], sums[TJ][4];
+  bool gaps = false;         // there are classes that are left out (or none, past the last)
   const int left = static_cast<int>(min<int64_t>(a.J - wave_j, TJ * 16));
 #pragma unroll
   for (int y = 0; y < TJ; ++y)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       bias[y][e] = y * 16 + g * 4 + e >= left ? -INFINITY : a.bias ? a.bias[j + y * 16 + e] : 0.0f;
+      gaps |= bias[y][e] == -INFINITY;
       sums[y][e] = 0.0f;
     }
+  gaps = __any(gaps);
   // The rows' terms by way of LDS: one wait for all of them, and no registers.
   typedef float f3 __attribute__((ext_vector_type(3)));
   typedef __attribute__((address_space(3))) f3 lds_f3;
@@ -362,6 +365,12 @@ __device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a,
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         v[y][e] = d * __builtin_amdgcn_exp2f(kLog2e * fmaf(acc[x][y][e], a.alpha, bias[y][e] - lse));
+    if (gaps) {                          // zeros whatever the sums hold, infinities too
+#pragma unroll
+      for (int y = 0; y < TJ; ++y)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[y][e] = bias[y][e] == -INFINITY ? 0.0f : v[y][e];
+    }
     if (__any(here)) {
 #pragma unroll
       for (int y = 0; y < TJ; ++y)

@@ -241,6 +241,30 @@ def test_weights_of_classes_that_are_left_out_do_not_reach_dx(mask, kind, layout
     assert _far(dbias, want[2]) <= 2.0 ** -16
 
 
+# (one launch of the scores, and a split k axis; the last classes share their tile with none)
+@pytest.mark.parametrize("M,N,K", [(300, 1000, 128), (60, 701, 4096)])
+@pytest.mark.parametrize("layout", ["feature", "unit"])
+def test_scores_of_classes_that_are_left_out_may_overflow(layout, M, N, K):
+    x, W, labels, bias, dloss = _inputs(M, N, K, "bf16", layout, ignored=0.1)
+    out = (torch.arange(N, device=DEV) % 3 == 0) | (torch.arange(N, device=DEV) >= N - 5)
+    inside = torch.nonzero(~out)[:, 0].int()
+    labels = torch.where((labels >= 0) & (labels < N), inside[labels.clamp(0, N - 1).long() % len(inside)], labels)
+    labels[0] = 3                                    # a label that is left out
+    bias[out] = float("-inf")
+    W[:, out] = 0.0
+    want = som.som_cross_entropy(x, W, labels, bias)
+    want += som.som_cross_entropy_backward(dloss, x, W, labels, want[1], bias)
+    assert all(bool(t.isfinite().all()) for t in want[1:])
+    labels[0], W[:, out] = int(inside[0]), 3e38
+    want = som.som_cross_entropy(x, W, labels, bias)
+    assert all(bool(t.isfinite().all()) for t in want)
+    got = som.som_cross_entropy_backward(dloss, x, W, labels, want[1], bias)
+    W[:, out] = 0.0
+    want = som.som_cross_entropy_backward(dloss, x, W, labels, want[1], bias)
+    for a, b in zip(got, want):
+        assert bool(a.isfinite().all()) and torch.equal(a, b)
+
+
 @pytest.mark.parametrize("layout", ["feature", "unit"])
 @pytest.mark.parametrize("kind", ["f16", "bf16"])
 def test_a_class_of_large_weights_moves_its_own_documents_alone(kind, layout):
