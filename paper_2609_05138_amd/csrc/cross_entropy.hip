@@ -8,7 +8,7 @@
 // exp(v - m) (8 bytes for 256 or 128 scores), and the label's score; k_loss_join puts a row's
 // pairs together.  Where the k axis is split, or the kernels of few rows are faster, the scores go
 // through the workspace, as fp32, to k_loss_scores, which makes the pairs of 8,192 columns, or of up to
-// 32,768 the loss itself.
+// 16,384 the loss itself.
 //
 // Backward: the product again, a piece of the classes at a time: its epilogue makes g of the
 // piece, in x's type because the matrix cores take 16 bits (as som_product_backward's dP), and
@@ -19,12 +19,13 @@
 // mean of up to 64 classes in its place; without it dx of a codebook of [0, 1) is 2.1 times as far
 // from 64 bits as its own rounding, with it 1.4 times, as where nothing is in common).  g is scaled
 // by a power of two that dloss's largest value sets, so that fp16 holds what a mean over many rows
-// gives (1 / M times a probability).
+// gives (1 / M times a probability).  Classes that are left out, and documents that count for nothing, give
+// zeros to g whatever their scores.
 //
 // Bound: the matrix cores at the clock that power leaves them (8,192 x 4,096 x 65,536 in bf16 3,172
-// to 3,240 us, 1,360 to 1,390 TFLOP/s; gradients of 8,192 x 2,048 x 65,536 5,220 us, 1,260, of
+// to 3,270 us, 1,340 to 1,390 TFLOP/s; gradients of 8,192 x 2,048 x 65,536 5,120 to 5,280 us, 1,250 to 1,290, of
 // which the scores' third, whose epilogue makes and writes g, 40%); one row: the weights' bytes
-// (65,536 x 2,048 40 us, 6.7 TB/s, and 10 us for the two launches after it); small gradients: five
+// (65,536 x 2,048 40 us, 6.7 TB/s, feature-major 42, and 10 us for the two launches after it); small gradients: five
 // launches.
 #include "cross_entropy.h"
 
@@ -34,7 +35,9 @@ namespace som {
 namespace {
 
 constexpr int kScoreThreads = 1024, kScoreColumns = kScoreThreads * 8;   // of a pass of k_loss_scores
-constexpr int64_t kOneWorkgroup = 4 * kScoreColumns;     // a row of so many goes without k_loss_join
+// A row of so many goes without k_loss_join (one document, us, without and with it: 16,384 classes 15.8 and
+// 17.0, 24,576 21.0 and 20.7, 32,768 26.1 and 24.4, 65,536 46.9 and 40.5).
+constexpr int64_t kOneWorkgroup = 2 * kScoreColumns;
 constexpr int64_t kRowsAtOnce = 65536;         // forward: rows of one launch, for the pairs' room
 // Backward: a piece's g has 2^27 bytes, half of what the memory-side cache holds, but no fewer than
 // 8,192 classes, since dx's sums are read and written for each (8,192 x 2,048 x 65,536: pieces of

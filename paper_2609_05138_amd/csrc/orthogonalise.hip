@@ -39,8 +39,9 @@ namespace {
 
 constexpr int kParts = 512;            // sums of squares, one a workgroup
 // Up to this size the small products are taken (us a call, theirs and the large ones': 64 x 64 46
-// and 57, 512 x 512 82 and 92, 1,024 x 512 104 and 116; 1,024 x 1,024 272 and 151, 256 x 4,096 147
-// and 118, since their fragments come from the L2 64 bytes a row).
+// and 51, 512 x 512 81 and 86, 1,024 x 512 105 and 112): 2^19 elements are 512 tiles, two a CU.  One more
+// is a round more (640 x 832 149 and 112, 768 x 768 186 and 128, 1,024 x 1,024 272 and 150, 256 x 4,096
+// 147 and 118, since their fragments come from the L2 64 bytes a row).
 constexpr int64_t kSmall = 1 << 19, kSmallSide = 1024;
 constexpr int64_t kLowSide = 256;      // what rounding leaves of B is kept up to this (512 x 512: 82 us, with it 94)
 

@@ -15,12 +15,15 @@
 // lane.  A lane multiplies its sums of a row by one factor (Q's blocks of 128 units:
 // the wave's columns share theirs), or by the row's and by its columns' (blocks of one unit).
 //
-// Bound, large: the matrix cores at the clock that power leaves them (busy in 47% of the cycles, at
-// 2.0 GHz, of 8,192 x 4,096 x 16,384 with GELU and its argument kept), the sums' entering, and the
-// step's LDS reads (8,192^3 into bf16 450 to 484 us over the cards measured on, 2,270 to 2,440
-// TFLOP/s; a variant without the factors took 442 us where with them it was 500, on zeros 359 and
-// 391; with factors of columns 527 to 588; into fp32 903 to 942, 1,170 to 1,220); small, few rows:
-// as the product's (one row of 4,096 x 4,096 5.7 us of device time).
+// Bound, large: a step's matrix instructions and the sums' entering, which take turns more than they
+// overlap, and a tile's start and epilogue, which stand alone, since one workgroup fills a CU.  8,192 x
+// 4,096 x 16,384 into bf16 (268 MB) takes 504 us, with GELU 556; of k = 512 128 and 192: so some 9 us a tile
+// beside its steps (72 of the 504 us), GELU 6 to 8 more, and the rest steps of 1.7 us; the matrix cores are
+// busy in 47% of the cycles with GELU.  8,192^3 into bf16 450 to 507 us over the cards measured on, 2,170 to
+// 2,440 TFLOP/s; a variant without the factors took 442 us where with them it was 500, on zeros 359 and
+// 391.  Factors of columns: 526 to 588, since a sum is multiplied twice (a tile's matrix
+// instruction, four multiplications and four FMAs; else one and four).  Into fp32 903 to 942, 1,170 to
+// 1,220.  Small, few rows: as the product's (one row of 4,096 x 4,096 6 us of device time).
 #pragma once
 
 #include "product.h"

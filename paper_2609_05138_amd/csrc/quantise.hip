@@ -3,8 +3,9 @@
 //
 //   s = max |x| / 448 over the block,  q = x / s
 //
-// Bound: HBM (a maximum, a quotient and a conversion per element; 16,384 x 8,192 in bf16 76 us, 5.3
-// TB/s, a copy's rate; transposed 89 us, 4.5).  An element is read once and stays in registers
+// Bound: HBM (a maximum, a quotient and a conversion per element; 16,384 x 8,192 in bf16 72 to 77 us, 5.3
+// to 5.6 TB/s, a copy's rate; transposed 88 to 94 us, 4.3 to 4.6; blocks of 128 x 128 77 to 80, and
+// transposed 87 to 91).  An element is read once and stays in registers
 // while its block's maximum is made.
 //
 //   rows    a wave takes 512 columns (four blocks) of four rows, 16 lanes a block; the
