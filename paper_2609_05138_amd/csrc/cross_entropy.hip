@@ -152,7 +152,7 @@ __device__ __forceinline__ bool no_row(const GradCall& c, int64_t i) {
   return label < 0 || label >= c.N || lse == -INFINITY || dloss == 0.0f;
 }
 
-// Workgroup 0: the head.  dloss's largest value is had by one workgroup, so it needs no second
+// Workgroup 0: the head.  dloss's largest finite value is had by one workgroup, so it needs no second
 // launch (8,192 rows: 6 us).
 __device__ void grad_head(const GradCall& c, int bits, GradHead* head, uint32_t* tops) {
   uint32_t top = 0;
@@ -162,7 +162,7 @@ __device__ void grad_head(const GradCall& c, int bits, GradHead* head, uint32_t*
     for (int d = 0; d < 4; ++d) {
       const int64_t i = min(i0 + d * 1024, c.M - 1);
       const uint32_t size = __float_as_uint(c.dloss[i]) & 0x7fffffffu;
-      one[d] = no_row(c, i) ? 0 : size;
+      one[d] = no_row(c, i) || size >= 0x7f800000u ? 0 : size;     // (finite ones: the others keep their digits)
     }
 #pragma unroll
     for (int d = 0; d < 4; ++d) top = max(top, one[d]);
@@ -171,7 +171,7 @@ __device__ void grad_head(const GradCall& c, int bits, GradHead* head, uint32_t*
   if (threadIdx.x) return;
   const float most = __uint_as_float(top);
   int e = 0;
-  if (top && most < INFINITY) e = bits - min(max(ilogbf(most), -100), 100);
+  if (top) e = bits - min(max(ilogbf(most), -100), 100);
   head->factor = ldexpf(1.0f, e);
   head->inverse = ldexpf(1.0f, -e);
 }

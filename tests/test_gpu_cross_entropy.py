@@ -387,6 +387,23 @@ def test_small_gradients_reach_fp16():
         assert bool(b.any()) and bool(((a.double() * 2.0 ** -20).half().double() - b.double()).abs().max() <= 2.0 ** -24)
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_a_loss_gradient_that_is_not_finite_leaves_the_other_documents_their_digits(bad):
+    # (1 / 300 times a probability of 1 / 4096 is among fp16's last digits unless it is scaled)
+    M, N, K = 300, 4096, 64
+    x, W, labels, bias, dloss = _inputs(M, N, K, "f16", "unit", ignored=0.1)
+    labels[7] = 11
+    lse = som.som_cross_entropy(x, W, labels, bias)[1]
+    _, _, want, _, _ = _double(x, W, labels, bias, 1.0, dloss)
+    dloss[7] = bad
+    dx, _, _ = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias)
+    rest = torch.arange(M, device=DEV) != 7
+    # dx's rounding and g's (see above), and half of fp16's smallest step for each element of dx
+    least = 2.0 ** -25 * (want[rest].numel() ** 0.5) / float(want[rest].norm())
+    assert _far(dx[rest], want[rest]) <= 1.7 * _far(want[rest].half(), want[rest]) + least
+    assert not bool(dx[7].isfinite().any())
+
+
 def test_only_what_is_needed_and_given_outputs():
     M, N, K = 90, 333, 200
     x, W, labels, bias, dloss = _inputs(M, N, K, "bf16", "unit", pad=8)
