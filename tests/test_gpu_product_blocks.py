@@ -149,6 +149,57 @@ def test_codes_of_every_kind():
         assert bool(y[:, :w_rows].isnan().all()) and torch.equal(y[:, w_rows:], clean[:, w_rows:])
 
 
+def _cuts(x, sx, x_rows, W, sw, w_rows):
+    """The most that cutting takes from each sum: of eight consecutive k seven products (the largest has no
+    digits to lose: the codes' product has eight) by a unit each of 2^-13 of the power of two that the
+    largest pair of exponents gives, times the block's factors."""
+    M, K = x.shape
+    N = W.shape[1]
+
+    def powers(codes):
+        e = torch.floor(torch.log2(codes.double().abs().clamp(min=2.0 ** -6)))         # subnormal codes: the least
+        e = torch.where(codes.double() == 0, torch.full_like(e, -100.0), e)
+        return torch.nn.functional.pad(e, (0, -K % 8), value=-100.0).view(len(e), -1, 8)
+
+    a, b = powers(x), powers(W.t())
+    cut = torch.zeros((M, N), dtype=torch.float64, device=DEV)
+    for group in range(a.shape[1]):
+        largest = (a[:, None, group] + b[None, :, group]).amax(2)
+        block = group * 8 // 128
+        factors = (sx.double()[torch.arange(M, device=DEV) // x_rows, block][:, None]
+                   * sw.double()[torch.arange(N, device=DEV) // w_rows, block][None])
+        cut += 7 * 2.0 ** -13 * torch.exp2(largest) * factors
+    return cut
+
+
+@pytest.mark.parametrize("out", ["bf16", "f16"])
+@pytest.mark.parametrize("w_rows", [128, 1])
+@pytest.mark.parametrize("kind", ["normal", "columns", "one column", "heavy", "few digits"])
+@pytest.mark.parametrize("M,N,K", [(90, 140, 14), (130, 70, 128), (64, 129, 1000)])
+def test_products_far_below_the_largest_of_eight_are_cut_as_documented(M, N, K, kind, w_rows, out):
+    rng = np.random.default_rng(M + N + K)
+    x, W = rng.normal(size=(M, K)), rng.normal(size=(N, K))
+    if kind == "columns":
+        x *= np.exp(2.0 * rng.normal(size=(1, K)))
+    elif kind == "one column":
+        x[:, ::16] *= 300.0
+    elif kind == "heavy":
+        x, W = rng.standard_t(1.5, size=(M, K)), rng.standard_t(1.5, size=(N, K))
+    elif kind == "few digits":             # the sum is what is left of two large products
+        x[:, 0::8], x[:, 1::8] = 1000.0, 1000.0
+        W[:, 1::8] = -W[:, 0::8][:, :W[:, 1::8].shape[1]]
+    qx, sx = som.som_quantise(torch.as_tensor(x, dtype=torch.float32, device=DEV))
+    qW, sW = som.som_quantise(torch.as_tensor(W, dtype=torch.float32, device=DEV) * K ** -0.5, w_rows)
+    y, _, calc = _want(qx, sx, qW.t(), sW, 1, w_rows, 1.0, "f32", False)
+    cut = _np(_cuts(qx, sx, 1, qW.t(), sW, w_rows))
+    got = som.som_product_blocks(qx, sx, qW.t(), sW, dtype=T[out], alpha=2.0 ** -8)
+    want = y / 256
+    _near(got, want, (cut + calc) / 256 * (1 + HALF[out]) + np.abs(want) * HALF[out] + TINY[out])
+    # into fp32 nothing is cut
+    got = som.som_product_blocks(qx, sx, qW.t(), sW, dtype=torch.float32, alpha=2.0 ** -8)
+    _near(got, want, calc / 256 + np.abs(want) * HALF["f32"])
+
+
 def test_quantised_products_and_their_gradients():
     """Forward, dx and dW of a projection, all in blocks of 8 bits, against the same of the codes' values."""
     g = torch.Generator(device=DEV)
