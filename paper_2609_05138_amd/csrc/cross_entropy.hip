@@ -177,10 +177,10 @@ __device__ void grad_head(const GradCall& c, int bits, GradHead* head, uint32_t*
 }
 
 // common[k] = the mean weight of up to 64 classes, spread over all that are not left out; a feature a wave,
-// a class a lane.  It is 0 where it is smaller than the weights' mean distance from it (what they have
-// by chance, or a few large ones make; not taking it back adds half to the error's square at the
-// most), and where it is further than 0 from the classes that as many documents are labelled with
-// (those whose bias leaves them no document may have any weights).
+// a class a lane.  It is 0 where it is no more than the weights' mean distance from it and three
+// errors of a mean of n (what they have by chance, or a few large ones make; not taking it back adds
+// 0.6 to the error's square of 2 at the most), and where it is further than 0 from the classes that as
+// many documents are labelled with (those whose bias leaves them no document may have any weights).
 template <typename T>
 __device__ void grad_common(const GradCall& c, int64_t group, float* common) {
   const T* const W = static_cast<const T*>(c.W);
@@ -199,7 +199,8 @@ __device__ void grad_common(const GradCall& c, int64_t group, float* common) {
     s += __shfl_xor(s, off, 64);
   }
   s /= n;
-  float more = in ? fabsf(s) - fabsf(w - s) : 0.0f, nearer = own ? fabsf(v) - fabsf(v - s) : 0.0f;
+  const float times = 1.0f + 3.0f * rsqrtf(n);
+  float more = in ? fabsf(s) - times * fabsf(w - s) : 0.0f, nearer = own ? fabsf(v) - fabsf(v - s) : 0.0f;
 #pragma unroll
   for (int off = 32; off; off >>= 1) {
     more += __shfl_xor(more, off, 64);

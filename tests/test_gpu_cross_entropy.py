@@ -227,6 +227,19 @@ def _left_out(M, N, K, kind, layout, out, junk, mask, seed=0):
     return got, (want[2], dW, dbias)
 
 
+# (seeds whose weights' mean over the few classes is large by chance in some feature)
+@pytest.mark.parametrize("M,N,K,kind,layout,pad,spread,alpha,with_bias,seed", [
+    (117, 3, 411, "bf16", "feature", 8, 3.0, 1.0, True, 1534),
+    (510, 9, 320, "bf16", "unit", 3, 1.0, 2.0, True, 2012),
+    (257, 5, 4, "f16", "unit", 3, 3.0, 2.0, True, 9194),
+    (24, 6, 384, "bf16", "unit", 0, 3.0, 1.0, True, 8729),
+    (128, 12, 129, "f16", "unit", 1, 3.0, 2.0, True, 8479),
+])
+def test_few_classes_have_nothing_in_common_by_chance(M, N, K, kind, layout, pad, spread, alpha, with_bias, seed):
+    x, W, labels, bias, dloss = _inputs(M, N, K, kind, layout, pad=pad, seed=seed, spread=spread)
+    _check(x, W, labels, bias if with_bias else None, dloss, alpha, kind)
+
+
 # (one launch of the scores, and a split k axis)
 @pytest.mark.parametrize("M,N,K", [(300, 1000, 128), (60, 700, 4096)])
 @pytest.mark.parametrize("layout", ["feature", "unit"])
