@@ -608,7 +608,9 @@ som_status som_cross_entropy(const void* x, int64_t ldx, const void* W, int64_t 
  * dx and dW (laid out as W is) are of x's type, dbias is fp32; each may be NULL.  The scores
  * are calculated again, for a piece of the classes at a time (128 MB of g, or 8,192 classes); g
  * is rounded to x's type for the two products, scaled by a power of two so that fp16 holds a
- * mean's small values, and dbias sums it unrounded.  A document without a label, with dloss 0 or
+ * mean's small values, and dbias sums it unrounded.  dx and dW are then 1.4 to 1.5 times as far from
+ * exact ones (2-norm) as their own rounding; of up to 256 documents, where what rounding takes from the labels'
+ * entries of g is multiplied too, 1.1 times.  A document without a label, with dloss 0 or
  * with no class left gives zeros to everything, whatever its x holds, NaN too (the weights of
  * classes that are left out have to be finite).  lse has no gradient of its own.  No output
  * overlaps an input. With M == 0 dW and dbias are set to zero.  M up to 2^30.  ws:

@@ -34,7 +34,8 @@ struct GradCall {
 };
 // `clean`, `dx`: M rows of ldx; `g`: M rows of ldg, a piece of the classes
 struct GradWs {
-  size_t head, g, clean, dx, column, common, lost, flags, lost_part, partial, total;
+  size_t head, g, clean, dx, column, common, lost, flags, lost_part, rest, partial, total;
+  bool few;                  // what rounding takes from labels' entries is kept in `rest`
   int64_t piece, ldg, ldx, ld_column;
 };
 GradWs grad_ws(int64_t M, int64_t N, int64_t K, int elem);

@@ -22,11 +22,17 @@
 // gives (1 / M times a probability).  Classes that are left out, and documents that count for nothing, give
 // zeros to g whatever their scores.
 //
+// Most of a row of g is its label's entry, one rounding of which reaches all of the document's dx and of
+// the label's dW.  Over many documents that averages out to the above; of one dx and dW are 2 to 3 times as far
+// from 64 bits as their own rounding.  So of up to 256 what rounding takes from the labels' entries is kept: dx gets
+// it where its parts are joined, and dW's rows of these classes are made again, on the vector units: 1.1
+// times at the most (1 x 2,048 x 65,536 202 to 207 us, 128 documents 236 to 250, 64 x 512 x 637 32 to 39).
+//
 // Bound: the matrix cores at the clock that power leaves them (8,192 x 4,096 x 65,536 in bf16 3,172
 // to 3,270 us, 1,340 to 1,390 TFLOP/s; gradients of 8,192 x 2,048 x 65,536 5,120 to 5,280 us, 1,250 to 1,290, of
 // which the scores' third, whose epilogue makes and writes g, 40%); one row: the weights' bytes
 // (65,536 x 2,048 40 us, 6.7 TB/s, feature-major 42, and 10 us for the two launches after it); small gradients: five
-// launches.
+// launches, of few documents six.
 #include "cross_entropy.h"
 
 #include "product_modes.h"
@@ -144,6 +150,10 @@ struct GradHead {
   int32_t swap;              // 1: a row that counts for nothing holds a NaN or an infinity
 };
 constexpr int kScanGroups = 512;       // and as many flags
+// Documents whose labels' roundings are kept and multiplied.  More are within 1.51 of their own rounding
+// without (129 drawn sizes up to 256: 1.11 at the most; 70 larger ones: 1.51, two of them over 1.5), and
+// the classes that are made again take the square of the documents.
+constexpr int64_t kFewRows = 256;
 
 // A row counts for nothing.
 __device__ __forceinline__ bool no_row(const GradCall& c, int64_t i) {
@@ -174,6 +184,11 @@ __device__ void grad_head(const GradCall& c, int bits, GradHead* head, uint32_t*
   if (top) e = bits - min(max(ilogbf(most), -100), 100);
   head->factor = ldexpf(1.0f, e);
   head->inverse = ldexpf(1.0f, -e);
+}
+
+// No label's rounding is known yet.
+__device__ __forceinline__ void clear_rest(const GradCall& c, float* rest) {
+  if (threadIdx.x < c.M) rest[threadIdx.x] = 0.0f;
 }
 
 // common[k] = the mean weight of up to 64 classes, spread over all that are not left out; a feature a wave,
@@ -232,9 +247,10 @@ __device__ void grad_scan(const GradCall& c, int64_t group, int64_t groups, int3
 // weights, `scans` for the rows (the grid may hold more).
 template <typename T>
 __global__ void __launch_bounds__(1024) k_grad_prepare(const GradCall c, int bits, GradHead* head, int64_t commons,
-                                                       float* common, int64_t scans, int32_t* flags) {
+                                                       float* common, int64_t scans, int32_t* flags, float* rest) {
   __shared__ uint32_t tops[16];
   const int64_t g = group_index();
+  if (g == 0 && rest) clear_rest(c, rest);
   if (g == 0)
     grad_head(c, bits, head, tops);
   else if (g <= commons)
@@ -323,7 +339,16 @@ __global__ void __launch_bounds__(256) k_grad_scores(const GradArgs a) {
     if (n > 0) {
       float v[8];
       join8(a, row, col, v);
-      grad8(a, grad_row(a, row, col, true), factor, bias, v);
+      const GradRow r = grad_row(a, row, col, true);
+      grad8(a, r, factor, bias, v);
+      if (a.rest && r.label >= 0 && r.label < n) {
+        float own = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) own = r.label == e ? v[e] : own;
+        own = rest_of(a.elem, own);
+        a.rest[row] = own;
+        lost -= own;
+      }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float four[4], rounded = 0.0f;
@@ -354,6 +379,93 @@ __global__ void __launch_bounds__(256) k_grad_scores(const GradArgs a) {
       a.column_part[static_cast<int64_t>(blockIdx.y) * a.ld_column + at] =
           (sums[0][c] + sums[1][c] + sums[2][c] + sums[3][c]) / factor;
   }
+}
+
+// dW of the classes that few documents are labelled with, once more, from g as it was before its rounding in
+// the labels' entries: a workgroup a document (the first of its label works) and 512 features, a wave a
+// quarter of the documents.
+struct GradLabels {
+  const void* g;
+  const float* rest;
+  const GradHead* head;
+  int64_t ldg, first, classes, chunks;
+};
+template <typename T>
+__device__ void grad_labels(const GradCall& c, const GradLabels& l, int64_t at) {
+  constexpr int kBlocks = kFewRows / 64, kDeep = 8;      // of 64 documents; documents on their way
+  __shared__ __align__(16) float sums[4][512];
+  const T* const g = static_cast<const T*>(l.g);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m = static_cast<int>(at / l.chunks), M = static_cast<int>(c.M);
+  if (m >= M) return;
+  const int32_t label = c.labels[m];
+  const int64_t n = label - l.first, k = (at % l.chunks) * 512 + lane * 8;
+  if (label < 0 || n < 0 || n >= l.classes) return;
+  // every document's g for this class; the ones that are labelled with it
+  float own[kBlocks];
+  uint64_t mine[kBlocks];
+  int one = M;                         // the first of them
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b) {
+    const int i = b * 64 + lane;
+    const bool in = i < M;
+    const bool same = in && c.labels[in ? i : 0] == label && c.lse[in ? i : 0] != -INFINITY && c.dloss[in ? i : 0] != 0.0f;
+    own[b] = in ? static_cast<float>(g[i * l.ldg + n]) + (same ? l.rest[i] : 0.0f) : 0.0f;
+    mine[b] = __ballot(same);
+  }
+#pragma unroll
+  for (int b = kBlocks - 1; b >= 0; --b)
+    if (mine[b]) one = b * 64 + __builtin_ctzll(mine[b]);
+  if (one != m) return;
+  const int some = c.K - k >= 8 ? 8 : c.K > k ? static_cast<int>(c.K - k) : 0;
+  float s[8] = {};
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b) {
+    // (a document whose g is 0 counts for nothing, or as good as that, and may hold anything)
+    uint64_t left = __ballot(own[b] != 0.0f) & 0xffffull << 16 * wave;
+    while (left) {
+      float by[kDeep], v[kDeep][8];
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d) {
+        const int bit = left ? __builtin_ctzll(left) : 0;
+        by[d] = left ? __shfl(own[b], bit, 64) : 0.0f;
+        load8(static_cast<const T*>(c.x) + (b * 64 + bit) * c.ldx + k, left ? some : 0, v[d]);
+        left &= left - 1;
+      }
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = fmaf(by[d], v[d][e], s[e]);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[wave][lane * 8 + e] = s[e];
+  __syncthreads();
+  if (wave) return;
+  const float scale = c.alpha * l.head->inverse;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    for (int w = 1; w < 4; ++w) s[e] += sums[w][lane * 8 + e];
+    s[e] *= scale;
+  }
+  T* const dW = static_cast<T*>(c.dW);
+  if (c.units) {
+    store8(dW + label * c.lddw + k, some, s);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < some) dW[(k + e) * c.lddw + label] = static_cast<T>(s[e]);
+  }
+}
+
+// What follows the products of few documents, by workgroups: `joins` for dx, the rest for dW's labels.
+template <typename T>
+__global__ void __launch_bounds__(256) k_grad_few(const GradCall c, const ExtraArgs dx, int64_t joins, const GradLabels l) {
+  const int64_t g = group_index();
+  if (g < joins)
+    join_extra(dx, g * 256 + threadIdx.x);
+  else if (l.g)
+    grad_labels<T>(c, l, g - joins);
 }
 
 int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
@@ -440,6 +552,12 @@ GradWs grad_ws(int64_t M, int64_t N, int64_t K, int elem) {
   o += sizeof(int32_t) * kScanGroups;
   w.lost_part = o;                     // a wave's columns: 32 at the least
   o += align_up(sizeof(float) * M * ((w.piece + 255) / 256 * 8), 256);
+  w.few = M <= kFewRows;
+  w.rest = o;
+  if (w.few) {
+    o += align_up(sizeof(float) * M, 256);
+    need = most(need, static_cast<size_t>(M) * w.ldx);           // dx's sums go by way of the join
+  }
   w.partial = o;
   w.total = o + align_up(sizeof(float) * need, 256);
   return w;
@@ -523,7 +641,7 @@ static hipError_t prepare(const GradCall& c, const GradWs& w, void* ws, hipStrea
   const int64_t commons = c.dx ? (c.K + 15) / 16 : 0, scans = c.dW ? scan_groups(c.M) : 0;
   hipLaunchKernelGGL(k_grad_prepare<T>, groups_grid(1 + commons + scans), dim3(1024), 0, stream, c,
                      c.dtype == kF16 ? 14 : 0, at<GradHead>(ws, w.head), commons, at<float>(ws, w.common),
-                     scans, at<int32_t>(ws, w.flags));
+                     scans, at<int32_t>(ws, w.flags), w.few ? at<float>(ws, w.rest) : nullptr);
   return hipGetLastError();
 }
 
@@ -554,6 +672,18 @@ static hipError_t between(const GradCall& c, const GradWs& w, const GradArgs& a,
   const int64_t groups = b.columns + b.losts + scans;
   if (groups == 0) return hipSuccess;
   hipLaunchKernelGGL(k_grad_between<T>, groups_grid(groups), dim3(1024), 0, stream, c, b);
+  return hipGetLastError();
+}
+
+// `dx` (its product launched into parts) is nullptr where it is not needed, or summed up as it is.
+template <typename T>
+static hipError_t finish_few(const GradCall& c, const GradWs& w, const ExtraArgs* dx, int64_t first, int64_t classes, void* ws,
+                             hipStream_t stream) {
+  GradLabels l{};
+  if (c.dW) l = {at<const void>(ws, w.g), at<float>(ws, w.rest), at<GradHead>(ws, w.head), w.ldg, first, classes, (c.K + 511) / 512};
+  const int64_t joins = dx ? (join_threads(*dx) + 255) / 256 : 0, labels = c.dW ? c.M * l.chunks : 0;
+  if (joins + labels == 0) return hipSuccess;
+  hipLaunchKernelGGL(k_grad_few<T>, groups_grid(joins + labels), dim3(256), 0, stream, c, dx ? *dx : ExtraArgs{}, joins, l);
   return hipGetLastError();
 }
 
@@ -592,10 +722,11 @@ hipError_t launch_loss_back(const GradCall& c, void* ws, hipStream_t stream) {
     a.column_part = c.dbias ? at<float>(ws, w.column) : nullptr;
     a.ld_column = w.ld_column;
     a.lost_part = c.dx ? at<float>(ws, w.lost_part) : nullptr;
+    a.rest = w.few ? at<float>(ws, w.rest) : nullptr;
     a.dma = rows_on_16(a);
     const ProductPlan p = plan_extra(a.I, a.J, a.K, a.elem, true, a.q_kc, a.dma);
     set_launch(a, p, partial);
-    e = launch_mode(kGrad, p.shape, a, stream);
+    e = launch_mode(w.few ? kGradFew : kGrad, p.shape, a, stream);
     if (e != hipSuccess) return e;
     const int64_t strips = p.splits > 1 ? (n + kLostStrip - 1) / kLostStrip : int64_t(a.tiles_j) * kInfo[p.shape].waves_j;
     int64_t groups = a.tiles_i;
@@ -615,8 +746,29 @@ hipError_t launch_loss_back(const GradCall& c, void* ws, hipStream_t stream) {
     d.factor = &head->inverse;
     d.beta = 1.0f;
     d.res_type = kF32;
+    if (c.dW) {
+      ExtraArgs dw = d;
+      dw.P = c.units ? g : c.x;
+      dw.ldp = c.units ? w.ldg : c.ldx;
+      dw.p_kc = false;
+      dw.Q = c.units ? c.x : g;
+      dw.ldq = c.units ? c.ldx : w.ldg;
+      dw.q_kc = false;
+      dw.I = c.units ? n : c.K;
+      dw.J = c.units ? c.K : n;
+      dw.K = c.M;
+      dw.out = static_cast<char*>(c.dW) + dskip;
+      dw.ldo = c.lddw;
+      dw.out_type = c.dtype;
+      dw.swap = &head->swap;
+      dw.swapped = at<void>(ws, w.clean);
+      dw.ld_swapped = w.ldx;
+      dw.swap_p = !c.units;
+      e = launch_extra(dw, partial, stream);
+      if (e != hipSuccess) return e;
+    }
+    const bool last = n0 + n == c.N, parts = w.few && last;
     if (c.dx) {
-      const bool last = n0 + n == c.N;
       float* const sum = at<float>(ws, w.dx);
       d.P = g;
       d.ldp = w.ldg;
@@ -634,29 +786,19 @@ hipError_t launch_loss_back(const GradCall& c, void* ws, hipStream_t stream) {
       d.out_type = last ? c.dtype : kF32;
       d.row = at<float>(ws, w.lost);
       d.column = at<float>(ws, w.common);
-      e = launch_extra(d, partial, stream);
+      if (parts) {                     // every label's rounding is known by now
+        d.rest = a.rest;
+        d.labels = c.labels;
+        d.other = c.W;
+        d.ld_other = c.ldw;
+        d.other_units = c.units;
+      }
+      e = parts ? launch_parts(d, partial, stream) : launch_extra(d, partial, stream);
       if (e != hipSuccess) return e;
     }
-    if (c.dW) {
-      d.P = c.units ? g : c.x;
-      d.ldp = c.units ? w.ldg : c.ldx;
-      d.p_kc = false;
-      d.Q = c.units ? c.x : g;
-      d.ldq = c.units ? c.ldx : w.ldg;
-      d.q_kc = false;
-      d.I = c.units ? n : c.K;
-      d.J = c.units ? c.K : n;
-      d.K = c.M;
-      d.row = nullptr;
-      d.residual = nullptr;
-      d.out = static_cast<char*>(c.dW) + dskip;
-      d.ldo = c.lddw;
-      d.out_type = c.dtype;
-      d.swap = &head->swap;
-      d.swapped = at<void>(ws, w.clean);
-      d.ld_swapped = w.ldx;
-      d.swap_p = !c.units;
-      e = launch_extra(d, partial, stream);
+    if (w.few) {
+      const ExtraArgs* const dx = c.dx && parts ? &d : nullptr;
+      e = c.dtype == kF16 ? finish_few<f16>(c, w, dx, n0, n, ws, stream) : finish_few<bf16>(c, w, dx, n0, n, ws, stream);
       if (e != hipSuccess) return e;
     }
   }

@@ -821,7 +821,7 @@ struct No {
 
 // What becomes of a tile's sums: the epilogue of som_product, or one of product_modes.h,
 // which take more arguments.
-constexpr int kPlain = 0, kExtra = 1, kLoss = 2, kGrad = 3, kMirror = 4;
+constexpr int kPlain = 0, kExtra = 1, kLoss = 2, kGrad = 3, kMirror = 4, kGradFew = 5;
 template <int MODE>
 struct ModeArgs;
 template <>

@@ -1,5 +1,6 @@
 // The matrix product's kernel with epilogues of its own: sums and factors that stay on the
-// device (kExtra), of symmetric products (kMirror), and the two passes of cross entropy (kLoss, kGrad).
+// device (kExtra), of symmetric products (kMirror), and the two passes of cross entropy (kLoss, kGrad;
+// kGradFew, by itself so that its registers are not kGrad's, keeps what is rounded away from labels).
 #pragma once
 
 #include "product.h"
@@ -25,6 +26,13 @@ struct ExtraArgs : ProductArgs {
   const void* swapped;
   int64_t ld_swapped;
   bool swap_p;
+  // Row i gets rest[i] times class labels[i]'s weights too (other_units: [class][ld_other], else [..][ld_other]
+  // by class): what P has less than it should in that entry.  In the join: every tile leaves parts then.
+  const float* rest;         // or nullptr
+  const int32_t* labels;
+  const void* other;
+  int64_t ld_other;
+  bool other_units;
 };
 
 // Scores v = alpha sum + bias of rows against J classes; of each row in each tile the largest and
@@ -45,6 +53,9 @@ struct GradArgs : ProductArgs {
   float* column_part;        // [tiles_i][ld_column] or nullptr
   int64_t ld_column;
   float* lost_part;          // [strips][I] or nullptr
+  // [I]: what g's rounding takes from each row's label (kGradFew; not in lost_part then), or nullptr;
+  // not written where the label is none of these columns' classes
+  float* rest;
 };
 constexpr int kLostStrip = 512;        // columns of a strip where k_grad_scores makes g
 
@@ -64,6 +75,10 @@ template <>
 struct ModeArgs<kGrad> {
   typedef GradArgs type;
 };
+template <>
+struct ModeArgs<kGradFew> {
+  typedef GradArgs type;
+};
 
 // The plan of a kExtra product (no kernels of few rows), and the product with the join of a split
 // k axis.
@@ -72,6 +87,9 @@ inline RuledPlan plan_extra(int64_t I, int64_t J, int64_t K, int elem, bool p_kc
   return plan_product_by(I, J, K, elem, p_kc, q_kc, dma, {false, kShape256, symmetric});
 }
 hipError_t launch_extra(ExtraArgs a, float* partial, hipStream_t stream);
+// The product alone, of `a` with `rest`, into parts that join_extra, of its join_threads, puts together;
+// fills the launch's fields.
+hipError_t launch_parts(ExtraArgs& a, float* partial, hipStream_t stream);
 // The kernel alone; `a`, the mode's arguments, has its launch's fields.
 hipError_t launch_mode(int mode, int shape, const ProductArgs& a, hipStream_t stream);
 hipError_t launch_modes_f16(int mode, int shape, const ProductArgs& a, hipStream_t stream);
@@ -113,6 +131,28 @@ __device__ __forceinline__ void add_outer(const ExtraArgs& a, int64_t i, const f
   for (int e = 0; e < 8; ++e) v[e] = fmaf(r, column[e], v[e]);
 }
 
+__device__ __forceinline__ void add_rest(const ExtraArgs& a, int64_t i, int64_t j, int n, float (&v)[8]) {
+  const float r = a.rest[i];
+  if (r == 0.0f) return;               // (also where there is no label)
+  const int64_t label = a.labels[i];
+  auto add = [&](auto type) __attribute__((always_inline)) {
+    const auto* const W = static_cast<const decltype(type)*>(a.other);
+    float w[8];
+    if (a.other_units) {
+      load8(W + label * a.ld_other + j, n, w);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = e < n ? static_cast<float>(W[(j + e) * a.ld_other + label]) : 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = fmaf(r, w[e], v[e]);
+  };
+  if (a.elem == kF16)
+    add(f16{});
+  else
+    add(bf16{});
+}
+
 template <bool kWhole>
 __device__ __forceinline__ void finish_extra(const ExtraArgs& a, int64_t i, int64_t j, int n, float (&v)[8],
                                              const RowTerms& r) {
@@ -141,12 +181,33 @@ __device__ __forceinline__ void finish8_extra(const ExtraArgs& a, int64_t i, int
     finish_extra<false>(a, i, j, n, v, r);
 }
 
+__device__ __forceinline__ float extra_scale(const ExtraArgs& a);
+
+// Eight columns of C from their parts: of the at'th thread.
+inline int64_t join_threads(const ExtraArgs& a) { return (a.J + 7) / 8 * a.I; }
+__device__ __forceinline__ void join_extra(const ExtraArgs& a, int64_t at) {
+  const int64_t groups = (a.J + 7) / 8;
+  if (at >= groups * a.I) return;
+  const int64_t i = at / groups, j = at % groups * 8;
+  const int n = static_cast<int>(min<int64_t>(8, a.J - j));
+  const RowTerms r = extra_terms(a, extra_scale(a), i, j, n);
+  float v[8];
+  join8(a, i, j, v);
+  if (a.row) {
+    float column[8];
+    load8(a.column + j, n, column);
+    add_outer(a, i, column, v);
+  }
+  if (a.rest) add_rest(a, i, j, n, v);
+  finish8_extra(a, i, j, n, v, r);
+}
+
 __device__ __forceinline__ float extra_scale(const ExtraArgs& a) { return a.factor ? a.alpha * *a.factor : a.alpha; }
 
 template <class TileOf, int TI, int TJ>
 __device__ __forceinline__ void extra_tile(const TileOf& tile, const ExtraArgs& a, const f4 (&acc)[TI][TJ],
                                            const TilePlace& place) {
-  if (a.splits > 1) return tile.part(a, acc, place.split);
+  if (a.splits > 1 || a.rest) return tile.part(a, acc, place.split);
   constexpr int kAhead = TileOf::kAhead;
   const float scale = extra_scale(a);
   auto terms = [&](int g) __attribute__((always_inline)) {
@@ -288,6 +349,11 @@ __device__ __forceinline__ void grad8(const GradArgs& a, const GradRow& r, float
   }
 }
 
+// What rounding to the operands' type takes from a value.
+__device__ __forceinline__ float rest_of(int elem, float v) {
+  return v - (elem == kF16 ? static_cast<float>(static_cast<f16>(v)) : static_cast<float>(static_cast<bf16>(v)));
+}
+
 // Four values rounded to the operands' type, as they are stored, and sum plus the rounded ones
 // (by the dot product with ones: two values an instruction).
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
@@ -315,7 +381,7 @@ __device__ __forceinline__ u2 round4(int elem, const float (&v)[4], float* sum) 
 // Straight from the matrix instructions' registers, as loss_tile: a lane has four consecutive classes
 // of a row in each of TJ places.  v - lse is alpha sum + (bias - lse), rounded at its own size, since
 // it is an exponent; the label's class is looked for once a row and wave.
-template <class TileOf, int TI, int TJ>
+template <bool FEW, class TileOf, int TI, int TJ>
 __device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a, const f4 (&acc)[TI][TJ],
                                           const TilePlace& place) {
   if (a.splits > 1) return tile.part(a, acc, place.split);
@@ -358,8 +424,8 @@ __device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a,
     const f3 r = terms[row];
     const float lse = r[1], d = r[2];
     const int label = __float_as_int(r[0]) - wj * TJ * 16;
-    const bool none = d == 0.0f, here = label >= 0 && label < TJ * 16 && (label >> 2 & 3) == g;
-    float v[TJ][4], lost = 0.0f;
+    const bool none = d == 0.0f, here = !none && label >= 0 && label < TJ * 16 && (label >> 2 & 3) == g;
+    float v[TJ][4], lost = 0.0f, rest = 0.0f;
 #pragma unroll
     for (int y = 0; y < TJ; ++y)
 #pragma unroll
@@ -376,7 +442,9 @@ __device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a,
       for (int y = 0; y < TJ; ++y)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (here && label == y * 16 + g * 4 + e) v[y][e] -= d;
+          if (here && label == y * 16 + g * 4 + e) rest = v[y][e] -= d;
+      rest = FEW ? rest_of(a.elem, rest) : 0.0f;
+      if (FEW && here) a.rest[tile.i0 + row] = rest;
     }
     if (__any(none)) {                   // zeros whatever the sums hold
 #pragma unroll
@@ -397,7 +465,7 @@ __device__ __forceinline__ void grad_tile(const TileOf& tile, const GradArgs& a,
         asm volatile("" : "+v"(sums[y][e]));
       }
     }
-    lost -= rounded;
+    lost -= rounded + rest;
     // Of two places 16 columns apart the lanes of odd g give up the first and those of even g the
     // second, so that a lane has eight consecutive columns and a row's lanes 64 bytes.
 #pragma unroll
@@ -448,7 +516,7 @@ __device__ __forceinline__ void finish_mode(const TileOf& tile, const typename M
   else if constexpr (MODE == kLoss)
     loss_tile(tile, a, acc, place);
   else
-    grad_tile(tile, a, acc, place);
+    grad_tile<MODE == kGradFew>(tile, a, acc, place);
 }
 
 }  // namespace som

@@ -5,20 +5,7 @@ namespace som {
 namespace {
 
 __global__ void __launch_bounds__(256) k_join_extra(const ExtraArgs a) {
-  const int64_t groups = (a.J + 7) / 8;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (at >= groups * a.I) return;
-  const int64_t i = at / groups, j = at % groups * 8;
-  const int n = static_cast<int>(min<int64_t>(8, a.J - j));
-  const RowTerms r = extra_terms(a, extra_scale(a), i, j, n);
-  float v[8];
-  join8(a, i, j, v);
-  if (a.row) {
-    float column[8];
-    load8(a.column + j, n, column);
-    add_outer(a, i, column, v);
-  }
-  finish8_extra(a, i, j, n, v, r);
+  join_extra(a, static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x);
 }
 
 }  // namespace
@@ -34,9 +21,15 @@ hipError_t launch_extra(ExtraArgs a, float* partial, hipStream_t stream) {
   if (p.upper) return launch_mirror_f16(p.shape, a, stream);
   const hipError_t e = launch_mode(kExtra, p.shape, a, stream);
   if (e != hipSuccess || p.splits == 1) return e;
-  const int64_t groups = (a.J + 7) / 8 * a.I;
-  hipLaunchKernelGGL(k_join_extra, dim3(static_cast<uint32_t>((groups + 255) / 256)), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(k_join_extra, dim3(static_cast<uint32_t>((join_threads(a) + 255) / 256)), dim3(256), 0, stream, a);
   return hipGetLastError();
+}
+
+hipError_t launch_parts(ExtraArgs& a, float* partial, hipStream_t stream) {
+  a.dma = rows_on_16(a);
+  const RuledPlan p = plan_extra(a.I, a.J, a.K, a.elem, a.p_kc, a.q_kc, a.dma);
+  set_launch(a, p, partial);
+  return launch_mode(kExtra, p.shape, a, stream);
 }
 
 }  // namespace som

@@ -28,6 +28,7 @@ template <int E>
 hipError_t launch_mode_elem(int mode, int shape, const ProductArgs& a, hipStream_t stream) {
   if (mode == kExtra) return launch_layout<E, kExtra>(shape, static_cast<const ModeArgs<kExtra>::type&>(a), stream);
   if (mode == kLoss) return launch_layout<E, kLoss>(shape, static_cast<const ModeArgs<kLoss>::type&>(a), stream);
+  if (mode == kGradFew) return launch_layout<E, kGradFew>(shape, static_cast<const ModeArgs<kGradFew>::type&>(a), stream);
   return launch_layout<E, kGrad>(shape, static_cast<const ModeArgs<kGrad>::type&>(a), stream);
 }
 

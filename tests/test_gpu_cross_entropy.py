@@ -296,6 +296,37 @@ def test_a_class_of_large_weights_moves_its_own_documents_alone(kind, layout):
     assert _far(dx[9:10], want[9:10]) <= 2 * HALF[kind]
 
 
+# (documents up to the most whose labels' roundings are kept, and one more; classes that several documents are
+# labelled with; split axes, and more than one piece of the classes)
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("layout", ["feature", "unit"])
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("M,N,K", [(1, 900, 700), (2, 5000, 520), (5, 3001, 333), (17, 700, 2000), (64, 640, 1280),
+                                   (100, 40000, 64), (150, 500000, 24), (255, 2000, 6000), (256, 1120, 512), (257, 3000, 128)])
+def test_gradients_of_few_documents_are_as_near_as_their_rounding(M, N, K, pad, layout, kind):
+    """A document's g is mostly its label's entry, one rounding of which reaches all of its row of dx and of
+    its class in dW: of few documents these do not average out (two times the outputs' own rounding for one). Kept
+    and multiplied, they leave the other entries', whose sum of squares is below a hundredth of the label's here (more
+    than 600 classes, scores within 4 of each other): sqrt(1 + 0.01) of the own rounding, which of K and more
+    elements is known within a tenth.  More documents go without: sqrt(2), within 1.55."""
+    x, W, labels, bias, dloss = _inputs(M, N, K, kind, layout, pad=pad, seed=5, ignored=0.0 if M < 5 else 0.1)
+    labels[M // 2:] = torch.where(labels[M // 2:] >= 0, labels[M // 2:] % max(1, N // 3), -1)
+    if M > 20:
+        labels[10:20] = 7                             # a class of many documents
+    if M < 5:
+        labels = labels.clamp(0, N - 1)
+    dloss = dloss * M
+    lse = som.som_cross_entropy(x, W, labels, bias)[1]
+    got = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias)
+    want = _double(x, W, labels, bias, 1.0, dloss)[2:]
+    limit = 1.11 if M <= 256 else 1.55
+    for a, w in zip(got[:2], want[:2]):
+        assert _far(a, w) <= limit * _far(w.to(T[kind]), w), (_far(a, w), _far(w.to(T[kind]), w))
+    assert _far(got[2], want[2]) <= 2.0 ** -16
+    again = som.som_cross_entropy_backward(dloss, x, W, labels, lse, bias)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
 def test_gradients_against_differences():
     M, N, K = 6, 40, 16
     x, W, labels, bias, dloss = _inputs(M, N, K, "f16", "feature", ignored=0.0)
